@@ -14,7 +14,8 @@
  *   avmp_translate   handle -> (pool, physical offset);
  *   avmp_gather_kv   paged gather of one attention layer into ragged batch buffers;
  *   avmp_gather_ssm  gather of one SSM layer's state blocks into batch buffers;
- *   avmp_scatter_*   the matching write side.
+ *   avmp_scatter_*   the matching write side;
+ *   avmp_ssm_*       the linear recurrence on the SSM blocks where they lie (prompts, single tokens).
  *
  * Conventions
  *   - "d_" arguments are DEVICE pointers, "h_" arguments are HOST pointers.
@@ -72,7 +73,8 @@ enum { AVMP_FSM_BALANCED = 0, AVMP_FSM_KV_PRESSURED = 1, AVMP_FSM_SSM_PRESSURED 
 enum {
     AVMP_DEV_OK = 0,
     AVMP_DEV_BAD_HANDLE = 1,     /* translate: handle does not resolve */
-    AVMP_DEV_BAD_REQUEST = 2,    /* gather / scatter: request slot out of range or holds nothing */
+    AVMP_DEV_BAD_REQUEST = 2,    /* gather / scatter / attn / ssm: request slot out of range or holds nothing,
+                                    or a row range that does not fit what it holds */
     AVMP_DEV_OUT_OVERFLOW = 3,   /* gather_kv: rows would pass out_capacity_tokens */
     AVMP_DEV_TIMEOUT = 4         /* a copy kernel gave up a bounded wait; the output is incomplete */
 };
@@ -321,6 +323,48 @@ AVMP_API int avmp_scatter_kv_layers(avmp_ctx *ctx, uint32_t first_layer, uint32_
 AVMP_API int avmp_scatter_ssm_layers(avmp_ctx *ctx, uint32_t first_layer, uint32_t n_layers, const uint32_t *d_reqs,
                                      uint32_t n_reqs, const void *d_in_state, uint64_t state_layer_stride_bytes,
                                      const void *d_in_conv, uint64_t conv_layer_stride_bytes, void *stream);
+
+/* ---- compute on the caches in place (no counterpart in the paper, which stops at the memory) ----
+ * The gathers above hand a model's kernels a dense copy of what they need; the entry points below
+ * are those kernels, reading pages and blocks where they lie, so a step touches its cache once.
+ * All rows ("tokens") of a batch are packed; a row stride of 0 in a descriptor means densely packed
+ * rows.  Pointers to rows must be 16-byte aligned and row strides multiples of 16 bytes (decays: 4).
+ * Outputs must not overlap inputs.  Nothing is allocated: where a call needs scratch it takes a caller's
+ * buffer, whose content need not be preserved and which two calls may share if they cannot overlap
+ * on the GPU.  An item that only the device can see to be wrong (see each call) is skipped, its output
+ * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST. */
+enum { AVMP_TYPE_BF16 = 0, AVMP_TYPE_F16 = 1 };   /* type of input and output rows (and of cached K and V) */
+
+/* Linear attention with a decay for each head (the recurrence of a state-space layer), on the state
+ * elements of the SSM blocks, laid out [heads][dv][dk] in fp32 (ssm_elem_bytes 4, ssm_state_elems =
+ * heads * dv * dk):   S <- exp(g) S + v k^T,   out = S q.
+ * Rows: q and k [groups][dk], v and out [heads][dv], g (log decay, fp32) [heads]; head h reads group
+ * h / (heads / groups).  g of -inf clears the state.  Supported: dk 16, 32, 64 or 128, dv a multiple of
+ * 32, heads a multiple of groups; else AVMP_EINVAL.  The convolution window of the block is not touched. */
+typedef struct {
+    uint32_t type, heads, groups, dk, dv;
+    uint32_t rsvd;             /* 0 */
+    uint64_t q_stride_bytes, k_stride_bytes, v_stride_bytes, decay_stride_bytes, out_stride_bytes;
+} avmp_ssm_desc;
+
+/* Scratch bytes avmp_ssm_prompt needs for these sizes (may be 0). */
+AVMP_API size_t avmp_ssm_workspace_bytes(const avmp_ctx *ctx, const avmp_ssm_desc *desc, uint32_t n_reqs, uint32_t total_tokens);
+
+/* Whole prompts: rows d_cu[k] .. d_cu[k+1] are consecutive tokens of request d_reqs[k]; the state after the last
+ * of them is left in its block.  d_resume[k] != 0: start from the state in the block; 0, or d_resume NULL:
+ * from zero (a fresh block holds leftovers), so that a request without rows gets a zero state.
+ * Skipped items: a slot that is not LIVE, a slot that an earlier entry of the list names, offsets that
+ * decrease or pass total_tokens.  n_reqs <= max_requests. */
+AVMP_API int avmp_ssm_prompt(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs,
+                             uint32_t n_reqs, const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume,
+                             const void *d_q, const void *d_k, const void *d_v, const float *d_log_decay, void *d_out,
+                             void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* One token per request: row k belongs to d_reqs[k].  Skipped items: a slot that is not LIVE, a slot that an
+ * earlier entry of the list names.  n_reqs <= max_requests. */
+AVMP_API int avmp_ssm_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs,
+                           uint32_t n_reqs, const void *d_q, const void *d_k, const void *d_v, const float *d_log_decay,
+                           void *d_out, void *stream);
 
 /* Counters -> host.  Synchronises the stream. */
 AVMP_API int avmp_get_stats(avmp_ctx *ctx, avmp_stats *h_out, void *stream);

@@ -71,6 +71,12 @@ class avmp_session_stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in SESSION_STAT_FIELDS]
 
 
+class avmp_ssm_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "heads", "groups", "dk", "dv", "rsvd")] + \
+               [(n, C.c_uint64) for n in ("q_stride_bytes", "k_stride_bytes", "v_stride_bytes", "decay_stride_bytes",
+                                          "out_stride_bytes")]
+
+
 _u32p = C.POINTER(C.c_uint32)
 
 
@@ -121,6 +127,10 @@ def _load():
         "avmp_scatter_ssm": (C.c_int, [vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp]),
         "avmp_scatter_kv_layers": (C.c_int, [vp, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp, C.c_uint64, vp]),
         "avmp_scatter_ssm_layers": (C.c_int, [vp, C.c_uint32, C.c_uint32, vp, C.c_uint32, vp, C.c_uint64, vp, C.c_uint64, vp]),
+        "avmp_ssm_workspace_bytes": (C.c_size_t, [vp, C.POINTER(avmp_ssm_desc), C.c_uint32, C.c_uint32]),
+        "avmp_ssm_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_ssm_desc), vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp, vp,
+                                      vp, vp, vp, C.c_size_t, vp]),
+        "avmp_ssm_step": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_ssm_desc), vp, C.c_uint32, vp, vp, vp, vp, vp, vp]),
         "avmp_get_stats": (C.c_int, [vp, C.POINTER(avmp_stats), vp]),
         "avmp_clear_error": (C.c_int, [vp, vp]),
         "avmp_export_tables": (C.c_int, [vp, C.POINTER(avmp_tables), vp]),
@@ -358,6 +368,33 @@ def avmp_scatter_ssm_layers(ctx, first_layer, n_layers, d_reqs, n_reqs, d_in_sta
                                        _stream(stream)), "avmp_scatter_ssm_layers")
 
 
+_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def ssm_desc(*, heads: int, groups: int, dk: int, dv: int, dtype: torch.dtype, q_stride_bytes: int = 0, k_stride_bytes: int = 0,
+             v_stride_bytes: int = 0, decay_stride_bytes: int = 0, out_stride_bytes: int = 0) -> avmp_ssm_desc:
+    if dtype not in _TYPES:
+        raise AvmpError(f"ssm_desc: {dtype} is not bfloat16 or float16")
+    return avmp_ssm_desc(_TYPES[dtype], heads, groups, dk, dv, 0, q_stride_bytes, k_stride_bytes, v_stride_bytes,
+                         decay_stride_bytes, out_stride_bytes)
+
+
+def avmp_ssm_workspace_bytes(ctx, desc: avmp_ssm_desc, n_reqs: int, total_tokens: int) -> int:
+    return lib.avmp_ssm_workspace_bytes(ctx, C.byref(desc), n_reqs, total_tokens)
+
+
+def avmp_ssm_prompt(ctx, ssm_layer, desc, d_reqs, n_reqs, d_cu, total_tokens, d_resume, d_q, d_k, d_v, d_log_decay, d_out,
+                    d_workspace, workspace_bytes, stream=None):
+    _check(lib.avmp_ssm_prompt(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_cu), total_tokens, _ptr(d_resume),
+                               _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_log_decay), _ptr(d_out), _ptr(d_workspace),
+                               workspace_bytes, _stream(stream)), "avmp_ssm_prompt")
+
+
+def avmp_ssm_step(ctx, ssm_layer, desc, d_reqs, n_reqs, d_q, d_k, d_v, d_log_decay, d_out, stream=None):
+    _check(lib.avmp_ssm_step(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_q), _ptr(d_k), _ptr(d_v),
+                             _ptr(d_log_decay), _ptr(d_out), _stream(stream)), "avmp_ssm_step")
+
+
 def avmp_get_stats(ctx, stream=None) -> dict:
     s = avmp_stats()
     _check(lib.avmp_get_stats(ctx, C.byref(s), _stream(stream)), "avmp_get_stats")
@@ -534,6 +571,17 @@ class Context:
 
     def scatter_ssm(self, layer, d_reqs, n, d_in_state, d_in_conv, stream=None):
         avmp_scatter_ssm(self.handle, layer, d_reqs, n, d_in_state, d_in_conv, stream)
+
+    def ssm_workspace_bytes(self, desc, n, total_tokens) -> int:
+        return avmp_ssm_workspace_bytes(self.handle, desc, n, total_tokens)
+
+    def ssm_prompt(self, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_q, d_k, d_v, d_log_decay, d_out,
+                   d_workspace=None, workspace_bytes=0, stream=None):
+        avmp_ssm_prompt(self.handle, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_q, d_k, d_v, d_log_decay,
+                        d_out, d_workspace, workspace_bytes, stream)
+
+    def ssm_step(self, layer, desc, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out, stream=None):
+        avmp_ssm_step(self.handle, layer, desc, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out, stream)
 
     def stats(self, stream=None) -> dict:
         return avmp_get_stats(self.handle, stream)

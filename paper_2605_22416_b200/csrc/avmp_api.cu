@@ -84,6 +84,39 @@ void fill_stats(const avmp_ctx *c, const DevState &d, avmp_stats *o)
     o->step_ns_migration_plan = (uint64_t)(d.cyc_mig * ns_per_cycle);
 }
 
+inline bool ssm_desc_ok(const avmp_ctx *c, const avmp_ssm_desc *d)
+{
+    if (!d || d->type > AVMP_TYPE_F16 || d->rsvd || c->spec.ssm_elem_bytes != 4 || c->spec.n_ssm_layers == 0) return false;
+    if (d->dk != 16 && d->dk != 32 && d->dk != 64 && d->dk != 128) return false;
+    if (d->dv == 0 || d->dv % 32 || d->heads == 0 || d->groups == 0 || d->heads % d->groups) return false;
+    if ((unsigned __int128)d->heads * d->dv * d->dk != c->spec.ssm_state_elems) return false;
+    const uint64_t qk = (uint64_t)d->groups * d->dk * 2, v = (uint64_t)d->heads * d->dv * 2;
+    auto stride_ok = [](uint64_t s, uint64_t row, uint64_t unit) { return s == 0 || (s >= row && s % unit == 0 && s < (1ull << 40)); };
+    return stride_ok(d->q_stride_bytes, qk, 16) && stride_ok(d->k_stride_bytes, qk, 16) && stride_ok(d->v_stride_bytes, v, 16) &&
+           stride_ok(d->out_stride_bytes, v, 16) && stride_ok(d->decay_stride_bytes, (uint64_t)d->heads * 4, 4);
+}
+
+SsmArgs ssm_args(const avmp_ssm_desc *d, uint32_t layer, const uint32_t *reqs, uint32_t n, const void *q, const void *k,
+                 const void *v, const float *decay, void *out)
+{
+    SsmArgs a = {};
+    a.layer = layer; a.n = n; a.heads = d->heads; a.groups = d->groups; a.dk = d->dk; a.dv = d->dv;
+    a.f16 = d->type == AVMP_TYPE_F16;
+    a.reqs = reqs;
+    a.q = static_cast<const uint8_t *>(q); a.k = static_cast<const uint8_t *>(k); a.v = static_cast<const uint8_t *>(v);
+    a.g = reinterpret_cast<const uint8_t *>(decay); a.out = static_cast<uint8_t *>(out);
+    const uint64_t qk = (uint64_t)d->groups * d->dk * 2, vr = (uint64_t)d->heads * d->dv * 2;
+    a.qs = d->q_stride_bytes ? d->q_stride_bytes : qk; a.ks = d->k_stride_bytes ? d->k_stride_bytes : qk;
+    a.vs = d->v_stride_bytes ? d->v_stride_bytes : vr; a.os = d->out_stride_bytes ? d->out_stride_bytes : vr;
+    a.gs = d->decay_stride_bytes ? d->decay_stride_bytes : (uint64_t)d->heads * 4;
+    return a;
+}
+
+bool ssm_rows_ok(const void *q, const void *k, const void *v, const float *decay, const void *out)
+{
+    return q && k && v && decay && out && !(((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) && !((uintptr_t)decay & 3);
+}
+
 // A snapshot is accepted only if the kernels could have produced it: they index the tables
 // without bounds checks, so a table that does not hang together must never reach the device.
 bool tables_consistent(const avmp_ctx *c, const avmp_tables *t)
@@ -492,6 +525,34 @@ int avmp_scatter_ssm_layers(avmp_ctx *c, uint32_t first_layer, uint32_t n_layers
     c->launches += 1;
     return cu(launch_ssm(c->g, true, first_layer, n_layers, d_reqs, n, const_cast<void *>(d_in_state),
                          state_layer_stride_bytes, const_cast<void *>(d_in_conv), conv_layer_stride_bytes, L(c, stream)));
+}
+
+size_t avmp_ssm_workspace_bytes(const avmp_ctx *, const avmp_ssm_desc *, uint32_t, uint32_t) { return 0; }
+
+int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n,
+                    const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume, const void *d_q, const void *d_k,
+                    const void *d_v, const float *d_log_decay, void *d_out, void *, size_t, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu || (((uintptr_t)d_reqs | (uintptr_t)d_cu | (uintptr_t)d_resume) & 3)) return AVMP_EINVAL;
+    if (total_tokens && !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
+    if ((uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
+    SsmArgs a = ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out);
+    a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
+    c->launches += 1;
+    return cu(launch_ssm_prompt(c->g, a, L(c, stream)));
+}
+
+int avmp_ssm_step(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n, const void *d_q,
+                  const void *d_k, const void *d_v, const float *d_log_decay, void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || ((uintptr_t)d_reqs & 3) || !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
+    if ((uint64_t)n * ((c->spec.ssm_state_elems + 1023u) / 1024u) >= (1ull << 31)) return AVMP_EINVAL;
+    c->launches += 1;
+    return cu(launch_ssm_step(c->g, ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out), L(c, stream)));
 }
 
 int avmp_get_stats(avmp_ctx *c, avmp_stats *h_out, void *stream)

@@ -201,6 +201,18 @@ cudaError_t launch_step_gather(const Geom &g, const uint32_t *reqs, uint32_t n, 
                                void *k, void *v, unsigned long long kv_layer_stride, unsigned long long cap_tokens,
                                uint32_t *cu_out, uint32_t ssm_layer0, uint32_t ssm_layers, void *state,
                                unsigned long long state_stride, void *conv, unsigned long long conv_stride, const Launch &l);
+// Linear recurrence on SSM blocks (avmp_ssm.cu).
+struct SsmArgs {
+    uint32_t layer, n, heads, groups, dk, dv, total;
+    bool f16;
+    const uint32_t *reqs, *cu, *resume;
+    const uint8_t *q, *k, *v;
+    const uint8_t *g;
+    uint8_t *out;
+    unsigned long long qs, ks, vs, gs, os;     // row strides in bytes
+};
+cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l);
+cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l);
 // Resolves the in-library scratch of avmp_gather_kv_static on the current device (= dev).
 cudaError_t static_gather_setup(int dev);
 

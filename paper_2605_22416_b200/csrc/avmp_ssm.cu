@@ -1,0 +1,518 @@
+// Linear attention with a decay for each head, on the state elements of the SSM blocks in place:
+//     S_t = exp(g_t) S_{t-1} + v_t k_t^T,   o_t = S_t q_t        (S: [dv][dk], fp32, one per request and head)
+//
+// ssm_step_kernel     one token per request: every state element is read once and written once, bound by HBM.
+// ssm_prompt_kernel   whole prompts by pieces of 64 tokens: inside a piece the recurrence is two triangular
+//                     products, between pieces only the state is carried.
+#include "avmp_dev.cuh"
+#include "avmp_mma.cuh"
+
+namespace avmp {
+
+namespace {
+
+// The block of d_reqs[k]'s layer, or null (dead slot, or named by an earlier entry of the list: two entries would
+// update one state at the same time).  Whole CTA; `report` tells which CTA of an item counts the error.
+__device__ __forceinline__ float *ssm_item(const Geom &g, const SsmArgs &a, uint32_t k, bool report)
+{
+    const uint32_t r = a.reqs[k];
+    uint32_t slot = kInvalid;
+    if (r < g.R) {
+        const uint32_t state = g.r_state[r], h = g.r_ssm[(unsigned long long)r * g.ns + a.layer];
+        if (state == AVMP_REQ_LIVE && h != kInvalid) slot = g.VT[1][h & 0x7FFFFFFFu];
+    }
+    bool dup = false;
+    for (uint32_t j = threadIdx.x; j < k; j += blockDim.x) dup |= a.reqs[j] == r;
+    dup = __syncthreads_or(dup);
+    if (slot == kInvalid || dup) {
+        if (report && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+        return nullptr;
+    }
+    return reinterpret_cast<float *>(unit_ptr(g, AVMP_POOL_SSM, slot));
+}
+
+// ---------------------------------------------------------------- one token
+constexpr int kStepCta = 256;
+constexpr uint32_t kStepTile = kStepCta * 4;      // state elements a CTA touches per round (a float4 per thread)
+constexpr int kStepRounds = 4;                    // rounds whose loads are in flight together
+
+template <class T, int DK>
+__global__ void __launch_bounds__(kStepCta)
+ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_elems)
+{
+    constexpr int LANES = DK / 4;                 // lanes that share a state row
+    pdl_prologue();
+    const uint32_t k = blockIdx.x / parts, part = blockIdx.x % parts;
+    float *S = ssm_item(g, a, k, part == 0);
+    if (!S) return;
+    const uint32_t elems = a.heads * a.dv * DK, rep = a.heads / a.groups;
+    const uint32_t end = min(elems, (part + 1) * part_elems);
+    const uint8_t *qrow = a.q + k * a.qs, *krow = a.k + k * a.ks;
+    const uint16_t *vrow = reinterpret_cast<const uint16_t *>(a.v + k * a.vs);
+    const float *grow = reinterpret_cast<const float *>(a.g + k * a.gs);
+    uint16_t *orow = reinterpret_cast<uint16_t *>(a.out + k * a.os);
+    const uint32_t col = (threadIdx.x * 4) % DK;
+    for (uint32_t e0 = part * part_elems + threadIdx.x * 4; e0 - threadIdx.x * 4 < end; e0 += kStepTile * kStepRounds) {
+        float4 s[kStepRounds];
+#pragma unroll
+        for (int u = 0; u < kStepRounds; ++u) {
+            const uint32_t e = e0 + u * kStepTile;
+            if (e < end) s[u] = __ldcs(reinterpret_cast<const float4 *>(S + e));
+        }
+#pragma unroll
+        for (int u = 0; u < kStepRounds; ++u) {
+            const uint32_t e = e0 + u * kStepTile;
+            float acc = 0.f;
+            uint32_t row = 0;
+            if (e < end) {
+                row = e / DK;
+                const uint32_t head = row / a.dv, grp = head / rep;
+                const uint2 kk = *reinterpret_cast<const uint2 *>(krow + (grp * DK + col) * 2);
+                const uint2 qq = *reinterpret_cast<const uint2 *>(qrow + (grp * DK + col) * 2);
+                const float2 k0 = T::unpack(kk.x), k1 = T::unpack(kk.y), q0 = T::unpack(qq.x), q1 = T::unpack(qq.y);
+                const float v = T::unpack(vrow[row]).x, w = expf(grow[head]);
+                // w == 0 clears the state, whatever it held
+                s[u].x = w == 0.f ? v * k0.x : fmaf(w, s[u].x, v * k0.x);
+                s[u].y = w == 0.f ? v * k0.y : fmaf(w, s[u].y, v * k0.y);
+                s[u].z = w == 0.f ? v * k1.x : fmaf(w, s[u].z, v * k1.x);
+                s[u].w = w == 0.f ? v * k1.y : fmaf(w, s[u].w, v * k1.y);
+                __stcs(reinterpret_cast<float4 *>(S + e), s[u]);
+                acc = s[u].x * q0.x + s[u].y * q0.y + s[u].z * q1.x + s[u].w * q1.y;
+            }
+#pragma unroll
+            for (int o = LANES / 2; o; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
+            if (e < end && col == 0) orow[row] = (uint16_t)T::pack(acc, 0.f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- whole prompts
+// One CTA per (request, head, 64 or 32 columns of dv).  Inside a piece of 64 tokens with running decays c_i,
+//     O = ((Q K^T) o D) V + diag(e^c) Q S^T,  D_ij = e^(c_i - c_j) for j <= i,
+//     S <- e^(c_64) S + sum_j e^(c_64 - c_j) v_j k_j^T.
+// Only the last line is sequential, and of it only the scaled sum: NT teams of four warps take the pieces in turn,
+// each works out its own products and waits for its predecessor's state alone, so that the loads, products and
+// exponentials of NT pieces overlap.  A named barrier per team carries the hand-over; there is no spinning.
+// What is rounded to 16 bits: the scores after their decay and the state as an operand of Q S^T (both enter an output
+// that is rounded to 16 bits itself).  The state's own update keeps 32 bits: e^(..) v_j is split into
+// 16-bit parts, two for fp16 and three for bf16 (k_j has 16 bits to begin with), 2^-23 relative, and summed in 32 bits.
+// fp16 has little range: its scores (per row) and states and updates (per 16 rows of S) carry a power of two each.
+constexpr int kC = 64;                            // tokens per piece
+
+template <int DK, int DVT, int NT>
+struct PromptSmem {
+    static constexpr int kQ = DK * 2 + 16;        // row strides: an odd number of 16-byte units, no bank conflicts
+    static constexpr int kV = DVT * 2 + 16;
+    static constexpr int kStageQ = 0, kStageK = kC * kQ, kStageV = 2 * kC * kQ, kStageG = kStageV + kC * kV;
+    static constexpr int kStage = kStageG + kC * 4;
+    static constexpr int kBufs = DK == 128 ? 1 : 2;          // loads run one piece ahead where the memory allows it
+    static constexpr int kRing = NT + 2;          // copies of the state in 16 bits: see the hand-over
+    static constexpr int kS = DVT * kQ;
+    static constexpr int kO = kC * kV;            // output staging
+    static constexpr int kF = DVT * DK * 4;       // the state in 32 bits, thread-private places
+    static constexpr int kW = kC * 2 * 4;         // running decays and tail weights
+    static constexpr int oStage = 0;
+    static constexpr int oS = oStage + NT * kBufs * kStage;
+    static constexpr int oO = oS + kRing * kS;
+    static constexpr int oF = oO + NT * kO;
+    static constexpr int oW = oF + kF;
+    static constexpr int oScale = oW + NT * kW;
+    static constexpr int kTotal = oScale + kRing * 4 * 4;
+};
+
+// A power of two that brings `m` (>= 0) to about 2^13; 1 for zero.
+__device__ __forceinline__ float pow2_to_2_13(float m)
+{
+    int e = (int)(__float_as_uint(m) >> 23) - 127;
+    if (m == 0.f) e = 13;
+    e = max(-100, min(100, 13 - e));
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+template <class T, int DK, int DVT, int NT>
+__global__ void __launch_bounds__(NT * 128, 1)
+ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
+{
+    using L = PromptSmem<DK, DVT, NT>;
+    constexpr int KS = DK / 16;                   // k-steps of a product over dk
+    constexpr int NV = DVT / 8;                   // 8-column tiles of the output
+    constexpr int ND = DK / 8;                    // 8-column tiles of the state
+    constexpr int WM = DVT / 16;                  // warps of a team that own 16 rows of the state each
+    extern __shared__ __align__(128) uint8_t smem[];
+    pdl_prologue();
+    const uint32_t per_req = a.heads * tiles;
+    const uint32_t k = blockIdx.x / per_req, head = (blockIdx.x % per_req) / tiles, tile = blockIdx.x % tiles;
+    const bool lead = blockIdx.x % per_req == 0;
+    float *S = ssm_item(g, a, k, lead);
+    if (!S) return;
+    const uint32_t row0 = a.cu[k], row1 = a.cu[k + 1];
+    if (row1 < row0 || row1 > a.total) {
+        if (lead && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+        return;
+    }
+    const uint32_t len = row1 - row0, pieces = (len + kC - 1) / kC;
+    const bool resume = a.resume && a.resume[k];
+    const uint32_t grp = head / (a.heads / a.groups);
+    const int team = threadIdx.x / 128, tid = threadIdx.x % 128, w = tid / 32, lane = tid % 32;
+    const int lr = lane >> 2, lc = (lane & 3) * 2;
+    uint8_t *stage0 = smem + L::oStage + team * L::kBufs * L::kStage;
+    float *F = reinterpret_cast<float *>(smem + L::oF);
+    float *cs = reinterpret_cast<float *>(smem + L::oW + team * L::kW), *wt = cs + kC;
+    float *sscale = reinterpret_cast<float *>(smem + L::oScale);
+    S += ((unsigned long long)head * a.dv + tile * DVT) * DK;
+
+    const uint8_t *qg = a.q + grp * DK * 2, *kg = a.k + grp * DK * 2;
+    const uint8_t *vg = a.v + ((unsigned long long)head * a.dv + tile * DVT) * 2;
+    const uint8_t *gg = a.g + head * 4;
+    uint8_t *og = a.out + ((unsigned long long)head * a.dv + tile * DVT) * 2;
+
+    auto load = [&](uint32_t p, int buf) {
+        if (p < pieces) {
+            const uint32_t base = smem_u32(stage0 + buf * L::kStage);
+            const uint32_t t0 = p * kC;
+            constexpr int CK = DK / 8, CV = DVT / 8;       // 16-byte units per row
+            for (int i = tid; i < kC * CK; i += 128) {
+                const uint32_t t = i / CK, c = i % CK;
+                const bool ok = t0 + t < len;
+                const unsigned long long row = row0 + (ok ? t0 + t : 0u);
+                cp_async16(base + L::kStageQ + t * L::kQ + c * 16, qg + row * a.qs + c * 16, ok);
+                cp_async16(base + L::kStageK + t * L::kQ + c * 16, kg + row * a.ks + c * 16, ok);
+            }
+            for (int i = tid; i < kC * CV; i += 128) {
+                const uint32_t t = i / CV, c = i % CV;
+                const bool ok = t0 + t < len;
+                const unsigned long long row = row0 + (ok ? t0 + t : 0u);
+                cp_async16(base + L::kStageV + t * L::kV + c * 16, vg + row * a.vs + c * 16, ok);
+            }
+            if (tid < kC) {
+                const bool ok = t0 + tid < len;
+                cp_async4(base + L::kStageG + tid * 4, gg + (unsigned long long)(row0 + (ok ? t0 + tid : 0u)) * a.gs, ok);
+            }
+        }
+        cp_async_commit();
+    };
+
+    // Publishes a state fragment as the 16-bit operand of piece p.
+    auto publish = [&](const float (&f)[ND][4], uint32_t p) {
+        const uint32_t slot = p % L::kRing;
+        uint8_t *sb = smem + L::oS + slot * L::kS;
+        float sc = 1.f;
+        if (T::kF16) {
+            float m = 0.f;
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, fabsf(f[n][i]));
+            m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
+            sc = pow2_to_2_13(m);
+            if (lane == 0) sscale[slot * 4 + w] = 1.f / sc;
+        }
+#pragma unroll
+        for (int n = 0; n < ND; ++n) {
+            *reinterpret_cast<uint32_t *>(sb + (w * 16 + lr) * L::kQ + (n * 8 + lc) * 2) = T::pack(f[n][0] * sc, f[n][1] * sc);
+            *reinterpret_cast<uint32_t *>(sb + (w * 16 + lr + 8) * L::kQ + (n * 8 + lc) * 2) = T::pack(f[n][2] * sc, f[n][3] * sc);
+        }
+    };
+    auto store_state = [&](const float (&f)[ND][4]) {
+#pragma unroll
+        for (int n = 0; n < ND; ++n) {
+            *reinterpret_cast<float2 *>(S + (w * 16 + lr) * DK + n * 8 + lc) = make_float2(f[n][0], f[n][1]);
+            *reinterpret_cast<float2 *>(S + (w * 16 + lr + 8) * DK + n * 8 + lc) = make_float2(f[n][2], f[n][3]);
+        }
+    };
+
+    load(team, 0);
+    if (team == 0 && w < WM) {
+        float f[ND][4];
+#pragma unroll
+        for (int n = 0; n < ND; ++n) {
+            float2 x = make_float2(0.f, 0.f), y = x;
+            if (resume) {
+                x = *reinterpret_cast<const float2 *>(S + (w * 16 + lr) * DK + n * 8 + lc);
+                y = *reinterpret_cast<const float2 *>(S + (w * 16 + lr + 8) * DK + n * 8 + lc);
+            }
+            f[n][0] = x.x; f[n][1] = x.y; f[n][2] = y.x; f[n][3] = y.y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) F[(n * 4 + i) * (WM * 32) + tid] = f[n][i];
+        }
+        publish(f, 0);
+        if (pieces == 0 && !resume) store_state(f);
+    }
+    __syncthreads();
+
+    static_assert(NT >= 2, "the hand-over goes from one team to another");
+    constexpr int kTeamBar = 1 + NT;
+    int buf = 0;
+    for (uint32_t p = team; p < pieces; p += NT) {
+        if (L::kBufs == 2) { load(p + NT, buf ^ 1); cp_async_wait<1>(); } else cp_async_wait<0>();
+        uint8_t *st = stage0 + buf * L::kStage;
+        const uint32_t sq = smem_u32(st + L::kStageQ), sk = smem_u32(st + L::kStageK), sv = smem_u32(st + L::kStageV);
+        bar_sync(kTeamBar + team, 128);
+        if (w == 0) {
+            // running sums in units of log2: from the front for the decays, from the back for the tail weights
+            // (the weights of the state keep their relative precision that way)
+            const float *gs = reinterpret_cast<const float *>(st + L::kStageG);
+            constexpr float kLog2e = 1.4426950408889634f;
+            float g0 = gs[2 * lane] * kLog2e, g1 = gs[2 * lane + 1] * kLog2e;
+            // 2^-300 is 0 in 32 bits; -inf itself would make differences of sums undefined
+            g0 = g0 < -300.f ? -300.f : g0; g1 = g1 < -300.f ? -300.f : g1;
+            float f = g0 + g1, b = f;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float x = __shfl_up_sync(0xFFFFFFFFu, f, o), y = __shfl_down_sync(0xFFFFFFFFu, b, o);
+                if (lane >= o) f += x;
+                if (lane + o < 32) b += y;
+            }
+            float b_next = __shfl_down_sync(0xFFFFFFFFu, b, 1);
+            if (lane == 31) b_next = 0.f;
+            float f_prev = __shfl_up_sync(0xFFFFFFFFu, f, 1);
+            if (lane == 0) f_prev = 0.f;
+            cs[2 * lane] = f_prev + g0; cs[2 * lane + 1] = f;
+            wt[2 * lane] = exp2_approx(b_next + g1); wt[2 * lane + 1] = exp2_approx(b_next);
+        }
+        bar_sync(kTeamBar + team, 128);
+
+        // ---- scores of this warp's 16 rows against the tokens up to their own, decayed and rounded
+        uint32_t aq[KS][4];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + (w * 16 + (lane & 15)) * L::kQ + s * 32 + (lane >> 4) * 16);
+        const float c0 = cs[w * 16 + lr], c1 = cs[w * 16 + lr + 8];
+        float o[NV][4];
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+        float inv0 = 1.f, inv1 = 1.f;
+        {
+            float sc[8][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {           // 16 tokens at a time
+                if (j > w) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[2 * j][i] = sc[2 * j + 1][i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    uint32_t b[4];
+                    ldsm4(b, sk + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
+                    T::mma(sc[2 * j], aq[s], b[0], b[1]);
+                    T::mma(sc[2 * j + 1], aq[s], b[2], b[3]);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int t = j * 16 + h * 8 + lc;
+                    const float2 ct = *reinterpret_cast<const float2 *>(cs + t);
+                    float *x = sc[2 * j + h];
+                    const int i0 = w * 16 + lr, i1 = i0 + 8;
+                    x[0] = t <= i0 ? x[0] * exp2_approx(c0 - ct.x) : 0.f;
+                    x[1] = t + 1 <= i0 ? x[1] * exp2_approx(c0 - ct.y) : 0.f;
+                    x[2] = t <= i1 ? x[2] * exp2_approx(c1 - ct.x) : 0.f;
+                    x[3] = t + 1 <= i1 ? x[3] * exp2_approx(c1 - ct.y) : 0.f;
+                }
+            }
+            float s0 = 1.f, s1 = 1.f;
+            if (T::kF16) {
+                float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j <= 2 * w + 1) {
+                        m0 = fmaxf(m0, fmaxf(fabsf(sc[j][0]), fabsf(sc[j][1])));
+                        m1 = fmaxf(m1, fmaxf(fabsf(sc[j][2]), fabsf(sc[j][3])));
+                    }
+#pragma unroll
+                for (int x = 1; x < 4; x <<= 1) {
+                    m0 = fmaxf(m0, __shfl_xor_sync(0xFFFFFFFFu, m0, x));
+                    m1 = fmaxf(m1, __shfl_xor_sync(0xFFFFFFFFu, m1, x));
+                }
+                s0 = pow2_to_2_13(m0); s1 = pow2_to_2_13(m1);
+                inv0 = 1.f / s0; inv1 = 1.f / s1;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j > w) continue;
+                const uint32_t pa[4] = {T::pack(sc[2 * j][0] * s0, sc[2 * j][1] * s0), T::pack(sc[2 * j][2] * s1, sc[2 * j][3] * s1),
+                                        T::pack(sc[2 * j + 1][0] * s0, sc[2 * j + 1][1] * s0), T::pack(sc[2 * j + 1][2] * s1, sc[2 * j + 1][3] * s1)};
+#pragma unroll
+                for (int n = 0; n < NV / 2; ++n) {
+                    uint32_t b[4];
+                    ldsm4_t(b, sv + (j * 16 + (lane & 15)) * L::kV + n * 32 + (lane >> 4) * 16);
+                    T::mma(o[2 * n], pa, b[0], b[1]);
+                    T::mma(o[2 * n + 1], pa, b[2], b[3]);
+                }
+            }
+        }
+
+        // ---- this piece's own contribution to the state (16 rows of dv per owning warp)
+        float ds[ND][4];
+        float dinv = 1.f;
+        if (w < WM) {
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ds[n][i] = 0.f;
+            float xs = 1.f;
+            if (T::kF16) {
+                float m = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v[4];
+                    ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 x = T::unpack(v[i]), y = *reinterpret_cast<const float2 *>(wt + j * 16 + (i >> 1) * 8 + lc);
+                        m = fmaxf(m, fmaxf(fabsf(x.x * y.x), fabsf(x.y * y.y)));
+                    }
+                }
+                m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
+                xs = pow2_to_2_13(m);
+                dinv = 1.f / xs;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t v[4], hi[4], lo[4], lo2[4];
+                ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float2 x = T::unpack(v[i]);
+                    const float2 y = *reinterpret_cast<const float2 *>(wt + j * 16 + (i >> 1) * 8 + lc);
+                    x.x *= y.x * xs; x.y *= y.y * xs;
+                    hi[i] = T::pack(x.x, x.y);
+                    const float2 h = T::unpack(hi[i]);
+                    x.x -= h.x; x.y -= h.y;
+                    lo[i] = T::pack(x.x, x.y);
+                    const float2 m = T::unpack(lo[i]);
+                    lo2[i] = T::pack(x.x - m.x, x.y - m.y);
+                }
+#pragma unroll
+                for (int n = 0; n < ND / 2; ++n) {
+                    uint32_t b[4];
+                    ldsm4_t(b, sk + (j * 16 + (lane & 15)) * L::kQ + n * 32 + (lane >> 4) * 16);
+                    T::mma(ds[2 * n], hi, b[0], b[1]);
+                    T::mma(ds[2 * n + 1], hi, b[2], b[3]);
+                    T::mma(ds[2 * n], lo, b[0], b[1]);
+                    T::mma(ds[2 * n + 1], lo, b[2], b[3]);
+                    if (!T::kF16) {
+                        T::mma(ds[2 * n], lo2, b[0], b[1]);
+                        T::mma(ds[2 * n + 1], lo2, b[2], b[3]);
+                    }
+                }
+            }
+        }
+
+        // ---- hand-over: wait for the state in front of this piece, pass the one behind it on at once
+        if (p > 0) bar_sync(1 + team, 256);
+        if (w < WM) {
+            const float dec = exp2_approx(cs[kC - 1]);
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float *f = F + (n * 4 + i) * (WM * 32) + tid;
+                    const float add = T::kF16 ? ds[n][i] * dinv : ds[n][i];
+                    ds[n][i] = dec == 0.f ? add : fmaf(dec, *f, add);
+                    *f = ds[n][i];
+                }
+            if (p + 1 < pieces) publish(ds, p + 1); else store_state(ds);
+        }
+        if (p + 1 < pieces) bar_arrive(1 + (team + 1) % NT, 256);
+
+        // ---- what the earlier pieces add to the outputs
+        const float e0 = exp2_approx(c0), e1 = exp2_approx(c1);
+        const uint32_t sb = smem_u32(smem + L::oS + (p % L::kRing) * L::kS);
+#pragma unroll
+        for (int n = 0; n < NV / 2; ++n) {
+            float x[2][4] = {};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                uint32_t b[4];
+                ldsm4(b, sb + (n * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
+                T::mma(x[0], aq[s], b[0], b[1]);
+                T::mma(x[1], aq[s], b[2], b[3]);
+            }
+            const float sc = T::kF16 ? sscale[(p % L::kRing) * 4 + n] : 1.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float *y = o[2 * n + h];
+                const float z0 = e0 * sc, z1 = e1 * sc;
+                // a cleared state adds nothing, whatever it held
+                y[0] = y[0] * inv0 + (e0 == 0.f ? 0.f : x[h][0] * z0); y[1] = y[1] * inv0 + (e0 == 0.f ? 0.f : x[h][1] * z0);
+                y[2] = y[2] * inv1 + (e1 == 0.f ? 0.f : x[h][2] * z1); y[3] = y[3] * inv1 + (e1 == 0.f ? 0.f : x[h][3] * z1);
+            }
+        }
+        // ---- rows out, whole 16-byte units
+        uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            *reinterpret_cast<uint32_t *>(so + lr * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][0], o[n][1]);
+            *reinterpret_cast<uint32_t *>(so + (lr + 8) * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][2], o[n][3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = lane; i < 16 * NV; i += 32) {
+            const uint32_t t = p * kC + w * 16 + i / NV, c = i % NV;
+            if (t < len)
+                *reinterpret_cast<uint4 *>(og + (unsigned long long)(row0 + t) * a.os + c * 16) =
+                    *reinterpret_cast<const uint4 *>(so + (i / NV) * L::kV + c * 16);
+        }
+        if (L::kBufs == 2) buf ^= 1;
+        bar_sync(kTeamBar + team, 128);             // the stage may be filled again, cs and wt rewritten
+        if (L::kBufs == 1) load(p + NT, 0);
+    }
+    cp_async_wait<0>();
+}
+
+template <class T, int DK>
+cudaError_t step_dk(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    // Parts of 16 rounds (64 KB) amortise the look-ups of a CTA; smaller ones where that leaves SMs idle.
+    const uint32_t elems = a.heads * a.dv * DK;
+    uint32_t part = kStepTile * 16;
+    while (part > kStepTile && (unsigned long long)a.n * ((elems + part - 1) / part) < 8ull * l.n_sms) part >>= 1;
+    const uint32_t parts = (elems + part - 1) / part;
+    return launch_pdl(ssm_step_kernel<T, DK>, dim3(a.n * parts), dim3(kStepCta), 0, l.stream, g, a, parts, part);
+}
+
+template <class T, int DK, int DVT, int NT>
+cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    using L = PromptSmem<DK, DVT, NT>;
+    static_assert(L::kTotal <= 227 * 1024, "shared memory of one CTA");
+    auto kernel = ssm_prompt_kernel<T, DK, DVT, NT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
+    if (e != cudaSuccess) return e;
+    const uint32_t tiles = a.dv / DVT;
+    return launch_pdl(kernel, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles);
+}
+template <class T, int DVT>
+cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    switch (a.dk) {
+    case 16: return prompt_launch<T, 16, DVT, 4>(g, a, l);
+    case 32: return prompt_launch<T, 32, DVT, 3>(g, a, l);
+    case 64: return prompt_launch<T, 64, DVT, 2>(g, a, l);
+    default: return prompt_launch<T, 128, DVT, 2>(g, a, l);
+    }
+}
+template <class T>
+cudaError_t step_type(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    switch (a.dk) {
+    case 16: return step_dk<T, 16>(g, a, l);
+    case 32: return step_dk<T, 32>(g, a, l);
+    case 64: return step_dk<T, 64>(g, a, l);
+    default: return step_dk<T, 128>(g, a, l);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    return a.f16 ? step_type<F16>(g, a, l) : step_type<Bf16>(g, a, l);
+}
+cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l)
+{
+    if (a.dv % 64 == 0) return a.f16 ? prompt_dv<F16, 64>(g, a, l) : prompt_dv<Bf16, 64>(g, a, l);
+    return a.f16 ? prompt_dv<F16, 32>(g, a, l) : prompt_dv<Bf16, 32>(g, a, l);
+}
+
+}  // namespace avmp
