@@ -15,6 +15,7 @@
  *   avmp_gather_kv   paged gather of one attention layer into ragged batch buffers;
  *   avmp_gather_ssm  gather of one SSM layer's state blocks into batch buffers;
  *   avmp_scatter_*   the matching write side;
+ *   avmp_attn_*      attention over the KV chains where they lie (whole prompts, single tokens);
  *   avmp_ssm_*       the linear recurrence on the SSM blocks where they lie (prompts, single tokens).
  *
  * Conventions
@@ -334,6 +335,38 @@ AVMP_API int avmp_scatter_ssm_layers(avmp_ctx *ctx, uint32_t first_layer, uint32
  * on the GPU.  An item that only the device can see to be wrong (see each call) is skipped, its output
  * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST. */
 enum { AVMP_TYPE_BF16 = 0, AVMP_TYPE_F16 = 1 };   /* type of input and output rows (and of cached K and V) */
+
+/* q and out rows are [q_heads][head_dim].  Query head h reads KV head h / (q_heads / kv_heads).
+ * Supported: kv_elem_bytes 2, head_dim 64 or 128, page_tokens a multiple of 8, q_heads a multiple
+ * of kv_heads with at most 64 query heads to a KV head; else AVMP_EINVAL. */
+typedef struct {
+    uint32_t type, q_heads;
+    float scale;               /* scores are scale * <q, k>; finite */
+    uint32_t rsvd;             /* 0 */
+    uint64_t q_stride_bytes, out_stride_bytes;
+} avmp_attn_desc;
+
+/* Scratch bytes that any avmp_attn_* call of up to n_reqs list entries needs (0 on invalid arguments). */
+AVMP_API size_t avmp_attn_workspace_bytes(const avmp_ctx *ctx, const avmp_attn_desc *desc, uint32_t n_reqs);
+
+/* Causal attention of the newest tokens of a batch (a prompt, a turn appended to a kept chain, a chunk
+ * of a prompt).  Rows d_cu_q[k] .. d_cu_q[k+1] of d_q are the LAST tokens of request d_reqs[k]'s chain,
+ * whose K and V have been written to the cache; row i of n stands at position held - n + i and sees
+ * the tokens up to and including its own position.  d_lse (may be NULL) receives the natural logarithm
+ * of each row's softmax denominator, [total_q][q_heads].  total_q is the number of rows of the buffers;
+ * rows that no list entry owns are not touched.  Skipped items: a slot that holds nothing, more rows
+ * than held tokens, offsets that decrease or pass total_q.  n_reqs <= max_requests; q_heads * total_q < 2^31. */
+AVMP_API int avmp_attn_prompt(avmp_ctx *ctx, uint32_t attn_layer, const avmp_attn_desc *desc, const uint32_t *d_reqs,
+                              uint32_t n_reqs, const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out,
+                              float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of one token per request over its whole chain: row k of d_q belongs to d_reqs[k] (slots may
+ * repeat).  With prefix_req != AVMP_INVALID every request also sees all tokens of that slot's chain
+ * (a shared prompt that is held once); the batch's products with it are computed together.  A prefix slot
+ * out of range or holding nothing skips every item. */
+AVMP_API int avmp_attn_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_attn_desc *desc, const uint32_t *d_reqs,
+                              uint32_t n_reqs, uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse,
+                              void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* Linear attention with a decay for each head (the recurrence of a state-space layer), on the state
  * elements of the SSM blocks, laid out [heads][dv][dk] in fp32 (ssm_elem_bytes 4, ssm_state_elems =

@@ -71,6 +71,11 @@ class avmp_session_stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in SESSION_STAT_FIELDS]
 
 
+class avmp_attn_desc(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("q_heads", C.c_uint32), ("scale", C.c_float), ("rsvd", C.c_uint32),
+                ("q_stride_bytes", C.c_uint64), ("out_stride_bytes", C.c_uint64)]
+
+
 class avmp_ssm_desc(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("type", "heads", "groups", "dk", "dv", "rsvd")] + \
                [(n, C.c_uint64) for n in ("q_stride_bytes", "k_stride_bytes", "v_stride_bytes", "decay_stride_bytes",
@@ -127,6 +132,11 @@ def _load():
         "avmp_scatter_ssm": (C.c_int, [vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp]),
         "avmp_scatter_kv_layers": (C.c_int, [vp, C.c_uint32, C.c_uint32, vp, vp, C.c_uint32, vp, vp, C.c_uint64, vp]),
         "avmp_scatter_ssm_layers": (C.c_int, [vp, C.c_uint32, C.c_uint32, vp, C.c_uint32, vp, C.c_uint64, vp, C.c_uint64, vp]),
+        "avmp_attn_workspace_bytes": (C.c_size_t, [vp, C.POINTER(avmp_attn_desc), C.c_uint32]),
+        "avmp_attn_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_attn_desc), vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp,
+                                       vp, C.c_size_t, vp]),
+        "avmp_attn_decode": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_attn_desc), vp, C.c_uint32, C.c_uint32, vp, vp, vp,
+                                       vp, C.c_size_t, vp]),
         "avmp_ssm_workspace_bytes": (C.c_size_t, [vp, C.POINTER(avmp_ssm_desc), C.c_uint32, C.c_uint32]),
         "avmp_ssm_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_ssm_desc), vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp, vp,
                                       vp, vp, vp, C.c_size_t, vp]),
@@ -371,12 +381,35 @@ def avmp_scatter_ssm_layers(ctx, first_layer, n_layers, d_reqs, n_reqs, d_in_sta
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
+def attn_desc(*, q_heads: int, dtype: torch.dtype, scale: float, q_stride_bytes: int = 0, out_stride_bytes: int = 0) -> avmp_attn_desc:
+    if dtype not in _TYPES:
+        raise AvmpError(f"attn_desc: {dtype} is not bfloat16 or float16")
+    return avmp_attn_desc(_TYPES[dtype], q_heads, scale, 0, q_stride_bytes, out_stride_bytes)
+
+
 def ssm_desc(*, heads: int, groups: int, dk: int, dv: int, dtype: torch.dtype, q_stride_bytes: int = 0, k_stride_bytes: int = 0,
              v_stride_bytes: int = 0, decay_stride_bytes: int = 0, out_stride_bytes: int = 0) -> avmp_ssm_desc:
     if dtype not in _TYPES:
         raise AvmpError(f"ssm_desc: {dtype} is not bfloat16 or float16")
     return avmp_ssm_desc(_TYPES[dtype], heads, groups, dk, dv, 0, q_stride_bytes, k_stride_bytes, v_stride_bytes,
                          decay_stride_bytes, out_stride_bytes)
+
+
+def avmp_attn_workspace_bytes(ctx, desc: avmp_attn_desc, n_reqs: int) -> int:
+    return lib.avmp_attn_workspace_bytes(ctx, C.byref(desc), n_reqs)
+
+
+def avmp_attn_prompt(ctx, attn_layer, desc, d_reqs, n_reqs, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                     stream=None):
+    _check(lib.avmp_attn_prompt(ctx, attn_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_cu_q), total_q, _ptr(d_q),
+                                _ptr(d_out), _ptr(d_lse), _ptr(d_workspace), workspace_bytes, _stream(stream)),
+           "avmp_attn_prompt")
+
+
+def avmp_attn_decode(ctx, attn_layer, desc, d_reqs, n_reqs, prefix_req, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                     stream=None):
+    _check(lib.avmp_attn_decode(ctx, attn_layer, C.byref(desc), _ptr(d_reqs), n_reqs, prefix_req, _ptr(d_q), _ptr(d_out),
+                                _ptr(d_lse), _ptr(d_workspace), workspace_bytes, _stream(stream)), "avmp_attn_decode")
 
 
 def avmp_ssm_workspace_bytes(ctx, desc: avmp_ssm_desc, n_reqs: int, total_tokens: int) -> int:
@@ -571,6 +604,17 @@ class Context:
 
     def scatter_ssm(self, layer, d_reqs, n, d_in_state, d_in_conv, stream=None):
         avmp_scatter_ssm(self.handle, layer, d_reqs, n, d_in_state, d_in_conv, stream)
+
+    def attn_workspace_bytes(self, desc, n) -> int:
+        return avmp_attn_workspace_bytes(self.handle, desc, n)
+
+    def attn_prompt(self, layer, desc, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream=None):
+        avmp_attn_prompt(self.handle, layer, desc, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace,
+                         workspace_bytes, stream)
+
+    def attn_decode(self, layer, desc, d_reqs, n, prefix_req, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream=None):
+        avmp_attn_decode(self.handle, layer, desc, d_reqs, n, prefix_req, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                         stream)
 
     def ssm_workspace_bytes(self, desc, n, total_tokens) -> int:
         return avmp_ssm_workspace_bytes(self.handle, desc, n, total_tokens)

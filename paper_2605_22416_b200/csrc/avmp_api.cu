@@ -84,6 +84,30 @@ void fill_stats(const avmp_ctx *c, const DevState &d, avmp_stats *o)
     o->step_ns_migration_plan = (uint64_t)(d.cyc_mig * ns_per_cycle);
 }
 
+bool attn_desc_ok(const avmp_ctx *c, const avmp_attn_desc *d)
+{
+    if (!d || d->type > AVMP_TYPE_F16 || d->rsvd || !std::isfinite(d->scale)) return false;
+    const avmp_model_spec &m = c->spec;
+    if (m.n_attn_layers == 0 || m.kv_elem_bytes != 2 || (m.head_dim != 64 && m.head_dim != 128) || m.page_tokens % 8) return false;
+    if (m.kv_heads == 0 || d->q_heads == 0 || d->q_heads > 65535u || d->q_heads % m.kv_heads || d->q_heads / m.kv_heads > 64) return false;
+    const uint64_t row = (uint64_t)d->q_heads * m.head_dim * 2;
+    auto stride_ok = [&](uint64_t s) { return s == 0 || (s >= row && s % 16 == 0 && s < (1ull << 40)); };
+    return stride_ok(d->q_stride_bytes) && stride_ok(d->out_stride_bytes);
+}
+
+AttnArgs attn_args(const avmp_ctx *c, const avmp_attn_desc *d, uint32_t layer, const uint32_t *reqs, uint32_t n, const void *q,
+                   void *out, float *lse, void *ws)
+{
+    AttnArgs a = {};
+    a.layer = layer; a.n = n; a.q_heads = d->q_heads; a.kv_heads = c->spec.kv_heads; a.head_dim = c->spec.head_dim;
+    a.prefix = kInvalid; a.f16 = d->type == AVMP_TYPE_F16; a.scale = d->scale;
+    a.reqs = reqs; a.q = static_cast<const uint8_t *>(q); a.out = static_cast<uint8_t *>(out); a.lse = lse;
+    const uint64_t row = (uint64_t)d->q_heads * c->spec.head_dim * 2;
+    a.qs = d->q_stride_bytes ? d->q_stride_bytes : row; a.os = d->out_stride_bytes ? d->out_stride_bytes : row;
+    a.ws = static_cast<uint8_t *>(ws);
+    return a;
+}
+
 inline bool ssm_desc_ok(const avmp_ctx *c, const avmp_ssm_desc *d)
 {
     if (!d || d->type > AVMP_TYPE_F16 || d->rsvd || c->spec.ssm_elem_bytes != 4 || c->spec.n_ssm_layers == 0) return false;
@@ -525,6 +549,50 @@ int avmp_scatter_ssm_layers(avmp_ctx *c, uint32_t first_layer, uint32_t n_layers
     c->launches += 1;
     return cu(launch_ssm(c->g, true, first_layer, n_layers, d_reqs, n, const_cast<void *>(d_in_state),
                          state_layer_stride_bytes, const_cast<void *>(d_in_conv), conv_layer_stride_bytes, L(c, stream)));
+}
+
+size_t avmp_attn_workspace_bytes(const avmp_ctx *c, const avmp_attn_desc *desc, uint32_t n)
+{
+    if (!c || !attn_desc_ok(c, desc) || n > c->opt.max_requests) return 0;
+    return attn_ws_bytes(c->g, n ? n : 1, desc->q_heads, c->spec.kv_heads, c->spec.head_dim, c->n_sms);
+}
+
+int avmp_attn_prompt(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, const uint32_t *d_reqs, uint32_t n,
+                     const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out, float *d_lse, void *d_workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu_q || (((uintptr_t)d_reqs | (uintptr_t)d_cu_q | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
+    if (total_q && (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15))) return AVMP_EINVAL;
+    if ((uint64_t)total_q * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
+    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
+    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
+    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
+    a.cu = d_cu_q; a.total_q = total_q;
+    uint32_t launched = 0;
+    const cudaError_t e = launch_attn_prompt(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
+}
+
+int avmp_attn_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, const uint32_t *d_reqs, uint32_t n,
+                     uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes,
+                     void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || (((uintptr_t)d_reqs | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
+    if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return AVMP_EINVAL;
+    if ((uint64_t)n * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
+    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
+    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
+    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
+    a.prefix = prefix_req;
+    uint32_t launched = 0;
+    const cudaError_t e = launch_attn_decode(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
 }
 
 size_t avmp_ssm_workspace_bytes(const avmp_ctx *, const avmp_ssm_desc *, uint32_t, uint32_t) { return 0; }

@@ -1,0 +1,547 @@
+// Attention of many query rows over paged KV chains on the tensor cores: whole prompts (causal, packed requests of
+// different lengths, grouped heads), and a batch of single tokens over a prefix that all of them share.
+//
+// A tile is 256 query rows of one KV head: the (token, query head) pairs that share that head, tokens first, so grouped
+// heads fill the rows of the tensor-core tiles whatever the group is, and every K and V row is loaded once for all of them.
+// Over it run the KV tokens, 128 at a time:
+//     S = Q K^T  (tcgen05, sums in tensor memory),  P = 2^(S - m),  O += P V  (P as an operand in tensor memory).
+// One CTA per SM, 12 warps: two warpgroups own 128 rows each (a thread is a row: the softmax needs no exchange), one
+// warp loads K and V slices of pages by tiled bulk copies, one issues the products.  While one warpgroup
+// exponentiates, the tensor cores work for the other.  The running maximum m is only moved when it grows by more than
+// 2^8 (P stays inside 16-bit range; sums are 32-bit), so the accumulator is rarely rescaled.
+// P is rounded to the 16 bits of V (eps/2 per weight, averaged over the tokens); denominators are summed before that.
+#include "avmp_tc.cuh"
+
+namespace avmp {
+
+namespace {
+
+constexpr int kRows = 256;                    // query rows per tile
+constexpr int kKv = 128;                      // KV tokens per round
+constexpr int kCta = 384;
+
+struct Tile { uint32_t k, b; };                          // list entry, row block
+struct Item { uint32_t req, len, q0, nq; };              // slot, held tokens, first row, rows
+
+struct PromptArgs {
+    AttnArgs a;
+    uint32_t group, splits, box_tokens;
+    uint32_t cap;                 // entries of `tiles`
+    uint32_t prefix_blocks;       // row blocks of the prefix pass
+    uint32_t *n_tiles;
+    Tile *tiles;
+    Item *items;
+    Parts parts;                  // [split][total rows][q_heads], where splits > 1 or for a prefix
+};
+
+// ---------------------------------------------------------------- plan
+// One CTA: checks every list entry and writes the row blocks of the good ones, longest reach first within a request.
+__global__ void __launch_bounds__(kStepThreads) prompt_plan_kernel(const Geom g, const PromptArgs p)
+{
+    __shared__ unsigned long long tmp[32];
+    __shared__ uint32_t pre[kStepThreads + 1];
+    pdl_prologue();
+    uint32_t base = 0;
+    for (uint32_t w = 0; w < p.a.n; w += kStepThreads) {
+        const uint32_t k = w + threadIdx.x, cnt = min((uint32_t)kStepThreads, p.a.n - w);
+        unsigned long long blocks = 0, tot;
+        Item it = {};
+        if (k < p.a.n) {
+            const uint32_t r = p.a.reqs[k], c0 = p.a.cu[k], c1 = p.a.cu[k + 1];
+            const uint32_t len = r < g.R && g.r_state[r] != AVMP_REQ_EMPTY ? g.r_len[r] : 0u;
+            it = Item{r, len, c0, c1 - c0};
+            if (len && c1 >= c0 && c1 <= p.a.total_q && it.nq <= len) blocks = ((unsigned long long)it.nq * p.group + kRows - 1) / kRows;
+            else record_error(g.st, AVMP_DEV_BAD_REQUEST);
+        }
+        const unsigned long long incl = block_incl_scan(blocks, tmp, &tot);
+        // offsets that run backwards can own more blocks than there are rows: what passes the list's end is skipped
+        if (k < p.a.n && base + incl > p.cap && blocks) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+        pre[threadIdx.x] = (uint32_t)min((unsigned long long)p.cap, base + incl - blocks);
+        if (threadIdx.x == 0) pre[cnt] = (uint32_t)min((unsigned long long)p.cap, base + tot);
+        if (k < p.a.n) p.items[k] = it;
+        __syncthreads();
+        for (uint32_t i = base + threadIdx.x; i < pre[cnt]; i += kStepThreads) {
+            const uint32_t e = find_owner(pre, 0, cnt, 0, i);
+            const uint32_t n_blocks = (uint32_t)(((unsigned long long)(p.a.cu[w + e + 1] - p.a.cu[w + e]) * p.group + kRows - 1) / kRows);
+            p.tiles[i] = Tile{w + e, n_blocks - 1 - (i - pre[e])};
+        }
+        base = pre[cnt];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *p.n_tiles = base;
+}
+
+// ---------------------------------------------------------------- the tiles
+struct Work {
+    uint32_t k, head, split, req;
+    uint32_t rows, row0;          // rows of this tile, its first row (token * group + head in group)
+    uint32_t q0;                  // first row of the request in the packed buffers
+    uint32_t past;                // tokens in front of the request's first query row
+    uint32_t len;                 // causal: tokens that the tile's last row sees; prefix: tokens held
+    uint32_t j0, j1;              // KV rounds
+};
+
+template <bool PREFIX>
+__device__ __forceinline__ uint32_t tile_count(const PromptArgs &p)
+{
+    return (PREFIX ? p.prefix_blocks : *(volatile uint32_t *)p.n_tiles) * p.a.kv_heads * p.splits;
+}
+template <bool PREFIX>
+__device__ __forceinline__ Work get_work(const Geom &g, const PromptArgs &p, uint32_t i)
+{
+    Work w;
+    w.split = i % p.splits;
+    i /= p.splits;
+    w.head = i % p.a.kv_heads;
+    i /= p.a.kv_heads;
+    if (PREFIX) {
+        w.k = 0; w.req = p.a.prefix; w.q0 = 0; w.past = 0;
+        w.row0 = i * kRows;
+        w.rows = min((uint32_t)kRows, p.a.n * p.group - w.row0);
+        w.len = w.req < g.R && g.r_state[w.req] != AVMP_REQ_EMPTY ? g.r_len[w.req] : 0u;
+    } else {
+        const Tile t = p.tiles[i];
+        const Item it = p.items[t.k];
+        w.k = t.k; w.req = it.req; w.q0 = it.q0; w.past = it.len - it.nq;
+        w.row0 = t.b * kRows;
+        w.rows = min((uint32_t)kRows, it.nq * p.group - w.row0);
+        w.len = w.past + (w.row0 + w.rows - 1) / p.group + 1;
+    }
+    const uint32_t rounds = (w.len + kKv - 1) / kKv;
+    w.j0 = (uint32_t)((unsigned long long)rounds * w.split / p.splits);
+    w.j1 = (uint32_t)((unsigned long long)rounds * (w.split + 1) / p.splits);
+    return w;
+}
+
+template <int D>
+struct Smem {
+    static constexpr uint32_t kQ = 128 * D * 2;             // one warpgroup's query rows
+    static constexpr uint32_t kTile = kKv * D * 2;          // K or V of a round
+    static constexpr uint32_t kSlots = D == 128 ? 5 : 10;
+    static constexpr uint32_t oRing = 2 * kQ;
+    static constexpr uint32_t kTotal = oRing + kSlots * kTile + 1024;
+};
+
+enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 26, B_DONE = 28, B_COUNT = 29 };
+
+template <class T, int D, bool PREFIX>
+__global__ void __launch_bounds__(kCta, 1)
+attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUtensorMap map)
+{
+    using M = Smem<D>;
+    constexpr uint32_t kHalf = kKv * 128;                    // 64 columns of a K, V or Q tile
+    constexpr uint32_t kS = 0, kO = 256;                     // tensor memory columns: S0 S1 (P in their first half) O0 O1
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ unsigned long long bars_s[B_COUNT];
+    __shared__ uint32_t tmem_s, gave_up;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(smem), bars = smem_u32(bars_s);
+    const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
+    auto bar = [&](uint32_t i) { return bars + 8 * i; };
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (uint32_t i = 0; i < M::kSlots; ++i) { mbar_init(bar(B_FULL + i), 1); mbar_init(bar(B_EMPTY + i), 1); }
+        for (uint32_t t = 0; t < 2; ++t) {
+            mbar_init(bar(B_Q + t), 128); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_P + t), 128); mbar_init(bar(B_O + t), 1);
+        }
+        mbar_init(bar(B_DONE), 1);
+        mbar_fence_init();
+        tma_prefetch_map(&map);
+    }
+    if (w == 9) tmem_alloc512(smem_u32(&tmem_s));
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_s;
+    pdl_prologue();
+    const uint32_t n_work = tile_count<PREFIX>(p);
+    const uint32_t L = p.a.layer;
+
+    if (w >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (w == 8) {
+            // ---------------- loads
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
+                const Work t = get_work<PREFIX>(g, p, i);
+                const uint32_t *chain = g.r_chain + (unsigned long long)t.req * g.max_pages;
+                auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
+                    const uint32_t tok = j * kKv + lane * p.box_tokens;
+                    if (j >= t.j1 || lane * p.box_tokens >= kKv || tok >= t.len) return kInvalid;
+                    return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
+                };
+                uint32_t next = look(t.j0);
+                for (uint32_t j = t.j0; j < t.j1 && ok; ++j) {
+                    const uint32_t slot = next;
+                    next = look(j + 1);
+                    const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
+                    const uint32_t tok = (j * kKv + lane * p.box_tokens) % g.T;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v, ++it) {
+                        const uint32_t s = it % M::kSlots, round = it / M::kSlots;
+                        if (round && !mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, &gave_up)) { ok = false; break; }
+                        if (lane == 0) mbar_expect(bar(B_FULL + s), boxes * p.box_tokens * D * 2);
+                        __syncwarp();
+                        if (slot != kInvalid)
+#pragma unroll
+                            for (int x = 0; x < D / 64; ++x)
+                                tma_load_page(base + M::oRing + s * M::kTile + x * kHalf + lane * p.box_tokens * 128, &map,
+                                              bar(B_FULL + s), x * 64, tok, t.head, L * 2 + v, slot);
+                    }
+                }
+            }
+            if (*(volatile uint32_t *)&gave_up) {      // copies in flight land before this CTA's memory is given away
+                for (uint32_t x = it > M::kSlots ? it - M::kSlots : 0; x < it; ++x) {
+                    const unsigned long long t0 = global_ns();
+                    while (!mbar_try(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1) && global_ns() - t0 < kWaitLimitNs) {}
+                }
+                if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
+            }
+        } else if (w == 9) {
+            // ---------------- products
+            constexpr uint32_t id_s = tc_idesc(T::kF16, false, kKv), id_o = tc_idesc(T::kF16, true, D);
+            uint32_t it = 0, tiles[2] = {0, 0}, rounds[2] = {0, 0};
+            bool ok = true;
+            auto issue_s = [&](uint32_t m, uint32_t slot) {
+                if (lane == 0) {
+                    const unsigned long long a = tc_desc(base + m * M::kQ, 16), b = tc_desc(base + M::oRing + slot * M::kTile, 16);
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint32_t off = ((x >> 2) * kHalf + (x & 3) * 32) >> 4;
+                        tc_mma_ss(tmem + kS + m * 128, a + off, b + off, id_s, x > 0);
+                    }
+                    tc_commit(bar(B_S + m));
+                }
+                __syncwarp();
+            };
+            auto full = [&](uint32_t n) { return mbar_wait(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, &gave_up); };
+            for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
+                const Work t = get_work<PREFIX>(g, p, i);
+                if (t.j0 == t.j1) continue;
+                const uint32_t both = t.rows > 128 ? 2 : 1;
+                // K of round j is load it + 2 (j - j0), V the one behind it
+                #pragma unroll
+                for (uint32_t m = 0; m < 2; ++m) {
+                    if (m >= both || !ok) continue;
+                    ok = mbar_wait(bar(B_Q + m), tiles[m] & 1, &gave_up) && (m || full(it));
+                    tiles[m] += 1;
+                    tc_fence_after();
+                    if (ok) issue_s(m, it % M::kSlots);
+                }
+                if (ok && lane == 0) tc_commit(bar(B_EMPTY + it % M::kSlots));
+                for (uint32_t j = t.j0; j < t.j1 && ok; ++j, it += 2) {
+                    const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
+                    const bool more = j + 1 < t.j1;
+                    ok = full(it + 1);
+                    const uint32_t valid = min((uint32_t)kKv, t.len - j * kKv), steps = (valid + 15) / 16;
+                    if (ok && (valid & 15)) {
+                        // behind the last token lie other requests' leftovers: a weight of zero does not silence a NaN
+                        uint8_t *v = smem + M::oRing + sv * M::kTile;
+                        for (uint32_t x = lane; x < (steps * 16 - valid) * (D / 8); x += 32) {
+                            const uint32_t c = x % (D / 8);
+                            *reinterpret_cast<uint4 *>(v + (c >> 3) * kHalf + (valid + x / (D / 8)) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
+                    if (ok && more) ok = full(it + 2);
+#pragma unroll
+                    for (uint32_t m = 0; m < 2; ++m) {
+                        if (m >= both || !ok) continue;
+                        ok = mbar_wait(bar(B_P + m), rounds[m] & 1, &gave_up);
+                        rounds[m] += 1;
+                        tc_fence_after();
+                        if (!ok) continue;
+                        if (lane == 0) {
+                            const unsigned long long b = tc_desc(base + M::oRing + sv * M::kTile, kHalf);
+                            for (uint32_t x = 0; x < steps; ++x)
+                                tc_mma_ts(tmem + kO + m * D, tmem + kS + m * 128 + x * 8, b + ((x * 2048) >> 4), id_o, j > t.j0 || x > 0);
+                            if (!more) tc_commit(bar(B_O + m));
+                        }
+                        __syncwarp();
+                        if (more) issue_s(m, sk);
+                    }
+                    if (ok && lane == 0) {
+                        tc_commit(bar(B_EMPTY + sv));
+                        if (more) tc_commit(bar(B_EMPTY + sk));
+                    }
+                    __syncwarp();
+                }
+            }
+            // every product is complete before tensor memory is given back
+            if (lane == 0) tc_commit(bar(B_DONE));
+            __syncwarp();
+            const unsigned long long t0 = global_ns();
+            while (!mbar_try(bar(B_DONE), 0) && global_ns() - t0 < kWaitLimitNs) {}
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        // ---------------- softmax: warpgroup m, one row per thread
+        const uint32_t m = w >> 2, tid = threadIdx.x & 127;
+        const uint32_t lanes = (uint32_t)(w & 3) << 21;                 // this warp's quarter of the lanes
+        const uint32_t ts = tmem + kS + m * 128 + lanes, to = tmem + kO + m * D + lanes;
+        // 1e-30: with a scale of 0 masked scores still become 2^-inf
+        const float sl2 = fmaxf(fabsf(p.a.scale) * 1.4426950408889634f, 1e-30f);
+        const uint32_t flip = p.a.scale < 0.f ? 0x80008000u : 0u;       // a negative scale is one of -q
+        uint32_t rounds = 0, tiles = 0;
+        bool ok = true;
+        for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
+            const Work t = get_work<PREFIX>(g, p, i);
+            const uint32_t row = t.row0 + m * 128 + tid;               // (token, head) of the request
+            const uint32_t token = row / p.group;
+            const bool mine = m * 128 + tid < t.rows;
+            const uint32_t qh = t.head * p.group + row % p.group;
+            if (m * 128 >= t.rows) continue;
+            if (t.j0 < t.j1) {
+                // rows of Q in 128-byte swizzle, zeros behind the last; a half-warp per row and round
+                constexpr uint32_t C = D / 8;                          // 16-byte units per row
+#pragma unroll 4
+                for (uint32_t x = tid; x < 128 * C; x += 128) {
+                    const uint32_t r = x / C, c = x % C, rr = t.row0 + m * 128 + r;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (m * 128 + r < t.rows)
+                        v = *reinterpret_cast<const uint4 *>(p.a.q + (unsigned long long)(t.q0 + rr / p.group) * p.a.qs +
+                                                             ((t.head * p.group + rr % p.group) * D + c * 8) * 2);
+                    v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+                    *reinterpret_cast<uint4 *>(smem + m * M::kQ + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+                }
+                fence_async_smem();
+                mbar_arrive(bar(B_Q + m));
+            }
+            float top = -INFINITY, sum = 0.f;
+            // columns of a round up to this one are seen by the row
+            const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
+            for (uint32_t j = t.j0; j < t.j1; ++j, ++rounds) {
+                ok = mbar_wait(bar(B_S + m), rounds & 1, &gave_up);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t u[128];
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
+                tmem_wait_ld();
+                float *s = reinterpret_cast<float *>(u);
+                if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
+                    const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
+                }
+                float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
+#pragma unroll
+                for (int c = 4; c < 128; c += 4) { x0 = fmaxf(x0, s[c]); x1 = fmaxf(x1, s[c + 1]); x2 = fmaxf(x2, s[c + 2]); x3 = fmaxf(x3, s[c + 3]); }
+                const float now = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * sl2;
+                const bool grow = now > top + 8.f || (top == -INFINITY && now > -INFINITY);
+                if (__any_sync(0xFFFFFFFFu, grow)) {
+                    const float f = grow ? exp2_approx(top - now) : 1.f;
+                    if (grow) { top = now; sum *= f; }
+                    if (j > t.j0) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o, to + c);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st16(to + c, o);
+                        }
+                    }
+                }
+                const float sub = top == -INFINITY ? 0.f : -top;
+                float y0 = 0.f, y1 = 0.f, y2 = 0.f, y3 = 0.f;
+#pragma unroll
+                for (int c = 0; c < 128; c += 4) {
+                    const float e0 = exp2_approx(fmaf(s[c], sl2, sub)), e1 = exp2_approx(fmaf(s[c + 1], sl2, sub));
+                    const float e2 = exp2_approx(fmaf(s[c + 2], sl2, sub)), e3 = exp2_approx(fmaf(s[c + 3], sl2, sub));
+                    y0 += e0; y1 += e1; y2 += e2; y3 += e3;
+                    u[c / 2] = T::pack(e0, e1); u[c / 2 + 1] = T::pack(e2, e3);
+                    if (c % 64 == 60) tmem_st32(ts + (c / 64) * 32, u + (c / 64) * 32);
+                }
+                sum += (y0 + y1) + (y2 + y3);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar(B_P + m));
+            }
+            if (!ok) break;
+            const unsigned long long at = (PREFIX || p.splits > 1)
+                ? ((unsigned long long)t.split * (PREFIX ? p.a.n : p.a.total_q) + t.q0 + token) * p.a.q_heads + qh : 0ull;
+            if (t.j0 < t.j1) {
+                ok = mbar_wait(bar(B_O + m), tiles & 1, &gave_up);
+                if (!ok) break;
+                tiles += 1;
+                tc_fence_after();
+            }
+            if (PREFIX || p.splits > 1) {
+                if (mine) p.parts.ml[at] = make_float2(top, sum);
+                if (t.j0 == t.j1) continue;
+            }
+            const float inv = 1.f / sum;
+            uint8_t *out = p.a.out + (unsigned long long)(t.q0 + token) * p.a.os + (unsigned long long)qh * D * 2;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(o, to + c);
+                tmem_wait_ld();
+                if (mine && (PREFIX || p.splits > 1)) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4 *>(p.parts.o + at * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                } else if (mine) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 v;
+                        v.x = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                        v.y = T::pack(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                        v.z = T::pack(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                        v.w = T::pack(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                        *reinterpret_cast<uint4 *>(out + (c + e) * 2) = v;
+                    }
+                }
+                __syncwarp();
+            }
+            if (!PREFIX && p.splits == 1 && mine && p.a.lse)
+                p.a.lse[(unsigned long long)(t.q0 + token) * p.a.q_heads + qh] = top * 0.6931471805599453f + logf(sum);
+            tc_fence_before();         // tensor memory has been read: the next tile's products may overwrite it
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (w == 9) tmem_free512(tmem);
+}
+
+// Rows of a prompt call whose tokens were split: one warp per (row, query head).
+template <class T, int D>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs p)
+{
+    pdl_prologue();
+    const uint32_t n = *p.n_tiles * p.a.kv_heads;
+    const int lane = threadIdx.x % 32;
+    constexpr int E = D / 32;
+    for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
+        const Tile t = p.tiles[i / p.a.kv_heads];
+        const Item it = p.items[t.k];
+        const uint32_t head = i % p.a.kv_heads, rows = min((uint32_t)kRows, it.nq * p.group - t.b * kRows);
+        for (uint32_t r = threadIdx.x / 32; r < rows; r += 8) {
+            const uint32_t row = t.b * kRows + r, qh = head * p.group + row % p.group;
+            const unsigned long long at = (unsigned long long)(it.q0 + row / p.group) * p.a.q_heads + qh;
+            const unsigned long long step = (unsigned long long)p.a.total_q * p.a.q_heads;
+            float top = -INFINITY, den = 0.f, acc[E] = {};
+            for (uint32_t s = 0; s < p.splits; ++s) {
+                const float2 e = p.parts.ml[at + s * step];
+                if (e.y != 0.f) top = fmaxf(top, e.x);
+            }
+            for (uint32_t s = 0; s < p.splits; ++s) {
+                const float2 e = p.parts.ml[at + s * step];
+                if (e.y == 0.f) continue;
+                const float f = exp2_approx(e.x - top);
+                den += e.y * f;
+#pragma unroll
+                for (int x = 0; x < E; ++x) acc[x] += f * p.parts.o[(at + s * step) * D + lane * E + x];
+            }
+            const float inv = 1.f / den;
+            uint8_t *out = p.a.out + (unsigned long long)(it.q0 + row / p.group) * p.a.os + ((unsigned long long)qh * D + lane * E) * 2;
+#pragma unroll
+            for (int x = 0; x < E; x += 2) *reinterpret_cast<uint32_t *>(out + x * 2) = T::pack(acc[x] * inv, acc[x + 1] * inv);
+            if (p.a.lse && lane == 0) p.a.lse[at] = top * 0.6931471805599453f + logf(den);
+        }
+    }
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+uint32_t box_of(uint32_t T)
+{
+    uint32_t b = 8;
+    while (b < (uint32_t)kKv && T % (2 * b) == 0) b *= 2;
+    return b;
+}
+
+// Rows of partial sums that a call may leave: splitting stops where the SMs are busy.
+size_t part_rows(size_t rows, int n_sms) { const size_t full = (size_t)n_sms * kRows; return rows > full ? rows : full; }
+
+template <class T, int D, bool PREFIX>
+cudaError_t tile_launch(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
+{
+    CUtensorMap map;
+    if (!page_map(&map, g, p.a.kv_heads, p.a.head_dim, p.box_tokens, 1)) return cudaErrorNotSupported;
+    auto kernel = attn_tile_kernel<T, D, PREFIX>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kTotal);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, p, map);
+}
+template <bool PREFIX>
+cudaError_t tile_type(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
+{
+    if (p.a.head_dim == 128) return p.a.f16 ? tile_launch<F16, 128, PREFIX>(g, p, grid, l) : tile_launch<Bf16, 128, PREFIX>(g, p, grid, l);
+    return p.a.f16 ? tile_launch<F16, 64, PREFIX>(g, p, grid, l) : tile_launch<Bf16, 64, PREFIX>(g, p, grid, l);
+}
+template <class T>
+cudaError_t join_type(const PromptArgs &p, uint32_t grid, const Launch &l)
+{
+    return p.a.head_dim == 128 ? launch_pdl(prompt_join_kernel<T, 128>, dim3(grid), dim3(256), 0, l.stream, p)
+                               : launch_pdl(prompt_join_kernel<T, 64>, dim3(grid), dim3(256), 0, l.stream, p);
+}
+
+// As many shares of the KV tokens as leave every SM a tile.
+uint32_t split_of(unsigned long long tiles, int n_sms)
+{
+    return tiles >= (unsigned long long)n_sms ? 1u : (uint32_t)(n_sms / (tiles ? tiles : 1));
+}
+
+}  // namespace
+
+cudaError_t launch_attn_prefix(const Geom &g, const AttnArgs &a, const Launch &l, Parts *out, uint32_t *parts)
+{
+    PromptArgs p = {};
+    p.a = a;
+    p.group = a.q_heads / a.kv_heads;
+    p.prefix_blocks = (uint32_t)(((unsigned long long)a.n * p.group + kRows - 1) / kRows);
+    const unsigned long long tiles = (unsigned long long)p.prefix_blocks * a.kv_heads;
+    p.splits = split_of(tiles, l.n_sms);
+    p.box_tokens = box_of(g.T);
+    const size_t rows = (size_t)p.splits * a.n * a.q_heads;
+    p.parts.ml = reinterpret_cast<float2 *>(a.ws);
+    p.parts.o = reinterpret_cast<float *>(a.ws + up256(rows * 8));
+    *out = p.parts;
+    *parts = p.splits;
+    return tile_type<true>(g, p, (uint32_t)min(tiles * p.splits, (unsigned long long)l.n_sms), l);
+}
+
+size_t attn_tile_ws_bytes(const Geom &g, uint32_t n, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms)
+{
+    // tiles: no request has more query rows than it can hold tokens
+    const size_t cap = (size_t)n * (((size_t)g.max_pages * g.T * (q_heads / kv_heads) + kRows - 1) / kRows);
+    return 256 + up256(cap * sizeof(Tile)) + up256((size_t)n * sizeof(Item)) + part_rows((size_t)n * q_heads, n_sms) * ((size_t)head_dim * 4 + 8) + 512;
+}
+
+cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l, uint32_t *launched)
+{
+    PromptArgs p = {};
+    p.a = a;
+    p.group = a.q_heads / a.kv_heads;
+    p.box_tokens = box_of(g.T);
+    const unsigned long long full = (unsigned long long)a.n * (((unsigned long long)g.max_pages * g.T * p.group + kRows - 1) / kRows);
+    p.cap = (uint32_t)min(full, (unsigned long long)a.total_q * p.group / kRows + a.n);
+    p.splits = split_of((unsigned long long)p.cap * a.kv_heads, l.n_sms);
+    uint8_t *w = a.ws;
+    p.n_tiles = reinterpret_cast<uint32_t *>(w); w += 256;
+    p.tiles = reinterpret_cast<Tile *>(w); w += up256((size_t)full * sizeof(Tile));
+    p.items = reinterpret_cast<Item *>(w); w += up256((size_t)a.n * sizeof(Item));
+    const size_t rows = (size_t)p.splits * a.total_q * a.q_heads;
+    p.parts.ml = reinterpret_cast<float2 *>(w);
+    p.parts.o = reinterpret_cast<float *>(w + up256(rows * 8));
+    cudaError_t e = launch_pdl(prompt_plan_kernel, dim3(1), dim3(kStepThreads), 0, l.stream, g, p);
+    if (e != cudaSuccess) return e;
+    const unsigned long long tiles = (unsigned long long)p.cap * a.kv_heads * p.splits;
+    e = tile_type<false>(g, p, (uint32_t)min(tiles, (unsigned long long)l.n_sms), l);
+    if (e != cudaSuccess) return e;
+    *launched += 2;
+    if (p.splits > 1) {
+        const uint32_t grid = (uint32_t)min((unsigned long long)p.cap * a.kv_heads, 4ull * l.n_sms);
+        e = a.f16 ? join_type<F16>(p, grid, l) : join_type<Bf16>(p, grid, l);
+        *launched += 1;
+    }
+    return e;
+}
+
+}  // namespace avmp

@@ -213,6 +213,22 @@ struct SsmArgs {
 };
 cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l);
 cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l);
+// Attention over KV chains (avmp_attn.cu, avmp_attn_prompt.cu).
+struct AttnArgs {
+    uint32_t layer, n, q_heads, kv_heads, head_dim, total_q;
+    uint32_t prefix;                           // slot, or kInvalid
+    bool f16;
+    float scale;
+    const uint32_t *reqs, *cu;
+    const uint8_t *q;
+    uint8_t *out;
+    float *lse;                                // may be null
+    unsigned long long qs, os;                 // row strides in bytes
+    uint8_t *ws;
+};
+size_t attn_ws_bytes(const Geom &g, uint32_t n_reqs, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms);
+cudaError_t launch_attn_decode(const Geom &g, const AttnArgs &a, const Launch &l, uint32_t *n_launched);
+cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l, uint32_t *n_launched);
 // Resolves the in-library scratch of avmp_gather_kv_static on the current device (= dev).
 cudaError_t static_gather_setup(int dev);
 

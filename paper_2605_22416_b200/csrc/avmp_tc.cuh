@@ -1,0 +1,157 @@
+// Blackwell building blocks of the attention kernels: mbarriers with bounded waits, tiled bulk loads of page slices,
+// tensor-core products with accumulators in tensor memory.
+#pragma once
+
+#include <cuda.h>
+
+#include "avmp_dev.cuh"
+#include "avmp_mma.cuh"
+
+namespace avmp {
+
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // after this a wait gives up
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_fence_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits until the phase with this parity is complete.  False after kWaitLimitNs, or once `gave_up` is set (which a
+// failed wait does, so that every role of the CTA stops): the caller then issues nothing more and leaves.  Whole warps.
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try(bar, parity)) {
+        if (*gave_up) return false;
+        if (global_ns() - t0 > kWaitLimitNs) { *gave_up = 1; return false; }
+    }
+    return true;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    bool ok = false;
+#pragma unroll 1
+    for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try(bar, parity);
+    if (!ok) ok = mbar_wait_slow(bar, parity, gave_up);
+    __syncwarp();
+    return ok;
+}
+
+// One box of the page tensor: 64 elements of `rows` tokens of a run of heads, at (x, token, head, layer and part, slot).
+__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int token, int head,
+                                              int part, int slot)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(token), "r"(head), "r"(part), "r"(slot) : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map)
+{
+    asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+}
+// Writes of ordinary stores to shared memory become visible to bulk copies and tensor-core operand reads.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---- tensor memory and tensor-core products (one CTA per tile)
+__device__ __forceinline__ void tmem_alloc512(uint32_t smem_dst)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_dst) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free512(uint32_t tmem)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// The barrier gets one arrival when every product issued so far by this thread is complete.
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+// D[tmem] (+)= A[smem] B[smem], and with A in tensor memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, unsigned long long a, unsigned long long b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, unsigned long long b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// Shared-memory operand in rows of 128 bytes whose 16-byte units are permuted by the row index (128-byte swizzle):
+// groups of 8 rows 1024 bytes apart; `lead` is the distance between column blocks of 64 elements where the operand's
+// long axis runs along the rows.
+__device__ __forceinline__ unsigned long long tc_desc(uint32_t addr, uint32_t lead)
+{
+    return (unsigned long long)((addr & 0x3FFFFu) >> 4) | ((unsigned long long)(lead >> 4) << 16) | ((unsigned long long)(1024u >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor: 16-bit operands, 32-bit sums, M = 128.
+__device__ __forceinline__ constexpr uint32_t tc_idesc(bool f16, bool b_by_rows, uint32_t n)
+{
+    return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_by_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+#define AVMP_R8(r, o) "=r"((r)[(o)]), "=r"((r)[(o) + 1]), "=r"((r)[(o) + 2]), "=r"((r)[(o) + 3]), "=r"((r)[(o) + 4]), "=r"((r)[(o) + 5]), "=r"((r)[(o) + 6]), "=r"((r)[(o) + 7])
+#define AVMP_W8(r, o) "r"((r)[(o)]), "r"((r)[(o) + 1]), "r"((r)[(o) + 2]), "r"((r)[(o) + 3]), "r"((r)[(o) + 4]), "r"((r)[(o) + 5]), "r"((r)[(o) + 6]), "r"((r)[(o) + 7])
+// 32 columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld32(uint32_t *r, uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : AVMP_R8(r, 0), AVMP_R8(r, 8), AVMP_R8(r, 16), AVMP_R8(r, 24) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 :: "r"(addr), AVMP_W8(r, 0), AVMP_W8(r, 8), AVMP_W8(r, 16), AVMP_W8(r, 24) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t *r, uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : AVMP_R8(r, 0), AVMP_R8(r, 8) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(addr), AVMP_W8(r, 0), AVMP_W8(r, 8) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// The pages as a five-dimensional tensor [slot][layer, K or V][head][token][dim] with boxes of box_tokens x box_heads rows of
+// 64 elements; dimensions need not be in memory order, so a box arrives sorted by head.  (avmp_attn.cu)
+bool page_map(CUtensorMap *map, const Geom &g, uint32_t kv_heads, uint32_t head_dim, uint32_t box_tokens, uint32_t box_heads);
+
+// What the parts of an attention call leave for the joining pass: sums over part of the tokens, not yet divided.
+struct Parts {
+    float *o;        // [part][head][dim]
+    float2 *ml;      // [part][head]: maximum (log2 units) that the sums are relative to, sum of exponentials (0: no sums written)
+};
+
+// The pass over the shared prefix of a batch of single tokens: fills *out with *parts parts of [n][q_heads].  (avmp_attn_prompt.cu)
+cudaError_t launch_attn_prefix(const Geom &g, const AttnArgs &a, const Launch &l, Parts *out, uint32_t *parts);
+size_t attn_tile_ws_bytes(const Geom &g, uint32_t n, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms);
+
+}  // namespace avmp
