@@ -19,6 +19,7 @@ namespace {
 constexpr int kRows = 256;                    // query rows per tile
 constexpr int kKv = 128;                      // KV tokens per round
 constexpr int kCta = 384;
+constexpr bool kPoly = true;                 // a quarter of the exponentials on the multiply-add pipe
 
 struct Tile { uint32_t k, b; };                          // list entry, row block
 struct Item { uint32_t req, len, q0, nq; };              // slot, held tokens, first row, rows
@@ -77,8 +78,10 @@ struct Work {
     uint32_t rows, row0;          // rows of this tile, its first row (token * group + head in group)
     uint32_t q0;                  // first row of the request in the packed buffers
     uint32_t past;                // tokens in front of the request's first query row
-    uint32_t len;                 // causal: tokens that the tile's last row sees; prefix: tokens held
+    uint32_t held;                // tokens of the chain
+    uint32_t len;                 // tokens that the tile's last row sees
     uint32_t j0, j1;              // KV rounds
+    uint32_t tok0, rem0;          // token and head in group of the tile's first row
 };
 
 template <bool PREFIX>
@@ -86,6 +89,9 @@ __device__ __forceinline__ uint32_t tile_count(const PromptArgs &p)
 {
     return (PREFIX ? p.prefix_blocks : *(volatile uint32_t *)p.n_tiles) * p.a.kv_heads * p.splits;
 }
+// The i-th tile of CTA c: the list runs from long tiles to short ones, every other pass over the CTAs backwards.
+__device__ __forceinline__ uint32_t nth_tile(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+
 template <bool PREFIX>
 __device__ __forceinline__ Work get_work(const Geom &g, const PromptArgs &p, uint32_t i)
 {
@@ -98,15 +104,16 @@ __device__ __forceinline__ Work get_work(const Geom &g, const PromptArgs &p, uin
         w.k = 0; w.req = p.a.prefix; w.q0 = 0; w.past = 0;
         w.row0 = i * kRows;
         w.rows = min((uint32_t)kRows, p.a.n * p.group - w.row0);
-        w.len = w.req < g.R && g.r_state[w.req] != AVMP_REQ_EMPTY ? g.r_len[w.req] : 0u;
+        w.len = w.held = w.req < g.R && g.r_state[w.req] != AVMP_REQ_EMPTY ? g.r_len[w.req] : 0u;
     } else {
         const Tile t = p.tiles[i];
         const Item it = p.items[t.k];
-        w.k = t.k; w.req = it.req; w.q0 = it.q0; w.past = it.len - it.nq;
+        w.k = t.k; w.req = it.req; w.q0 = it.q0; w.past = it.len - it.nq; w.held = it.len;
         w.row0 = t.b * kRows;
         w.rows = min((uint32_t)kRows, it.nq * p.group - w.row0);
         w.len = w.past + (w.row0 + w.rows - 1) / p.group + 1;
     }
+    w.tok0 = w.row0 / p.group; w.rem0 = w.row0 - w.tok0 * p.group;
     const uint32_t rounds = (w.len + kKv - 1) / kKv;
     w.j0 = (uint32_t)((unsigned long long)rounds * w.split / p.splits);
     w.j1 = (uint32_t)((unsigned long long)rounds * (w.split + 1) / p.splits);
@@ -122,7 +129,7 @@ struct Smem {
     static constexpr uint32_t kTotal = oRing + kSlots * kTile + 1024;
 };
 
-enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 26, B_DONE = 28, B_COUNT = 29 };
+enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_COUNT = 31 };
 
 template <class T, int D, bool PREFIX>
 __global__ void __launch_bounds__(kCta, 1)
@@ -142,7 +149,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         gave_up = 0;
         for (uint32_t i = 0; i < M::kSlots; ++i) { mbar_init(bar(B_FULL + i), 1); mbar_init(bar(B_EMPTY + i), 1); }
         for (uint32_t t = 0; t < 2; ++t) {
-            mbar_init(bar(B_Q + t), 128); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_P + t), 128); mbar_init(bar(B_O + t), 1);
+            mbar_init(bar(B_Q + t), 128); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_O + t), 1);
+            mbar_init(bar(B_P + 2 * t), 128); mbar_init(bar(B_P + 2 * t + 1), 128);
         }
         mbar_init(bar(B_DONE), 1);
         mbar_fence_init();
@@ -155,7 +163,6 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     const uint32_t tmem = tmem_s;
     pdl_prologue();
     const uint32_t n_work = tile_count<PREFIX>(p);
-    const uint32_t L = p.a.layer;
 
     if (w >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -163,12 +170,13 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
             // ---------------- loads
             uint32_t it = 0;
             bool ok = true;
-            for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
+            for (uint32_t n = 0, i; (i = nth_tile(n)) < n_work && ok; ++n) {
                 const Work t = get_work<PREFIX>(g, p, i);
                 const uint32_t *chain = g.r_chain + (unsigned long long)t.req * g.max_pages;
+                const uint32_t need = min((t.len + 15u) & ~15u, t.held);     // products run over whole steps of 16 tokens
                 auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
                     const uint32_t tok = j * kKv + lane * p.box_tokens;
-                    if (j >= t.j1 || lane * p.box_tokens >= kKv || tok >= t.len) return kInvalid;
+                    if (j >= t.j1 || lane * p.box_tokens >= kKv || tok >= need) return kInvalid;
                     return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
                 };
                 uint32_t next = look(t.j0);
@@ -187,7 +195,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
 #pragma unroll
                             for (int x = 0; x < D / 64; ++x)
                                 tma_load_page(base + M::oRing + s * M::kTile + x * kHalf + lane * p.box_tokens * 128, &map,
-                                              bar(B_FULL + s), x * 64, tok, t.head, L * 2 + v, slot);
+                                              bar(B_FULL + s), x * 64, tok, t.head, p.a.layer * 2 + v, slot);
                     }
                 }
             }
@@ -199,81 +207,72 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
             }
         } else if (w == 9) {
-            // ---------------- products
-            constexpr uint32_t id_s = tc_idesc(T::kF16, false, kKv), id_o = tc_idesc(T::kF16, true, D);
-            uint32_t it = 0, tiles[2] = {0, 0}, rounds[2] = {0, 0};
-            bool ok = true;
-            auto issue_s = [&](uint32_t m, uint32_t slot) {
-                if (lane == 0) {
-                    const unsigned long long a = tc_desc(base + m * M::kQ, 16), b = tc_desc(base + M::oRing + slot * M::kTile, 16);
+            // ---------------- products, all by one thread
+            if (elect_one()) {
+                const uint32_t id_s = tc_idesc(T::kF16, false, kKv) | (p.a.scale < 0.f ? kNegateA : 0u);    // a negative scale is one of -q
+                constexpr uint32_t id_o = tc_idesc(T::kF16, true, D);
+                uint32_t it = 0, tiles0 = 0, tiles1 = 0, rounds0 = 0, rounds1 = 0;
+                bool ok = true;
+                const unsigned long long q_desc = tc_desc(base, 16), k_desc = tc_desc(base + M::oRing, 16), v_desc = tc_desc(base + M::oRing, kHalf);
+                auto issue_s = [&](uint32_t m, uint32_t slot) {
+                    const unsigned long long a = q_desc + ((m * M::kQ) >> 4), b = k_desc + ((slot * M::kTile) >> 4);
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
                         const uint32_t off = ((x >> 2) * kHalf + (x & 3) * 32) >> 4;
                         tc_mma_ss(tmem + kS + m * 128, a + off, b + off, id_s, x > 0);
                     }
                     tc_commit(bar(B_S + m));
-                }
-                __syncwarp();
-            };
-            auto full = [&](uint32_t n) { return mbar_wait(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, &gave_up); };
-            for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
-                const Work t = get_work<PREFIX>(g, p, i);
-                if (t.j0 == t.j1) continue;
-                const uint32_t both = t.rows > 128 ? 2 : 1;
-                // K of round j is load it + 2 (j - j0), V the one behind it
-                #pragma unroll
-                for (uint32_t m = 0; m < 2; ++m) {
-                    if (m >= both || !ok) continue;
-                    ok = mbar_wait(bar(B_Q + m), tiles[m] & 1, &gave_up) && (m || full(it));
-                    tiles[m] += 1;
+                };
+                auto full = [&](uint32_t n) { return mbar_wait_one(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, &gave_up); };
+                for (uint32_t n = 0, i; (i = nth_tile(n)) < n_work && ok; ++n) {
+                    const Work t = get_work<PREFIX>(g, p, i);
+                    if (t.j0 == t.j1) continue;
+                    const bool two = t.rows > 128;
+                    // K of round j is load it + 2 (j - j0), V the one behind it
+                    ok = full(it) && mbar_wait_one(bar(B_Q), tiles0++ & 1, &gave_up);
+                    if (!ok) break;
                     tc_fence_after();
-                    if (ok) issue_s(m, it % M::kSlots);
-                }
-                if (ok && lane == 0) tc_commit(bar(B_EMPTY + it % M::kSlots));
-                for (uint32_t j = t.j0; j < t.j1 && ok; ++j, it += 2) {
-                    const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
-                    const bool more = j + 1 < t.j1;
-                    ok = full(it + 1);
-                    const uint32_t valid = min((uint32_t)kKv, t.len - j * kKv), steps = (valid + 15) / 16;
-                    if (ok && (valid & 15)) {
-                        // behind the last token lie other requests' leftovers: a weight of zero does not silence a NaN
-                        uint8_t *v = smem + M::oRing + sv * M::kTile;
-                        for (uint32_t x = lane; x < (steps * 16 - valid) * (D / 8); x += 32) {
-                            const uint32_t c = x % (D / 8);
-                            *reinterpret_cast<uint4 *>(v + (c >> 3) * kHalf + (valid + x / (D / 8)) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                    }
-                    if (ok && more) ok = full(it + 2);
-#pragma unroll
-                    for (uint32_t m = 0; m < 2; ++m) {
-                        if (m >= both || !ok) continue;
-                        ok = mbar_wait(bar(B_P + m), rounds[m] & 1, &gave_up);
-                        rounds[m] += 1;
+                    issue_s(0, it % M::kSlots);
+                    if (two) {
+                        ok = mbar_wait_one(bar(B_Q + 1), tiles1++ & 1, &gave_up);
+                        if (!ok) break;
                         tc_fence_after();
-                        if (!ok) continue;
-                        if (lane == 0) {
-                            const unsigned long long b = tc_desc(base + M::oRing + sv * M::kTile, kHalf);
-                            for (uint32_t x = 0; x < steps; ++x)
-                                tc_mma_ts(tmem + kO + m * D, tmem + kS + m * 128 + x * 8, b + ((x * 2048) >> 4), id_o, j > t.j0 || x > 0);
-                            if (!more) tc_commit(bar(B_O + m));
-                        }
-                        __syncwarp();
-                        if (more) issue_s(m, sk);
+                        issue_s(1, it % M::kSlots);
                     }
-                    if (ok && lane == 0) {
+                    tc_commit(bar(B_EMPTY + it % M::kSlots));
+                    for (uint32_t j = t.j0; j < t.j1; ++j, it += 2) {
+                        const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
+                        const bool more = j + 1 < t.j1;
+                        const uint32_t steps = min((uint32_t)kKv / 16, (t.len - j * kKv + 15) / 16);
+                        ok = full(it + 1) && (!more || full(it + 2));
+                        if (!ok) break;
+                        const unsigned long long b = v_desc + ((sv * M::kTile) >> 4);
+                        auto weigh = [&](uint32_t m, uint32_t r) {
+                            // first the half of the tokens whose weights are written first
+#pragma unroll
+                            for (uint32_t h = 0; h < 2; ++h) {
+                                if (!mbar_wait_one(bar(B_P + 2 * m + h), r & 1, &gave_up)) return false;
+                                tc_fence_after();
+#pragma unroll
+                                for (uint32_t x = h * 4; x < h * 4 + 4; ++x)
+                                    if (x < steps) tc_mma_ts(tmem + kO + m * D, tmem + kS + m * 128 + x * 8, b + ((x * 2048) >> 4), id_o, j > t.j0 || x > 0);
+                            }
+                            if (!more) tc_commit(bar(B_O + m));
+                            else issue_s(m, sk);
+                            return true;
+                        };
+                        ok = weigh(0, rounds0++) && (!two || weigh(1, rounds1++));
+                        if (!ok) break;
                         tc_commit(bar(B_EMPTY + sv));
                         if (more) tc_commit(bar(B_EMPTY + sk));
                     }
-                    __syncwarp();
                 }
+                // every product is complete before tensor memory is given back
+                tc_commit(bar(B_DONE));
+                const unsigned long long t0 = global_ns();
+                while (!mbar_try(bar(B_DONE), 0) && global_ns() - t0 < kWaitLimitNs) {}
             }
-            // every product is complete before tensor memory is given back
-            if (lane == 0) tc_commit(bar(B_DONE));
             __syncwarp();
-            const unsigned long long t0 = global_ns();
-            while (!mbar_try(bar(B_DONE), 0) && global_ns() - t0 < kWaitLimitNs) {}
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
@@ -283,32 +282,45 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         const uint32_t ts = tmem + kS + m * 128 + lanes, to = tmem + kO + m * D + lanes;
         // 1e-30: with a scale of 0 masked scores still become 2^-inf
         const float sl2 = fmaxf(fabsf(p.a.scale) * 1.4426950408889634f, 1e-30f);
-        const uint32_t flip = p.a.scale < 0.f ? 0x80008000u : 0u;       // a negative scale is one of -q
-        uint32_t rounds = 0, tiles = 0;
-        bool ok = true;
-        for (uint32_t i = blockIdx.x; i < n_work && ok; i += gridDim.x) {
-            const Work t = get_work<PREFIX>(g, p, i);
-            const uint32_t row = t.row0 + m * 128 + tid;               // (token, head) of the request
-            const uint32_t token = row / p.group;
-            const bool mine = m * 128 + tid < t.rows;
-            const uint32_t qh = t.head * p.group + row % p.group;
-            if (m * 128 >= t.rows) continue;
-            if (t.j0 < t.j1) {
-                // rows of Q in 128-byte swizzle, zeros behind the last; a half-warp per row and round
-                constexpr uint32_t C = D / 8;                          // 16-byte units per row
-#pragma unroll 4
-                for (uint32_t x = tid; x < 128 * C; x += 128) {
-                    const uint32_t r = x / C, c = x % C, rr = t.row0 + m * 128 + r;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (m * 128 + r < t.rows)
-                        v = *reinterpret_cast<const uint4 *>(p.a.q + (unsigned long long)(t.q0 + rr / p.group) * p.a.qs +
-                                                             ((t.head * p.group + rr % p.group) * D + c * 8) * 2);
-                    v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
-                    *reinterpret_cast<uint4 *>(smem + m * M::kQ + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
-                }
-                fence_async_smem();
-                mbar_arrive(bar(B_Q + m));
+        const unsigned long long sl22 = pack2(sl2, sl2);
+        const uint32_t magic = (0xFFFFFFFFu / p.group) + 1u;            // x / group for x < 2^26
+        auto per_group = [&](uint32_t x) { return p.group == 1 ? x : __umulhi(x, magic); };
+        // rows of Q in 128-byte swizzle, zeros behind the last
+        auto load_q = [&](const Work &t) {
+            constexpr uint32_t C = D / 8, R = 128 / C;                 // 16-byte units per row; rows per pass
+            const uint32_t c = tid % C;
+#pragma unroll
+            for (uint32_t x = 0; x < C; ++x) {
+                const uint32_t r = tid / C + x * R, y = t.rem0 + m * 128 + r, tok = per_group(y);
+                const bool there = m * 128 + r < t.rows;
+                const uint8_t *src = p.a.q + (unsigned long long)(t.q0 + t.tok0 + tok) * p.a.qs + ((t.head * p.group + y - tok * p.group) * D + c * 8) * 2;
+                cp_async16(base + m * M::kQ + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4), there ? src : p.a.q, there);
             }
+            cp_async_commit();
+        };
+        auto q_there = [&] {
+            cp_async_wait<0>();
+            fence_async_smem();
+            mbar_arrive(bar(B_Q + m));
+        };
+        uint32_t rounds = 0, tiles = 0, it = 0;                         // it: loads of the tiles before
+        bool ok = true;
+        uint32_t n = 0, i = nth_tile(0);
+        Work t = {};
+        // the next tile that has rows for this warpgroup
+        auto advance = [&] {
+            for (; (i = nth_tile(n)) < n_work; ++n) {
+                t = get_work<PREFIX>(g, p, i);
+                if (m * 128 < t.rows) return true;        // only a short tile has none for the second
+            }
+            return false;
+        };
+        bool have = advance();
+        if (have && t.j0 < t.j1) { load_q(t); q_there(); }
+        while (have && ok) {
+            const uint32_t y = t.rem0 + m * 128 + tid, tok = per_group(y), token = t.tok0 + tok;
+            const bool mine = m * 128 + tid < t.rows;
+            const uint32_t qh = t.head * p.group + y - tok * p.group;
             float top = -INFINITY, sum = 0.f;
             // columns of a round up to this one are seen by the row
             const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
@@ -328,8 +340,12 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 }
                 float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
 #pragma unroll
-                for (int c = 4; c < 128; c += 4) { x0 = fmaxf(x0, s[c]); x1 = fmaxf(x1, s[c + 1]); x2 = fmaxf(x2, s[c + 2]); x3 = fmaxf(x3, s[c + 3]); }
-                const float now = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * sl2;
+                for (int c = 4; c < 124; c += 8) {
+                    x0 = max3_nan(x0, s[c], s[c + 1]); x1 = max3_nan(x1, s[c + 2], s[c + 3]);
+                    x2 = max3_nan(x2, s[c + 4], s[c + 5]); x3 = max3_nan(x3, s[c + 6], s[c + 7]);
+                }
+                x0 = max3_nan(x0, s[124], s[125]); x1 = max3_nan(x1, s[126], s[127]);
+                const float now = max3_nan(max3_nan(x0, x1, x2), x3, x3) * sl2;
                 const bool grow = now > top + 8.f || (top == -INFINITY && now > -INFINITY);
                 if (__any_sync(0xFFFFFFFFu, grow)) {
                     const float f = grow ? exp2_approx(top - now) : 1.f;
@@ -346,62 +362,94 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         }
                     }
                 }
-                const float sub = top == -INFINITY ? 0.f : -top;
-                float y0 = 0.f, y1 = 0.f, y2 = 0.f, y3 = 0.f;
-#pragma unroll
-                for (int c = 0; c < 128; c += 4) {
-                    const float e0 = exp2_approx(fmaf(s[c], sl2, sub)), e1 = exp2_approx(fmaf(s[c + 1], sl2, sub));
-                    const float e2 = exp2_approx(fmaf(s[c + 2], sl2, sub)), e3 = exp2_approx(fmaf(s[c + 3], sl2, sub));
-                    y0 += e0; y1 += e1; y2 += e2; y3 += e3;
-                    u[c / 2] = T::pack(e0, e1); u[c / 2 + 1] = T::pack(e2, e3);
-                    if (c % 64 == 60) tmem_st32(ts + (c / 64) * 32, u + (c / 64) * 32);
+                // a NaN among the scores makes every weight one
+                const float sub = now != now ? now : top == -INFINITY ? 0.f : -top;
+                const unsigned long long sub2 = pack2(sub, sub);
+                if (m == 0 && t.held - j * kKv < min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16)) {
+                    // V behind the last token of the chain: leftovers of other requests, and a weight of zero does not
+                    // silence a NaN.  Rows up to the next step of 16 become zeros before this round's weights are announced.
+                    const uint32_t x = it + 2 * (j - t.j0) + 1, valid = t.held - j * kKv, rows = (t.len - j * kKv + 15) / 16 * 16;
+                    ok = mbar_wait(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1, &gave_up);
+                    if (!ok) break;
+                    uint8_t *v = smem + M::oRing + (x % M::kSlots) * M::kTile;
+                    for (uint32_t y = tid; y < (rows - valid) * (D / 8); y += 128) {
+                        const uint32_t c = y % (D / 8);
+                        *reinterpret_cast<uint4 *>(v + (c >> 3) * kHalf + (valid + y / (D / 8)) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
                 }
-                sum += (y0 + y1) + (y2 + y3);
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(bar(B_P + m));
+                unsigned long long sum0 = 0, sum1 = 0;
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) {
+                    float2 e[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const unsigned long long v = fma2(pack2(s[c + 2 * x], s[c + 2 * x + 1]), sl22, sub2);
+                        if (x == 3 && kPoly) e[x] = exp2_poly2(v);
+                        else { const float2 z = unpack2(v); e[x] = make_float2(exp2_approx(z.x), exp2_approx(z.y)); }
+                    }
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) u[c / 2 + x] = T::pack(e[x].x, e[x].y);
+                    sum0 = add2(sum0, add2(pack2(e[0].x, e[0].y), pack2(e[1].x, e[1].y)));
+                    sum1 = add2(sum1, add2(pack2(e[2].x, e[2].y), pack2(e[3].x, e[3].y)));
+                    if (c % 64 == 56) {
+                        tmem_st32(ts + (c / 64) * 32, u + (c / 64) * 32);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(bar(B_P + 2 * m + c / 64));
+                    }
+                }
+                const float2 z = unpack2(add2(sum0, sum1));
+                sum += z.x + z.y;
             }
             if (!ok) break;
+            // ---------------- rows out; the next tile's query rows are on their way meanwhile
+            const Work d = t;
+            n += 1;
+            it += 2 * (d.j1 - d.j0);
+            have = advance();
+            if (have && t.j0 < t.j1) load_q(t);
             const unsigned long long at = (PREFIX || p.splits > 1)
-                ? ((unsigned long long)t.split * (PREFIX ? p.a.n : p.a.total_q) + t.q0 + token) * p.a.q_heads + qh : 0ull;
-            if (t.j0 < t.j1) {
+                ? ((unsigned long long)d.split * (PREFIX ? p.a.n : p.a.total_q) + d.q0 + token) * p.a.q_heads + qh : 0ull;
+            if (d.j0 < d.j1) {
                 ok = mbar_wait(bar(B_O + m), tiles & 1, &gave_up);
                 if (!ok) break;
                 tiles += 1;
                 tc_fence_after();
             }
-            if (PREFIX || p.splits > 1) {
-                if (mine) p.parts.ml[at] = make_float2(top, sum);
-                if (t.j0 == t.j1) continue;
-            }
-            const float inv = 1.f / sum;
-            uint8_t *out = p.a.out + (unsigned long long)(t.q0 + token) * p.a.os + (unsigned long long)qh * D * 2;
+            if (have && t.j0 < t.j1) q_there();
+            if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top, sum);
+            if (d.j0 < d.j1) {
+                const float inv = 1.f / sum;
+                uint8_t *out = p.a.out + (unsigned long long)(d.q0 + token) * p.a.os + (unsigned long long)qh * D * 2;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tmem_ld32(o, to + c);
-                tmem_wait_ld();
-                if (mine && (PREFIX || p.splits > 1)) {
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(o, to + c);
+                    tmem_wait_ld();
+                    if (mine && (PREFIX || p.splits > 1)) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4 *>(p.parts.o + at * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                } else if (mine) {
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<uint4 *>(p.parts.o + at * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    } else if (mine) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 v;
-                        v.x = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                        v.y = T::pack(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                        v.z = T::pack(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                        v.w = T::pack(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                        *reinterpret_cast<uint4 *>(out + (c + e) * 2) = v;
+                        for (int e = 0; e < 32; e += 8) {
+                            uint4 v;
+                            v.x = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                            v.y = T::pack(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                            v.z = T::pack(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                            v.w = T::pack(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                            *reinterpret_cast<uint4 *>(out + (c + e) * 2) = v;
+                        }
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (!PREFIX && p.splits == 1 && mine && p.a.lse)
+                    p.a.lse[(unsigned long long)(d.q0 + token) * p.a.q_heads + qh] = top * 0.6931471805599453f + logf(sum);
+                tc_fence_before();     // the accumulator has been read: the next weights let products overwrite it
             }
-            if (!PREFIX && p.splits == 1 && mine && p.a.lse)
-                p.a.lse[(unsigned long long)(t.q0 + token) * p.a.q_heads + qh] = top * 0.6931471805599453f + logf(sum);
-            tc_fence_before();         // tensor memory has been read: the next tile's products may overwrite it
         }
+        cp_async_wait<0>();
     }
     tc_fence_before();
     __syncthreads();

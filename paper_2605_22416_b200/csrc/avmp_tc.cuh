@@ -54,6 +54,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return ok;
 }
 
+// The same for one thread on its own.
+__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+{
+    bool ok = false;
+#pragma unroll 1
+    for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try(bar, parity);
+    return ok || mbar_wait_slow(bar, parity, gave_up);
+}
+// One thread of a converged warp (the form the compiler knows as a single issuing thread).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+
 // One box of the page tensor: 64 elements of `rows` tokens of a run of heads, at (x, token, head, layer and part, slot).
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int token, int head,
                                               int part, int slot)
@@ -107,6 +123,7 @@ __device__ __forceinline__ unsigned long long tc_desc(uint32_t addr, uint32_t le
            (1ull << 46) | (2ull << 61);
 }
 // Instruction descriptor: 16-bit operands, 32-bit sums, M = 128.
+constexpr uint32_t kNegateA = 1u << 13;
 __device__ __forceinline__ constexpr uint32_t tc_idesc(bool f16, bool b_by_rows, uint32_t n)
 {
     return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_by_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
@@ -139,6 +156,58 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---- pairs of 32-bit floats in one instruction
+__device__ __forceinline__ unsigned long long pack2(float lo, float hi)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(unsigned long long v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Largest of three; a NaN wins.
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of a pair on the multiply-add pipe (the special-function unit gives 4 exponentials a cycle and scheduler and is what a
+// softmax runs out of first).  x is split into an integer n, by adding and taking away 1.5 * 2^23, and |f| <= 1/2;
+// 2^f is a polynomial of degree 4 fitted for least relative error (2.6e-6) on that interval, 2^n is added to the
+// exponent.  x <= 2^6; below -126 the result is 2^-126 or less instead of 0.
+__device__ __forceinline__ float2 exp2_poly2(unsigned long long x)
+{
+    float2 t = unpack2(x);
+    t.x = fmaxf(t.x, -126.f); t.y = fmaxf(t.y, -126.f);
+    const unsigned long long v = pack2(t.x, t.y);
+    const unsigned long long n = add2(v, pack2(12582912.f, 12582912.f));
+    const unsigned long long f = add2(v, fma2(n, pack2(-1.f, -1.f), pack2(12582912.f, 12582912.f)));
+    unsigned long long y = fma2(f, pack2(9.570101754e-03f, 9.570101754e-03f), pack2(5.591786031e-02f, 5.591786031e-02f));
+    y = fma2(y, f, pack2(2.402474483e-01f, 2.402474483e-01f));
+    y = fma2(y, f, pack2(6.931218147e-01f, 6.931218147e-01f));
+    y = fma2(y, f, pack2(9.999992614e-01f, 9.999992614e-01f));
+    const float2 m = unpack2(n), z = unpack2(y);
+    return make_float2(__uint_as_float(__float_as_uint(z.x) + (__float_as_uint(m.x) << 23)),
+                       __uint_as_float(__float_as_uint(z.y) + (__float_as_uint(m.y) << 23)));
+}
 
 // The pages as a five-dimensional tensor [slot][layer, K or V][head][token][dim] with boxes of box_tokens x box_heads rows of
 // 64 elements; dimensions need not be in memory order, so a box arrives sorted by head.  (avmp_attn.cu)
