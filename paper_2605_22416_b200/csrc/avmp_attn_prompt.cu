@@ -166,9 +166,10 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
 
     if (w >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (w == 8) {
-            // ---------------- loads
-            uint32_t it = 0;
+        if (w == 8 || w == 10) {
+            // ---------------- loads: K by one warp, V by another.  The lanes look the pages up a round ahead; one thread issues.
+            const uint32_t v = w == 8 ? 0 : 1;
+            uint32_t it = v;
             bool ok = true;
             for (uint32_t n = 0, i; (i = nth_tile(n)) < n_work && ok; ++n) {
                 const Work t = get_work<PREFIX>(g, p, i);
@@ -180,27 +181,30 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
                 };
                 uint32_t next = look(t.j0);
-                for (uint32_t j = t.j0; j < t.j1 && ok; ++j) {
+                for (uint32_t j = t.j0; j < t.j1 && ok; ++j, it += 2) {
                     const uint32_t slot = next;
-                    next = look(j + 1);
                     const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
-                    const uint32_t tok = (j * kKv + lane * p.box_tokens) % g.T;
-#pragma unroll
-                    for (int v = 0; v < 2; ++v, ++it) {
-                        const uint32_t s = it % M::kSlots, round = it / M::kSlots;
-                        if (round && !mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, &gave_up)) { ok = false; break; }
-                        if (lane == 0) mbar_expect(bar(B_FULL + s), boxes * p.box_tokens * D * 2);
-                        __syncwarp();
-                        if (slot != kInvalid)
+                    uint32_t tok = (j * kKv) % g.T;
+                    const uint32_t s = it % M::kSlots, round = it / M::kSlots, full = bar(B_FULL + s);
+                    ok = !round || mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, &gave_up);
+                    if (!ok) break;
+                    uint32_t dst = base + M::oRing + s * M::kTile;
+                    if (elect_one()) mbar_expect(full, boxes * p.box_tokens * D * 2);
+                    for (uint32_t b = 0; b < boxes; ++b) {
+                        const uint32_t page = __shfl_sync(0xFFFFFFFFu, slot, b);
+                        if (elect_one())
 #pragma unroll
                             for (int x = 0; x < D / 64; ++x)
-                                tma_load_page(base + M::oRing + s * M::kTile + x * kHalf + lane * p.box_tokens * 128, &map,
-                                              bar(B_FULL + s), x * 64, tok, t.head, p.a.layer * 2 + v, slot);
+                                tma_load_page(dst + x * kHalf, &map, full, x * 64, tok, t.head, p.a.layer * 2 + v, page);
+                        dst += p.box_tokens * 128;
+                        tok += p.box_tokens;
+                        if (tok >= g.T) tok = 0;
                     }
+                    next = look(j + 1);
                 }
             }
             if (*(volatile uint32_t *)&gave_up) {      // copies in flight land before this CTA's memory is given away
-                for (uint32_t x = it > M::kSlots ? it - M::kSlots : 0; x < it; ++x) {
+                for (uint32_t x = it > M::kSlots ? (it - M::kSlots + 1) & ~1u | v : v; x < it; x += 2) {
                     const unsigned long long t0 = global_ns();
                     while (!mbar_try(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1) && global_ns() - t0 < kWaitLimitNs) {}
                 }
