@@ -12,25 +12,46 @@
 
 namespace avmp {
 
-bool page_map(CUtensorMap *map, const Geom &g, uint32_t kv_heads, uint32_t head_dim, uint32_t box_tokens, uint32_t box_heads)
+namespace {
+
+template <int N>
+bool encode(CUtensorMap *map, const void *base, const cuuint64_t (&dims)[N], const cuuint64_t (&strides)[N - 1], const cuuint32_t (&box)[N])
 {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
-        void *fn = nullptr;
+    static const Encode fn = [] {
+        void *f = nullptr;
         cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
             q != cudaDriverEntryPointSuccess)
-            fn = nullptr;
-        return reinterpret_cast<Encode>(fn);
+            f = nullptr;
+        return reinterpret_cast<Encode>(f);
     }();
-    if (!encode) return false;
-    const cuuint64_t dims[5] = {head_dim, g.T, kv_heads, 2ull * g.na, g.V[0]};
-    const cuuint64_t strides[4] = {g.row_bytes, head_dim * 2ull, g.T * g.row_bytes, g.U[0]};
-    const cuuint32_t box[5] = {64, box_tokens, box_heads, 1, 1}, one[5] = {1, 1, 1, 1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, g.arena, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+    return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, N, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+bool page_map(CUtensorMap *map, const Geom &g, uint32_t kv_heads, uint32_t head_dim, uint32_t box_tokens, uint32_t box_heads)
+{
+    return encode<5>(map, g.arena, {head_dim, g.T, kv_heads, 2ull * g.na, g.V[0]},
+                  {g.row_bytes, head_dim * 2ull, g.T * g.row_bytes, g.U[0]}, {64, box_tokens, box_heads, 1, 1});
+}
+
+bool row_map(CUtensorMap *map, const Geom &g, uint32_t head_dim, uint32_t box_tokens)
+{
+    const uint64_t row = head_dim * 2ull;
+    return encode<5>(map, g.arena, {64, 8, head_dim / 64, g.T / 8, g.V[0] * (g.U[0] / row)}, {g.row_bytes, 128, 8 * g.row_bytes, row},
+                  {64, 8, head_dim / 64, box_tokens / 8, 1});
+}
+
+bool query_map(CUtensorMap *map, const void *q, uint32_t head_dim, uint32_t q_heads, uint32_t rows, unsigned long long stride,
+               uint32_t box_tokens, uint32_t box_heads)
+{
+    return encode<3>(map, q, {head_dim, q_heads, rows}, {head_dim * 2ull, stride}, {64, box_heads, box_tokens});
 }
 
 namespace {

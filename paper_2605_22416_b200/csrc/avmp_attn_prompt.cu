@@ -19,7 +19,8 @@ namespace {
 constexpr int kRows = 256;                    // query rows per tile
 constexpr int kKv = 128;                      // KV tokens per round
 constexpr int kCta = 384;
-constexpr bool kPoly = true;                 // a quarter of the exponentials on the multiply-add pipe
+constexpr int kAnnounce = 64;                 // the first 64 tokens' weights are announced behind the weights from here
+constexpr int kPoly = 0x08;                   // which of 8 pairs of exponentials go to the multiply-add pipe
 
 struct Tile { uint32_t k, b; };                          // list entry, row block
 struct Item { uint32_t req, len, q0, nq; };              // slot, held tokens, first row, rows
@@ -27,6 +28,7 @@ struct Item { uint32_t req, len, q0, nq; };              // slot, held tokens, f
 struct PromptArgs {
     AttnArgs a;
     uint32_t group, splits, box_tokens;
+    bool q_boxes;                 // query rows come in by tiled copies (groups of 1, 2, 4 .. 64)
     uint32_t cap;                 // entries of `tiles`
     uint32_t prefix_blocks;       // row blocks of the prefix pass
     uint32_t *n_tiles;
@@ -84,40 +86,85 @@ struct Work {
     uint32_t tok0, rem0;          // token and head in group of the tile's first row
 };
 
-template <bool PREFIX>
-__device__ __forceinline__ uint32_t tile_count(const PromptArgs &p)
-{
-    return (PREFIX ? p.prefix_blocks : *(volatile uint32_t *)p.n_tiles) * p.a.kv_heads * p.splits;
-}
 // The i-th tile of CTA c: the list runs from long tiles to short ones, every other pass over the CTAs backwards.
 __device__ __forceinline__ uint32_t nth_tile(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
 
-template <bool PREFIX>
-__device__ __forceinline__ Work get_work(const Geom &g, const PromptArgs &p, uint32_t i)
+__device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint32_t req, uint32_t held, uint32_t past, uint32_t q0,
+                                          uint32_t all_rows, uint32_t block, uint32_t head, uint32_t split, bool causal)
 {
     Work w;
-    w.split = i % p.splits;
-    i /= p.splits;
-    w.head = i % p.a.kv_heads;
-    i /= p.a.kv_heads;
-    if (PREFIX) {
-        w.k = 0; w.req = p.a.prefix; w.q0 = 0; w.past = 0;
-        w.row0 = i * kRows;
-        w.rows = min((uint32_t)kRows, p.a.n * p.group - w.row0);
-        w.len = w.held = w.req < g.R && g.r_state[w.req] != AVMP_REQ_EMPTY ? g.r_len[w.req] : 0u;
-    } else {
-        const Tile t = p.tiles[i];
-        const Item it = p.items[t.k];
-        w.k = t.k; w.req = it.req; w.q0 = it.q0; w.past = it.len - it.nq; w.held = it.len;
-        w.row0 = t.b * kRows;
-        w.rows = min((uint32_t)kRows, it.nq * p.group - w.row0);
-        w.len = w.past + (w.row0 + w.rows - 1) / p.group + 1;
-    }
+    w.k = k; w.req = req; w.held = held; w.past = past; w.q0 = q0; w.head = head; w.split = split;
+    w.row0 = block * kRows;
+    w.rows = min((uint32_t)kRows, all_rows - w.row0);
     w.tok0 = w.row0 / p.group; w.rem0 = w.row0 - w.tok0 * p.group;
+    w.len = causal ? past + (w.row0 + w.rows - 1) / p.group + 1 : held;
     const uint32_t rounds = (w.len + kKv - 1) / kKv;
-    w.j0 = (uint32_t)((unsigned long long)rounds * w.split / p.splits);
-    w.j1 = (uint32_t)((unsigned long long)rounds * (w.split + 1) / p.splits);
+    w.j0 = (uint32_t)((unsigned long long)rounds * split / p.splits);
+    w.j1 = (uint32_t)((unsigned long long)rounds * (split + 1) / p.splits);
     return w;
+}
+
+// One warp hands the CTA's tiles out, a few ahead of the others, through a ring in shared memory.  `give(work)` returns
+// false when the CTA stops.  A work item of 0 rows ends the list.
+//   prefix: row blocks of the whole batch.
+//   up to 32 list entries: a lane per entry; tiles in descending order of their KV rounds over all entries, so that the
+//     long ones start first.  How many row blocks have R rounds or more has a closed form per entry, so the i-th of
+//     that order is found by bisection over R and a sum over the lanes, without a list.
+//   more: the list that prompt_plan_kernel wrote.
+template <bool PREFIX, class Give>
+__device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Give give)
+{
+    const uint32_t lane = threadIdx.x % 32, per = p.a.kv_heads * p.splits;
+    Work w = {};
+    if (PREFIX) {
+        const uint32_t r = p.a.prefix, held = r < g.R && g.r_state[r] != AVMP_REQ_EMPTY ? g.r_len[r] : 0u;
+        for (uint32_t n = 0, i; (i = nth_tile(n)) < p.prefix_blocks * per; ++n)
+            if (!give(make_work(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
+    } else if (p.tiles) {
+        const uint32_t n_tiles = *(volatile uint32_t *)p.n_tiles;
+        for (uint32_t n = 0, i; (i = nth_tile(n)) < n_tiles * per; ++n) {
+            const Tile t = p.tiles[i / per];
+            const Item it = p.items[t.k];
+            if (!give(make_work(p, t.k, it.req, it.len, it.len - it.nq, it.q0, it.nq * p.group, t.b, i % per / p.splits, i % p.splits, true))) return;
+        }
+    } else {
+        uint32_t req = 0, held = 0, q0 = 0, nq = 0, blocks = 0, top = 0;
+        if (lane < p.a.n) {
+            req = p.a.reqs[lane]; q0 = p.a.cu[lane];
+            const uint32_t q1 = p.a.cu[lane + 1];
+            held = req < g.R && g.r_state[req] != AVMP_REQ_EMPTY ? g.r_len[req] : 0u;
+            if (held && q1 >= q0 && q1 <= p.a.total_q && q1 - q0 <= held) {
+                nq = q1 - q0;
+                blocks = (uint32_t)(((unsigned long long)nq * p.group + kRows - 1) / kRows);
+                if (nq) top = (held + kKv - 1) / kKv;
+            } else if (blockIdx.x == 0) {
+                record_error(g.st, AVMP_DEV_BAD_REQUEST);
+            }
+        }
+        const uint32_t past = held - nq, all = __reduce_add_sync(0xFFFFFFFFu, blocks), most = __reduce_max_sync(0xFFFFFFFFu, top);
+        // first row block of this lane's entry with at least R rounds (R >= 1)
+        auto first = [&](uint32_t R) {
+            const uint32_t x = (R - 1) * kKv;            // its last token stands at position x or later
+            if (x <= past) return 0u;
+            return x - past >= nq ? blocks : min(blocks, (uint32_t)((unsigned long long)(x - past) * p.group / kRows));
+        };
+        for (uint32_t n = 0, i; (i = nth_tile(n)) < all * per; ++n) {
+            const uint32_t e = i / per;
+            uint32_t lo = 1, hi = most + 1;              // count(lo) > e >= count(hi)
+            while (lo + 1 < hi) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (__reduce_add_sync(0xFFFFFFFFu, blocks - first(mid)) > e) lo = mid; else hi = mid;
+            }
+            const uint32_t f0 = first(lo), f1 = first(lo + 1), mine = f1 - f0;      // blocks with exactly lo rounds
+            const uint32_t incl = (uint32_t)warp_incl_scan(mine), at = e - __reduce_add_sync(0xFFFFFFFFu, blocks - f1);
+            const uint32_t owner = __ffs(__ballot_sync(0xFFFFFFFFu, incl > at)) - 1;
+            const uint32_t block = __shfl_sync(0xFFFFFFFFu, f0 + at - (incl - mine), owner);
+            if (!give(make_work(p, owner, __shfl_sync(0xFFFFFFFFu, req, owner), __shfl_sync(0xFFFFFFFFu, held, owner),
+                                __shfl_sync(0xFFFFFFFFu, past, owner), __shfl_sync(0xFFFFFFFFu, q0, owner),
+                                __shfl_sync(0xFFFFFFFFu, nq, owner) * p.group, block, i % per / p.splits, i % p.splits, true))) return;
+        }
+    }
+    give(w);
 }
 
 template <int D>
@@ -129,17 +176,20 @@ struct Smem {
     static constexpr uint32_t kTotal = oRing + kSlots * kTile + 1024;
 };
 
-enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_COUNT = 31 };
+enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_WORK = 31, B_TAKEN = 35, B_QFREE = 39, B_COUNT = 41 };
+constexpr uint32_t kWorks = 4;                // ring of work items
 
 template <class T, int D, bool PREFIX>
 __global__ void __launch_bounds__(kCta, 1)
-attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUtensorMap map)
+attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map)
 {
     using M = Smem<D>;
-    constexpr uint32_t kHalf = kKv * 128;                    // 64 columns of a K, V or Q tile
+    constexpr uint32_t kHalf = kKv * 128;                    // 64 columns of a Q tile
+    constexpr uint32_t kGroup = 8 * D * 2;                   // 8 tokens of a K or V tile: its column blocks one behind the other
     constexpr uint32_t kS = 0, kO = 256;                     // tensor memory columns: S0 S1 (P in their first half) O0 O1
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned long long bars_s[B_COUNT];
+    __shared__ Work works[kWorks];
     __shared__ uint32_t tmem_s, gave_up;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem), bars = smem_u32(bars_s);
@@ -149,12 +199,14 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         gave_up = 0;
         for (uint32_t i = 0; i < M::kSlots; ++i) { mbar_init(bar(B_FULL + i), 1); mbar_init(bar(B_EMPTY + i), 1); }
         for (uint32_t t = 0; t < 2; ++t) {
-            mbar_init(bar(B_Q + t), 128); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_O + t), 1);
+            mbar_init(bar(B_Q + t), p.q_boxes ? 1 : 128); mbar_init(bar(B_QFREE + t), 1); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_O + t), 1);
             mbar_init(bar(B_P + 2 * t), 128); mbar_init(bar(B_P + 2 * t + 1), 128);
         }
+        for (uint32_t i = 0; i < kWorks; ++i) { mbar_init(bar(B_WORK + i), 1); mbar_init(bar(B_TAKEN + i), 11); }
         mbar_init(bar(B_DONE), 1);
         mbar_fence_init();
         tma_prefetch_map(&map);
+        if (p.q_boxes) tma_prefetch_map(&q_map);
     }
     if (w == 9) tmem_alloc512(smem_u32(&tmem_s));
     tc_fence_before();
@@ -162,26 +214,49 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     tc_fence_after();
     const uint32_t tmem = tmem_s;
     pdl_prologue();
-    const uint32_t n_work = tile_count<PREFIX>(p);
 
     if (w >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (w == 8 || w == 10) {
             // ---------------- loads: K by one warp, V by another.  The lanes look the pages up a round ahead; one thread issues.
-            const uint32_t v = w == 8 ? 0 : 1;
-            uint32_t it = v;
+            const uint32_t v = w == 8 ? 0 : 1, page_rows = (uint32_t)(g.U[0] / (D * 2));
+            uint32_t it = v, q_tiles[2] = {0, 0};
             bool ok = true;
-            for (uint32_t n = 0, i; (i = nth_tile(n)) < n_work && ok; ++n) {
-                const Work t = get_work<PREFIX>(g, p, i);
-                const uint32_t *chain = g.r_chain + (unsigned long long)t.req * g.max_pages;
+            for (uint32_t n = 0; ok; ++n) {
+                ok = mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                if (!ok) break;
+                const Work &t = works[n % kWorks];
+                const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, head = t.head, token = t.q0 + t.tok0;
                 const uint32_t need = min((t.len + 15u) & ~15u, t.held);     // products run over whole steps of 16 tokens
+                const uint32_t *chain = g.r_chain + (unsigned long long)t.req * g.max_pages;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_TAKEN + n % kWorks));
+                if (rows == 0) break;
+                const uint32_t part_row = (p.a.layer * 2 + v) * g.T * p.a.kv_heads + head;
                 auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
                     const uint32_t tok = j * kKv + lane * p.box_tokens;
-                    if (j >= t.j1 || lane * p.box_tokens >= kKv || tok >= need) return kInvalid;
+                    if (j >= j1 || lane * p.box_tokens >= kKv || tok >= need) return kInvalid;
                     return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
                 };
-                uint32_t next = look(t.j0);
-                for (uint32_t j = t.j0; j < t.j1 && ok; ++j, it += 2) {
+                uint32_t next = look(j0);
+                if (v == 1 && p.q_boxes && j0 < j1) {
+                    // query rows, as soon as the products of the tile before have read theirs
+#pragma unroll
+                    for (uint32_t m = 0; m < 2; ++m) {
+                        if (m * 128 >= rows || !ok) continue;
+                        if (q_tiles[m]) ok = mbar_wait(bar(B_QFREE + m), (q_tiles[m] - 1) & 1, &gave_up);
+                        q_tiles[m] += 1;
+                        if (ok && elect_one()) {
+                            mbar_expect(bar(B_Q + m), M::kQ);
+#pragma unroll
+                            for (int x = 0; x < D / 64; ++x)
+                                tma_load_query(base + m * M::kQ + x * kHalf, &q_map, bar(B_Q + m), x * 64, head * p.group, token + m * 128 / p.group);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                }
+                for (uint32_t j = j0; j < j1; ++j, it += 2) {
                     const uint32_t slot = next;
                     const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
                     uint32_t tok = (j * kKv) % g.T;
@@ -192,11 +267,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     if (elect_one()) mbar_expect(full, boxes * p.box_tokens * D * 2);
                     for (uint32_t b = 0; b < boxes; ++b) {
                         const uint32_t page = __shfl_sync(0xFFFFFFFFu, slot, b);
-                        if (elect_one())
-#pragma unroll
-                            for (int x = 0; x < D / 64; ++x)
-                                tma_load_page(dst + x * kHalf, &map, full, x * 64, tok, t.head, p.a.layer * 2 + v, page);
-                        dst += p.box_tokens * 128;
+                        if (elect_one()) tma_load_rows(dst, &map, full, tok / 8, page * page_rows + part_row);
+                        dst += p.box_tokens * D * 2;
                         tok += p.box_tokens;
                         if (tok >= g.T) tok = 0;
                     }
@@ -211,45 +283,52 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
             }
         } else if (w == 9) {
-            // ---------------- products, all by one thread
+            // ---------------- products, all by one thread and for the two warpgroups in turn: that keeps them apart, so that one
+            // exponentiates while the tensor cores work for the other.  (With a thread for each they fall into step and
+            // contend for everything: 10.4 against 8.2 ms for the long prompt.)
             if (elect_one()) {
                 const uint32_t id_s = tc_idesc(T::kF16, false, kKv) | (p.a.scale < 0.f ? kNegateA : 0u);    // a negative scale is one of -q
                 constexpr uint32_t id_o = tc_idesc(T::kF16, true, D);
                 uint32_t it = 0, tiles0 = 0, tiles1 = 0, rounds0 = 0, rounds1 = 0;
                 bool ok = true;
-                const unsigned long long q_desc = tc_desc(base, 16), k_desc = tc_desc(base + M::oRing, 16), v_desc = tc_desc(base + M::oRing, kHalf);
+                const unsigned long long q_desc = tc_desc(base, 1024, 16), k_desc = tc_desc(base + M::oRing, kGroup, 16), v_desc = tc_desc(base + M::oRing, kGroup, 1024);
                 auto issue_s = [&](uint32_t m, uint32_t slot) {
                     const unsigned long long a = q_desc + ((m * M::kQ) >> 4), b = k_desc + ((slot * M::kTile) >> 4);
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
-                        const uint32_t off = ((x >> 2) * kHalf + (x & 3) * 32) >> 4;
-                        tc_mma_ss(tmem + kS + m * 128, a + off, b + off, id_s, x > 0);
+                        tc_mma_ss(tmem + kS + m * 128, a + (((x >> 2) * kHalf + (x & 3) * 32) >> 4), b + (((x >> 2) * 1024 + (x & 3) * 32) >> 4), id_s, x > 0);
                     }
                     tc_commit(bar(B_S + m));
                 };
                 auto full = [&](uint32_t n) { return mbar_wait_one(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, &gave_up); };
-                for (uint32_t n = 0, i; (i = nth_tile(n)) < n_work && ok; ++n) {
-                    const Work t = get_work<PREFIX>(g, p, i);
-                    if (t.j0 == t.j1) continue;
-                    const bool two = t.rows > 128;
+                for (uint32_t n = 0; ok; ++n) {
+                    ok = mbar_wait_one(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                    if (!ok) break;
+                    const Work &t = works[n % kWorks];
+                    const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, len = t.len;
+                    mbar_arrive(bar(B_TAKEN + n % kWorks));
+                    if (rows == 0) break;
+                    if (j0 == j1) continue;
+                    const bool two = rows > 128;
                     // K of round j is load it + 2 (j - j0), V the one behind it
                     ok = full(it) && mbar_wait_one(bar(B_Q), tiles0++ & 1, &gave_up);
                     if (!ok) break;
                     tc_fence_after();
                     issue_s(0, it % M::kSlots);
+                    if (j0 + 1 == j1) tc_commit(bar(B_QFREE));
                     if (two) {
                         ok = mbar_wait_one(bar(B_Q + 1), tiles1++ & 1, &gave_up);
                         if (!ok) break;
                         tc_fence_after();
                         issue_s(1, it % M::kSlots);
+                        if (j0 + 1 == j1) tc_commit(bar(B_QFREE + 1));
                     }
                     tc_commit(bar(B_EMPTY + it % M::kSlots));
-                    for (uint32_t j = t.j0; j < t.j1; ++j, it += 2) {
+                    ok = full(it + 1) && (j0 + 1 == j1 || full(it + 2));
+                    for (uint32_t j = j0; j < j1 && ok; ++j, it += 2) {
                         const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
-                        const bool more = j + 1 < t.j1;
-                        const uint32_t steps = min((uint32_t)kKv / 16, (t.len - j * kKv + 15) / 16);
-                        ok = full(it + 1) && (!more || full(it + 2));
-                        if (!ok) break;
+                        const bool more = j + 1 < j1;
+                        const uint32_t steps = min((uint32_t)kKv / 16, (len - j * kKv + 15) / 16);
                         const unsigned long long b = v_desc + ((sv * M::kTile) >> 4);
                         auto weigh = [&](uint32_t m, uint32_t r) {
                             // first the half of the tokens whose weights are written first
@@ -259,13 +338,18 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                                 tc_fence_after();
 #pragma unroll
                                 for (uint32_t x = h * 4; x < h * 4 + 4; ++x)
-                                    if (x < steps) tc_mma_ts(tmem + kO + m * D, tmem + kS + m * 128 + x * 8, b + ((x * 2048) >> 4), id_o, j > t.j0 || x > 0);
+                                    if (x < steps) tc_mma_ts(tmem + kO + m * D, tmem + kS + m * 128 + x * 8, b + ((x * 2 * kGroup) >> 4), id_o, j > j0 || x > 0);
                             }
-                            if (!more) tc_commit(bar(B_O + m));
-                            else issue_s(m, sk);
+                            if (more) issue_s(m, sk);
+                            else tc_commit(bar(B_O + m));
+                            if (j + 2 == j1) tc_commit(bar(B_QFREE + m));       // the last products with these query rows
                             return true;
                         };
-                        ok = weigh(0, rounds0++) && (!two || weigh(1, rounds1++));
+                        ok = weigh(0, rounds0++);
+                        // the next round's V and K: looked at here, where the tensor cores have work in hand (an mbarrier
+                        // costs this thread 100 to 250 cycles, and behind the last product they would be idle ones)
+                        if (more) ok = ok && full(it + 3) && (j + 2 == j1 || full(it + 4));
+                        ok = ok && (!two || weigh(1, rounds1++));
                         if (!ok) break;
                         tc_commit(bar(B_EMPTY + sv));
                         if (more) tc_commit(bar(B_EMPTY + sk));
@@ -277,9 +361,19 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 while (!mbar_try(bar(B_DONE), 0) && global_ns() - t0 < kWaitLimitNs) {}
             }
             __syncwarp();
+        } else {
+            // ---------------- tiles
+            uint32_t n = 0;
+            hand_out<PREFIX>(g, p, [&](const Work &t) {
+                if (n >= kWorks && !mbar_wait(bar(B_TAKEN + n % kWorks), (n / kWorks - 1) & 1, &gave_up)) return false;
+                if (lane == 0) { works[n % kWorks] = t; mbar_arrive(bar(B_WORK + n % kWorks)); }
+                __syncwarp();
+                n += 1;
+                return true;
+            });
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---------------- softmax: warpgroup m, one row per thread
         const uint32_t m = w >> 2, tid = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(w & 3) << 21;                 // this warp's quarter of the lanes
@@ -309,18 +403,23 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         };
         uint32_t rounds = 0, tiles = 0, it = 0;                         // it: loads of the tiles before
         bool ok = true;
-        uint32_t n = 0, i = nth_tile(0);
+        uint32_t n = 0;
         Work t = {};
-        // the next tile that has rows for this warpgroup
+        // the next tile that has rows for this warpgroup (a short one has none for the second)
         auto advance = [&] {
-            for (; (i = nth_tile(n)) < n_work; ++n) {
-                t = get_work<PREFIX>(g, p, i);
-                if (m * 128 < t.rows) return true;        // only a short tile has none for the second
+            for (;; ++n) {
+                ok = ok && mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                if (!ok) return false;
+                t = works[n % kWorks];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_TAKEN + n % kWorks));
+                if (t.rows == 0) return false;
+                if (m * 128 < t.rows) { n += 1; return true; }
+                it += 2 * (t.j1 - t.j0);
             }
-            return false;
         };
         bool have = advance();
-        if (have && t.j0 < t.j1) { load_q(t); q_there(); }
+        if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
         while (have && ok) {
             const uint32_t y = t.rem0 + m * 128 + tid, tok = per_group(y), token = t.tok0 + tok;
             const bool mine = m * 128 + tid < t.rows;
@@ -366,10 +465,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         }
                     }
                 }
-                // a NaN among the scores makes every weight one
-                const float sub = now != now ? now : top == -INFINITY ? 0.f : -top;
-                const unsigned long long sub2 = pack2(sub, sub);
-                if (m == 0 && t.held - j * kKv < min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16)) {
+                if (t.held - j * kKv < min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16)) {
                     // V behind the last token of the chain: leftovers of other requests, and a weight of zero does not
                     // silence a NaN.  Rows up to the next step of 16 become zeros before this round's weights are announced.
                     const uint32_t x = it + 2 * (j - t.j0) + 1, valid = t.held - j * kKv, rows = (t.len - j * kKv + 15) / 16 * 16;
@@ -377,42 +473,52 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     if (!ok) break;
                     uint8_t *v = smem + M::oRing + (x % M::kSlots) * M::kTile;
                     for (uint32_t y = tid; y < (rows - valid) * (D / 8); y += 128) {
-                        const uint32_t c = y % (D / 8);
-                        *reinterpret_cast<uint4 *>(v + (c >> 3) * kHalf + (valid + y / (D / 8)) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        const uint32_t c = y % (D / 8), r = valid + y / (D / 8);
+                        *reinterpret_cast<uint4 *>(v + (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_async_smem();
                 }
+                // a NaN among the scores makes every weight one
+                const float sub = now != now ? now : top == -INFINITY ? 0.f : -top;
+                const unsigned long long sub2 = pack2(sub, sub);
                 unsigned long long sum0 = 0, sum1 = 0;
+                // weights of 16 tokens at a time, rounded, to the first registers that are free again
 #pragma unroll
-                for (int c = 0; c < 128; c += 8) {
-                    float2 e[4];
+                for (int c = 0; c < 128; c += 16) {
+                    float2 e[8];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const unsigned long long v = fma2(pack2(s[c + 2 * x], s[c + 2 * x + 1]), sl22, sub2);
-                        if (x == 3 && kPoly) e[x] = exp2_poly2(v);
-                        else { const float2 z = unpack2(v); e[x] = make_float2(exp2_approx(z.x), exp2_approx(z.y)); }
+                    for (int y = 0; y < 8; ++y) {
+                        const unsigned long long v = fma2(pack2(s[c + 2 * y], s[c + 2 * y + 1]), sl22, sub2);
+                        if (kPoly >> y & 1) e[y] = exp2_poly2(v);
+                        else { const float2 z = unpack2(v); e[y] = make_float2(exp2_approx(z.x), exp2_approx(z.y)); }
                     }
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) u[c / 2 + x] = T::pack(e[x].x, e[x].y);
-                    sum0 = add2(sum0, add2(pack2(e[0].x, e[0].y), pack2(e[1].x, e[1].y)));
-                    sum1 = add2(sum1, add2(pack2(e[2].x, e[2].y), pack2(e[3].x, e[3].y)));
-                    if (c % 64 == 56) {
-                        tmem_st32(ts + (c / 64) * 32, u + (c / 64) * 32);
+                    for (int y = 0; y < 8; ++y) u[c / 2 + y] = T::pack(e[y].x, e[y].y);
+#pragma unroll
+                    for (int y = 0; y < 8; y += 4) {
+                        sum0 = add2(sum0, add2(pack2(e[y].x, e[y].y), pack2(e[y + 1].x, e[y + 1].y)));
+                        sum1 = add2(sum1, add2(pack2(e[y + 2].x, e[y + 2].y), pack2(e[y + 3].x, e[y + 3].y)));
+                    }
+                    if (c == 48) tmem_st32(ts, u);
+                    if (c == kAnnounce) {                    // the store has landed meanwhile
                         tmem_wait_st();
                         tc_fence_before();
-                        mbar_arrive(bar(B_P + 2 * m + c / 64));
+                        mbar_arrive(bar(B_P + 2 * m));
                     }
                 }
+                tmem_st32(ts + 32, u + 32);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar(B_P + 2 * m + 1));
                 const float2 z = unpack2(add2(sum0, sum1));
                 sum += z.x + z.y;
             }
             if (!ok) break;
-            // ---------------- rows out; the next tile's query rows are on their way meanwhile
+            // ---------------- rows out, while the tensor cores start on the next tile
             const Work d = t;
-            n += 1;
             it += 2 * (d.j1 - d.j0);
             have = advance();
-            if (have && t.j0 < t.j1) load_q(t);
+            if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
             const unsigned long long at = (PREFIX || p.splits > 1)
                 ? ((unsigned long long)d.split * (PREFIX ? p.a.n : p.a.total_q) + d.q0 + token) * p.a.q_heads + qh : 0ull;
             if (d.j0 < d.j1) {
@@ -421,7 +527,6 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 tiles += 1;
                 tc_fence_after();
             }
-            if (have && t.j0 < t.j1) q_there();
             if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top, sum);
             if (d.j0 < d.j1) {
                 const float inv = 1.f / sum;
@@ -515,11 +620,16 @@ template <class T, int D, bool PREFIX>
 cudaError_t tile_launch(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
 {
     CUtensorMap map;
-    if (!page_map(&map, g, p.a.kv_heads, p.a.head_dim, p.box_tokens, 1)) return cudaErrorNotSupported;
+    if (!row_map(&map, g, p.a.head_dim, p.box_tokens)) return cudaErrorNotSupported;
     auto kernel = attn_tile_kernel<T, D, PREFIX>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kTotal);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, p, map);
+    CUtensorMap q_map = {};
+    PromptArgs a = p;
+    const uint32_t rows = PREFIX ? p.a.n : p.a.total_q;
+    a.q_boxes = (p.group & (p.group - 1)) == 0 && rows &&
+                query_map(&q_map, p.a.q, p.a.head_dim, p.a.q_heads, rows, p.a.qs, 128 / p.group, p.group);
+    return launch_pdl(kernel, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, a, map, q_map);
 }
 template <bool PREFIX>
 cudaError_t tile_type(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
@@ -582,12 +692,18 @@ cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l
     const size_t rows = (size_t)p.splits * a.total_q * a.q_heads;
     p.parts.ml = reinterpret_cast<float2 *>(w);
     p.parts.o = reinterpret_cast<float *>(w + up256(rows * 8));
-    cudaError_t e = launch_pdl(prompt_plan_kernel, dim3(1), dim3(kStepThreads), 0, l.stream, g, p);
-    if (e != cudaSuccess) return e;
+    cudaError_t e = cudaSuccess;
+    if (a.n <= 32 && p.splits == 1) {
+        p.tiles = nullptr;                 // the tile kernel plans for itself
+    } else {
+        e = launch_pdl(prompt_plan_kernel, dim3(1), dim3(kStepThreads), 0, l.stream, g, p);
+        if (e != cudaSuccess) return e;
+        *launched += 1;
+    }
     const unsigned long long tiles = (unsigned long long)p.cap * a.kv_heads * p.splits;
     e = tile_type<false>(g, p, (uint32_t)min(tiles, (unsigned long long)l.n_sms), l);
     if (e != cudaSuccess) return e;
-    *launched += 2;
+    *launched += 1;
     if (p.splits > 1) {
         const uint32_t grid = (uint32_t)min((unsigned long long)p.cap * a.kv_heads, 4ull * l.n_sms);
         e = a.f16 ? join_type<F16>(p, grid, l) : join_type<Bf16>(p, grid, l);

@@ -115,11 +115,11 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, unsigned long 
                  :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
 // Shared-memory operand in rows of 128 bytes whose 16-byte units are permuted by the row index (128-byte swizzle):
-// groups of 8 rows 1024 bytes apart; `lead` is the distance between column blocks of 64 elements where the operand's
+// groups of 8 rows `group` bytes apart; `lead` is the distance between column blocks of 64 elements where the operand's
 // long axis runs along the rows.
-__device__ __forceinline__ unsigned long long tc_desc(uint32_t addr, uint32_t lead)
+__device__ __forceinline__ unsigned long long tc_desc(uint32_t addr, uint32_t group, uint32_t lead)
 {
-    return (unsigned long long)((addr & 0x3FFFFu) >> 4) | ((unsigned long long)(lead >> 4) << 16) | ((unsigned long long)(1024u >> 4) << 32) |
+    return (unsigned long long)((addr & 0x3FFFFu) >> 4) | ((unsigned long long)(lead >> 4) << 16) | ((unsigned long long)(group >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
 }
 // Instruction descriptor: 16-bit operands, 32-bit sums, M = 128.
@@ -212,6 +212,24 @@ __device__ __forceinline__ float2 exp2_poly2(unsigned long long x)
 // The pages as a five-dimensional tensor [slot][layer, K or V][head][token][dim] with boxes of box_tokens x box_heads rows of
 // 64 elements; dimensions need not be in memory order, so a box arrives sorted by head.  (avmp_attn.cu)
 bool page_map(CUtensorMap *map, const Geom &g, uint32_t kv_heads, uint32_t head_dim, uint32_t box_tokens, uint32_t box_heads);
+
+// The rows of one head as [head row of the arena][8-token group][64 columns][token of the group][column]: a box of whole
+// groups arrives as [group][column block][token], which is what the tensor cores read, in one copy.  The outermost
+// coordinate counts rows of head_dim elements from the arena's start (pages and heads lie at multiples of them).
+bool row_map(CUtensorMap *map, const Geom &g, uint32_t head_dim, uint32_t box_tokens);
+// Query rows as [token][query head][dim], boxes of box_tokens x box_heads rows of 64 elements.
+bool query_map(CUtensorMap *map, const void *q, uint32_t head_dim, uint32_t q_heads, uint32_t rows, unsigned long long stride,
+               uint32_t box_tokens, uint32_t box_heads);
+__device__ __forceinline__ void tma_load_query(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int head, int token)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(head), "r"(token) : "memory");
+}
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int group, int row)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%5, %5, %5, %3, %4}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(group), "r"(row), "r"(0) : "memory");
+}
 
 // What the parts of an attention call leave for the joining pass: sums over part of the tokens, not yet divided.
 struct Parts {
