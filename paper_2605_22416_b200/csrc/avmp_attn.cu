@@ -77,6 +77,7 @@ struct DecodeArgs {
     AttnArgs a;
     Split s;
     Plan ws;                   // in the workspace
+    uint2 *jobs;               // [P] per border: the request that is cut there for the first time and its last CTA, or kInvalid
     Parts own;                 // [2 P] cut requests, then [n] whole ones (only with a prefix)
     Parts pre;                 // [pre_parts][n]
     uint32_t pre_parts;
@@ -118,6 +119,23 @@ __global__ void __launch_bounds__(kStepThreads) attn_plan_kernel(const Geom g, c
     make_plan(g, d, d.ws, tmp, true);
 }
 
+// Four 8-column tiles of an accumulator row, two columns a lane: afterwards the lane holds the eight columns of tile `lane & 3`
+// (a 4 x 4 transpose inside the quad), so that rows are stored in 16-byte units.
+__device__ __forceinline__ void quad_transpose(uint32_t (&a)[4])
+{
+    const bool o1 = threadIdx.x & 1, o2 = threadIdx.x & 2;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o1 ? a[i] : a[i + 1], 1);
+        if (o1) a[i] = y; else a[i + 1] = y;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o2 ? a[i] : a[i + 2], 2);
+        if (o2) a[i] = y; else a[i + 2] = y;
+    }
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUtensorMap map)
@@ -139,7 +157,10 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
         mbar_fence_init();
         tma_prefetch_map(&map);
     }
-    pdl_prologue();
+    // Behind a prefix pass: that pass lets this kernel start once everything in front of itself is complete, and the two
+    // touch nothing in common, so there is nothing to wait for here (the joining pass needs both: see the end).
+    const bool behind = d.a.prefix != kInvalid && n <= kLocalPlanMax;
+    if (behind) asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); else pdl_prologue();
     Plan p = d.ws;
     if (n <= kLocalPlanMax) {
         p.cu = reinterpret_cast<uint32_t *>(smem + s.stages * s.stage_bytes);
@@ -210,6 +231,7 @@ drain:
             }
             if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
         }
+        if (behind) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
 
@@ -249,7 +271,7 @@ drain:
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         for (uint32_t c = st; c < seg_end; ++c, ++it) {
             const uint32_t stage = it % s.stages;
-            if (!mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, &gave_up)) return;
+            if (!mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, &gave_up)) return;      // (the loading warp still waits for the pass in front)
             const uint32_t base = ring + stage * s.stage_bytes;
             const uint32_t t0 = (c - begin) * step_tokens + share * 16;
             if (works && t0 < len) {
@@ -352,10 +374,16 @@ drain:
                 const float i0 = 1.f / l0, i1 = 1.f / l1;
                 uint8_t *out = d.a.out + k * d.a.os;
 #pragma unroll
-                for (int i = 0; i < ND; ++i) {
-                    if (row0) *reinterpret_cast<uint32_t *>(out + ((unsigned long long)qh0 * D + i * 8 + lc) * 2) = T::pack(o[i][0] * i0, o[i][1] * i0);
-                    if (row1) *reinterpret_cast<uint32_t *>(out + ((unsigned long long)qh1 * D + i * 8 + lc) * 2) = T::pack(o[i][2] * i1, o[i][3] * i1);
-                }
+                for (int i = 0; i < ND; i += 4)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) v[x] = T::pack(o[i + x][2 * r] * (r ? i1 : i0), o[i + x][2 * r + 1] * (r ? i1 : i0));
+                        quad_transpose(v);
+                        if (r ? row1 : row0)
+                            *reinterpret_cast<uint4 *>(out + ((unsigned long long)(r ? qh1 : qh0) * D + (i + (lane & 3)) * 8) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
                 if (d.a.lse && (lane & 3) == 0) {
                     constexpr float kLn2 = 0.6931471805599453f;
                     if (row0) d.a.lse[(unsigned long long)k * d.a.q_heads + qh0] = m0 * kLn2 + logf(l0);
@@ -365,10 +393,20 @@ drain:
                 const uint32_t part = cut_front ? 2 * blockIdx.x : cut_back ? 2 * blockIdx.x + 1 : 2 * s.ctas + k;
                 const unsigned long long at = (unsigned long long)part * d.a.q_heads;
 #pragma unroll
-                for (int i = 0; i < ND; ++i) {
-                    if (row0) *reinterpret_cast<float2 *>(d.own.o + (at + qh0) * D + i * 8 + lc) = make_float2(o[i][0], o[i][1]);
-                    if (row1) *reinterpret_cast<float2 *>(d.own.o + (at + qh1) * D + i * 8 + lc) = make_float2(o[i][2], o[i][3]);
-                }
+                for (int i = 0; i < ND; i += 4)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        uint32_t v[4], z[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) { v[x] = __float_as_uint(o[i + x][2 * r]); z[x] = __float_as_uint(o[i + x][2 * r + 1]); }
+                        quad_transpose(v);
+                        quad_transpose(z);
+                        if (r ? row1 : row0) {
+                            uint4 *to = reinterpret_cast<uint4 *>(d.own.o + (at + (r ? qh1 : qh0)) * D + (i + (lane & 3)) * 8);
+                            to[0] = make_uint4(v[0], z[0], v[1], z[1]);
+                            to[1] = make_uint4(v[2], z[2], v[3], z[3]);
+                        }
+                    }
                 if ((lane & 3) == 0) {
                     if (row0) d.own.ml[at + qh0] = make_float2(m0, l0);
                     if (row1) d.own.ml[at + qh1] = make_float2(m1, l1);
@@ -377,87 +415,85 @@ drain:
         }
         st = seg_end;
     }
-}
-
-// Sum of the parts of one (row, query head): `part(i)` gives the place of part i.  128 threads, four warps taking every fourth part.
-template <class T, int D, class F>
-__device__ __forceinline__ void join_parts(uint32_t parts, F part, uint8_t *out, float *lse)
-{
-    __shared__ float acc_s[4][D];
-    const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
-    float top = -INFINITY, den = 0.f;
-    for (uint32_t i = lane; i < parts; i += 32) {
-        float2 *ml; float *o;
-        part(i, o, ml);
-        if (ml->y != 0.f) top = fmaxf(top, ml->x);
-    }
-#pragma unroll
-    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-    for (uint32_t i = lane; i < parts; i += 32) {
-        float2 *ml; float *o;
-        part(i, o, ml);
-        if (ml->y != 0.f) den += ml->y * exp2_approx(ml->x - top);
-    }
-#pragma unroll
-    for (int x = 16; x; x >>= 1) den += __shfl_xor_sync(0xFFFFFFFFu, den, x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (lane < D / 4) {
-#pragma unroll 4
-        for (uint32_t i = w; i < parts; i += 4) {
-            float2 *ml; float *o;
-            part(i, o, ml);
-            const float2 e = *ml;
-            const float4 v = *reinterpret_cast<const float4 *>(o + lane * 4);
-            if (e.y != 0.f) {                      // an empty part wrote no sums
-                const float f = exp2_approx(e.x - top);
-                acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-            }
+    if (threadIdx.x == 0 && blockIdx.y == 0 && d.a.prefix == kInvalid && blockIdx.x < s.ctas) {
+        // the border behind this CTA, for the joining pass
+        uint2 job = make_uint2(kInvalid, 0);
+        if (last > first && last < total) {
+            const uint32_t c = find_owner(p.cu, 0, n, 0, last);
+            if (p.cu[c] != last && p.cu[c] >= first) job = make_uint2(c, (uint32_t)(((unsigned long long)p.cu[c + 1] * P - 1) / total));
         }
-        *reinterpret_cast<float4 *>(&acc_s[w][lane * 4]) = acc;
+        d.jobs[blockIdx.x] = job;
     }
-    __syncthreads();
-    for (int c = threadIdx.x * 2; c < D; c += 256) {
-        const float inv = 1.f / den;
-        const float x = acc_s[0][c] + acc_s[1][c] + acc_s[2][c] + acc_s[3][c];
-        const float y = acc_s[0][c + 1] + acc_s[1][c + 1] + acc_s[2][c + 1] + acc_s[3][c + 1];
-        *reinterpret_cast<uint32_t *>(out + c * 2) = T::pack(x * inv, y * inv);
-    }
-    if (lse && threadIdx.x == 0) *lse = top * 0.6931471805599453f + logf(den);
 }
 
-// Without a prefix: CTA (j, head) joins the request that the border between CTAs j and j + 1 cuts, if that is its first
-// cut.  With one: CTA (k, head) joins the prefix parts and the own parts of request k.
+// Joins parts, a warp per (request, query head): weights of 32 parts a time, one per lane, sums of 16 parts in flight.
+//   without a prefix: CTA (j, y) joins the request that the border behind decode CTA j cuts for the first time;
+//   with one: CTA (k, y) joins the prefix parts and the own parts of request k.
+// y counts groups of blockDim.x / 32 query heads.
 template <class T, int D>
 __global__ void __launch_bounds__(128) attn_join_kernel(const DecodeArgs d)
 {
     pdl_prologue();
-    const uint32_t n = d.a.n, head = blockIdx.y;
-    const unsigned long long total = d.ws.cu[n];
-    const uint32_t P = busy_ctas(d.s, total);
-    uint32_t k = blockIdx.x, own;
+    const uint32_t n = d.a.n, w = threadIdx.x / 32, lane = threadIdx.x % 32, head = blockIdx.y * (blockDim.x / 32) + w;
+    uint32_t k, i0, i1;
     if (d.a.prefix == kInvalid) {
-        if (blockIdx.x + 1 >= P) return;
-        const uint32_t border = (uint32_t)(total * (blockIdx.x + 1) / P), before = (uint32_t)(total * blockIdx.x / P);
-        k = find_owner(d.ws.cu, 0, n, 0, border);
-        if (d.ws.cu[k] == border || d.ws.cu[k] < before) return;
-        own = 0;
-    } else if (d.ws.len[k] == 0) {
-        return;
+        const uint2 job = d.jobs[blockIdx.x];
+        if (job.x == kInvalid) return;
+        k = job.x; i0 = blockIdx.x; i1 = job.y;
+    } else {
+        k = blockIdx.x;
+        const uint32_t begin = d.ws.cu[k], end = d.ws.cu[k + 1];
+        const unsigned long long total = d.ws.cu[n];
+        if (begin == end) return;
+        const uint32_t P = busy_ctas(d.s, total);
+        i0 = (uint32_t)((((unsigned long long)begin + 1) * P - 1) / total);
+        i1 = (uint32_t)(((unsigned long long)end * P - 1) / total);
     }
-    const uint32_t begin = d.ws.cu[k], end = d.ws.cu[k + 1];
-    const uint32_t i0 = (uint32_t)((((unsigned long long)begin + 1) * P - 1) / total), i1 = (uint32_t)(((unsigned long long)end * P - 1) / total);
-    own = i1 - i0 + 1;
-    join_parts<T, D>(own + d.pre_parts, [&](uint32_t i, float *&o, float2 *&ml) {
-        unsigned long long at;
-        if (i < d.pre_parts) {
-            at = ((unsigned long long)i * n + k) * d.a.q_heads + head;
-            o = d.pre.o + at * D; ml = d.pre.ml + at;
-        } else {
-            const uint32_t c = i0 + i - d.pre_parts;
-            at = (unsigned long long)(own == 1 ? 2 * d.s.ctas + k : c == i0 ? 2 * c + 1 : 2 * c) * d.a.q_heads + head;
-            o = d.own.o + at * D; ml = d.own.ml + at;
+    const uint32_t own = i1 - i0 + 1, parts = own + d.pre_parts;
+    if (head >= d.a.q_heads) return;
+    auto place = [&](uint32_t i) -> unsigned long long {      // of part i, in units of query heads
+        if (i < d.pre_parts) return ((unsigned long long)i * n + k) * d.a.q_heads + head;
+        const uint32_t c = i0 + i - d.pre_parts;
+        return (unsigned long long)(own == 1 ? 2 * d.s.ctas + k : c == i0 ? 2 * c + 1 : 2 * c) * d.a.q_heads + head;
+    };
+    auto sums = [&](uint32_t i) { return i < parts ? (i < d.pre_parts ? d.pre.ml : d.own.ml)[place(i)] : make_float2(0.f, 0.f); };
+    constexpr uint32_t kFly = 16;
+    float4 v[kFly], acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fetch = [&](uint32_t b) {
+#pragma unroll
+        for (uint32_t i = 0; i < kFly; ++i)
+            if (b + i < parts && lane < D / 4)
+                v[i] = *reinterpret_cast<const float4 *>((b + i < d.pre_parts ? d.pre.o : d.own.o) + place(b + i) * D + lane * 4);
+    };
+    float2 e = sums(lane);
+    fetch(0);
+    float top = e.y == 0.f ? -INFINITY : e.x;
+    for (uint32_t c = 32 + lane; c < parts; c += 32) { const float2 x = sums(c); if (x.y != 0.f) top = fmaxf(top, x.x); }
+#pragma unroll
+    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+    float den = 0.f;
+    for (uint32_t c = 0; c < parts; c += 32) {
+        if (c) e = sums(c + lane);
+        const float f = e.y == 0.f ? 0.f : exp2_approx(e.x - top);
+        den += e.y * f;
+#pragma unroll
+        for (uint32_t b = 0; b < 32; b += kFly) {
+            if (c + b >= parts) break;
+            if (c + b) fetch(c + b);
+#pragma unroll
+            for (uint32_t i = 0; i < kFly; ++i) {
+                const float fi = __shfl_sync(0xFFFFFFFFu, f, b + i);
+                if (fi != 0.f) { acc.x += v[i].x * fi; acc.y += v[i].y * fi; acc.z += v[i].z * fi; acc.w += v[i].w * fi; }   // an empty part wrote no sums
+            }
         }
-    }, d.a.out + k * d.a.os + (unsigned long long)head * D * 2, d.a.lse ? d.a.lse + (unsigned long long)k * d.a.q_heads + head : nullptr);
+    }
+#pragma unroll
+    for (int x = 16; x; x >>= 1) den += __shfl_xor_sync(0xFFFFFFFFu, den, x);
+    const float inv = 1.f / den;
+    if (lane < D / 4)
+        *reinterpret_cast<uint2 *>(d.a.out + k * d.a.os + ((unsigned long long)head * D + lane * 4) * 2) =
+            make_uint2(T::pack(acc.x * inv, acc.y * inv), T::pack(acc.z * inv, acc.w * inv));
+    if (d.a.lse && lane == 0) d.a.lse[(unsigned long long)k * d.a.q_heads + head] = top * 0.6931471805599453f + logf(den);
 }
 
 Split make_split(const Geom &g, const AttnArgs &a, int n_sms)
@@ -494,7 +530,7 @@ cudaError_t decode_launch(const Geom &g, const DecodeArgs &d, const CUtensorMap 
     const uint32_t jobs = d.a.prefix == kInvalid ? d.s.ctas - 1 : d.a.n;
     if (jobs == 0) return cudaSuccess;
     *launched += 1;
-    return launch_pdl(attn_join_kernel<T, D>, dim3(jobs, d.a.q_heads), dim3(128), 0, l.stream, d);
+    return launch_pdl(attn_join_kernel<T, D>, dim3(jobs, (d.a.q_heads + 3) / 4), dim3(128), 0, l.stream, d);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -511,6 +547,7 @@ cudaError_t launch_attn_decode(const Geom &g, const AttnArgs &a, const Launch &l
     d.ws.req = d.ws.cu + a.n + 1;
     d.ws.len = d.ws.req + a.n;
     w += up256(3 * ((size_t)a.n + 1) * 4);
+    d.jobs = reinterpret_cast<uint2 *>(w); w += up256((size_t)d.s.ctas * 8);
     const size_t own = (2 * (size_t)d.s.ctas + a.n) * a.q_heads;
     d.own.ml = reinterpret_cast<float2 *>(w); w += up256(own * 8);
     d.own.o = reinterpret_cast<float *>(w); w += up256(own * a.head_dim * 4);
@@ -530,7 +567,7 @@ cudaError_t launch_attn_decode(const Geom &g, const AttnArgs &a, const Launch &l
 size_t attn_ws_bytes(const Geom &g, uint32_t n, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms)
 {
     const size_t row = (size_t)head_dim * 4 + 8;
-    const size_t decode = up256(3 * ((size_t)n + 1) * 4) + (2 * (size_t)n_sms + n) * q_heads * row + 1024;
+    const size_t decode = up256(3 * ((size_t)n + 1) * 4) + up256((size_t)n_sms * 8) + (2 * (size_t)n_sms + n) * q_heads * row + 1024;
     return decode + attn_tile_ws_bytes(g, n, q_heads, kv_heads, head_dim, n_sms);
 }
 

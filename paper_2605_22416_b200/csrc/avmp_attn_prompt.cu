@@ -213,7 +213,13 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_s;
-    pdl_prologue();
+    if (PREFIX) {
+        // the decode kernel that follows starts without waiting for this one: let it only once all in front is complete
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    } else {
+        pdl_prologue();
+    }
 
     if (w >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
