@@ -99,7 +99,7 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
 // fp16 has little range: its scores (per row) and states and updates (per 16 rows of S) carry a power of two each.
 constexpr int kC = 64;                            // tokens per piece
 
-template <int DK, int DVT, int NT>
+template <int DK, int DVT, int NT, bool FOLD_K>
 struct PromptSmem {
     static constexpr int kQ = DK * 2 + 16;        // row strides: an odd number of 16-byte units, no bank conflicts
     static constexpr int kV = DVT * 2 + 16;
@@ -111,13 +111,15 @@ struct PromptSmem {
     static constexpr int kO = kC * kV;            // output staging
     static constexpr int kF = DVT * DK * 4;       // the state in 32 bits, thread-private places
     static constexpr int kW = kC * 2 * 4;         // running decays and tail weights
+    static constexpr int kParts = FOLD_K ? 3 * kC * kQ : 0;     // weighted keys in three parts
     static constexpr int oStage = 0;
     static constexpr int oS = oStage + NT * kBufs * kStage;
     static constexpr int oO = oS + kRing * kS;
     static constexpr int oF = oO + NT * kO;
     static constexpr int oW = oF + kF;
     static constexpr int oScale = oW + NT * kW;
-    static constexpr int kTotal = oScale + kRing * 4 * 4;
+    static constexpr int oParts = (oScale + kRing * 4 * 4 + 15) / 16 * 16;
+    static constexpr int kTotal = oParts + NT * kParts;
 };
 
 // A power of two that brings `m` (>= 0) to about 2^13; 1 for zero.
@@ -125,7 +127,7 @@ __device__ __forceinline__ float pow2_to_2_13(float m)
 {
     int e = (int)(__float_as_uint(m) >> 23) - 127;
     if (m == 0.f) e = 13;
-    e = max(-100, min(100, 13 - e));
+    e = max(-60, min(60, 13 - e));
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
@@ -133,7 +135,10 @@ template <class T, int DK, int DVT, int NT>
 __global__ void __launch_bounds__(NT * 128, 1)
 ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 {
-    using L = PromptSmem<DK, DVT, NT>;
+    // The weights of the update go to the keys where those are the fewer numbers (done once per team); for fp16, whose range
+    // needs a scale over all tokens, and for long keys to the values (16 columns a warp).
+    constexpr bool kFoldK = !T::kF16 && DK < 64;
+    using L = PromptSmem<DK, DVT, NT, kFoldK>;
     constexpr int KS = DK / 16;                   // k-steps of a product over dk
     constexpr int NV = DVT / 8;                   // 8-column tiles of the output
     constexpr int ND = DK / 8;                    // 8-column tiles of the state
@@ -161,33 +166,39 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
     float *sscale = reinterpret_cast<float *>(smem + L::oScale);
     S += ((unsigned long long)head * a.dv + tile * DVT) * DK;
 
-    const uint8_t *qg = a.q + grp * DK * 2, *kg = a.k + grp * DK * 2;
-    const uint8_t *vg = a.v + ((unsigned long long)head * a.dv + tile * DVT) * 2;
-    const uint8_t *gg = a.g + head * 4;
-    uint8_t *og = a.out + ((unsigned long long)head * a.dv + tile * DVT) * 2;
+    // Loads by running pointers: a thread copies the same 16-byte column of rows that are kRowsQ (kRowsV) apart.
+    constexpr int CK = DK / 8, CV = DVT / 8;               // 16-byte units per row
+    constexpr int kRowsQ = 128 / CK, kRowsV = 128 / CV;
+    const unsigned long long own_row = row0 + (unsigned long long)team * kC;
+    const uint8_t *qg = a.q + (own_row + tid / CK) * a.qs + grp * DK * 2 + tid % CK * 16;
+    const uint8_t *kg = a.k + (own_row + tid / CK) * a.ks + grp * DK * 2 + tid % CK * 16;
+    const uint8_t *vg = a.v + (own_row + tid / CV) * a.vs + ((unsigned long long)head * a.dv + tile * DVT) * 2 + tid % CV * 16;
+    const uint8_t *gg = a.g + (own_row + tid % kC) * a.gs + head * 4;
+    uint8_t *og = a.out + (own_row + w * 16 + lane / CV) * a.os + ((unsigned long long)head * a.dv + tile * DVT) * 2 + lane % CV * 16;
+    const unsigned long long q_next = (unsigned long long)NT * kC * a.qs, k_next = (unsigned long long)NT * kC * a.ks,
+                             v_next = (unsigned long long)NT * kC * a.vs, g_next = (unsigned long long)NT * kC * a.gs;
+    const uint32_t dq = tid / CK * L::kQ + tid % CK * 16, dvv = L::kStageV + tid / CV * L::kV + tid % CV * 16;
 
+    // Piece p of this team (called for p = team, team + NT, ... in turn).
     auto load = [&](uint32_t p, int buf) {
         if (p < pieces) {
-            const uint32_t base = smem_u32(stage0 + buf * L::kStage);
-            const uint32_t t0 = p * kC;
-            constexpr int CK = DK / 8, CV = DVT / 8;       // 16-byte units per row
-            for (int i = tid; i < kC * CK; i += 128) {
-                const uint32_t t = i / CK, c = i % CK;
-                const bool ok = t0 + t < len;
-                const unsigned long long row = row0 + (ok ? t0 + t : 0u);
-                cp_async16(base + L::kStageQ + t * L::kQ + c * 16, qg + row * a.qs + c * 16, ok);
-                cp_async16(base + L::kStageK + t * L::kQ + c * 16, kg + row * a.ks + c * 16, ok);
+            const uint32_t base = smem_u32(stage0 + buf * L::kStage), left = len - p * kC;
+#pragma unroll
+            for (int i = 0; i < kC / kRowsQ; ++i) {
+                const bool ok = (uint32_t)(tid / CK + i * kRowsQ) < left;
+                cp_async16(base + L::kStageQ + dq + i * kRowsQ * L::kQ, ok ? qg + i * kRowsQ * a.qs : a.q, ok);
+                cp_async16(base + L::kStageK + dq + i * kRowsQ * L::kQ, ok ? kg + i * kRowsQ * a.ks : a.k, ok);
             }
-            for (int i = tid; i < kC * CV; i += 128) {
-                const uint32_t t = i / CV, c = i % CV;
-                const bool ok = t0 + t < len;
-                const unsigned long long row = row0 + (ok ? t0 + t : 0u);
-                cp_async16(base + L::kStageV + t * L::kV + c * 16, vg + row * a.vs + c * 16, ok);
+#pragma unroll
+            for (int i = 0; i < kC / kRowsV; ++i) {
+                const bool ok = (uint32_t)(tid / CV + i * kRowsV) < left;
+                cp_async16(base + dvv + i * kRowsV * L::kV, ok ? vg + i * kRowsV * a.vs : a.v, ok);
             }
             if (tid < kC) {
-                const bool ok = t0 + tid < len;
-                cp_async4(base + L::kStageG + tid * 4, gg + (unsigned long long)(row0 + (ok ? t0 + tid : 0u)) * a.gs, ok);
+                const bool ok = (uint32_t)tid < left;
+                cp_async4(base + L::kStageG + tid * 4, ok ? gg : a.g, ok);
             }
+            qg += q_next; kg += k_next; vg += v_next; gg += g_next;
         }
         cp_async_commit();
     };
@@ -272,74 +283,116 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         }
         bar_sync(kTeamBar + team, 128);
 
-        // ---- scores of this warp's 16 rows against the tokens up to their own, decayed and rounded
+        uint8_t *parts = smem + L::oParts + team * L::kParts;
+        if (kFoldK) {
+            // keys times their tail weights, in three 16-bit parts
+#pragma unroll
+            for (int i = 0; i < kC / kRowsQ; ++i) {
+                const int t = tid / CK + i * kRowsQ;
+                const uint4 x = *reinterpret_cast<const uint4 *>(st + L::kStageK + dq + i * kRowsQ * L::kQ);
+                const float wj = wt[t];
+                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+                uint32_t hi[4], mi[4], lo[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    float2 f = T::unpack(in[y]);
+                    f.x *= wj; f.y *= wj;
+                    hi[y] = T::pack(f.x, f.y);
+                    float2 z = T::unpack(hi[y]);
+                    f.x -= z.x; f.y -= z.y;
+                    mi[y] = T::pack(f.x, f.y);
+                    z = T::unpack(mi[y]);
+                    lo[y] = T::pack(f.x - z.x, f.y - z.y);
+                }
+                uint8_t *to = parts + dq + i * kRowsQ * L::kQ;
+                *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(to + kC * L::kQ) = make_uint4(mi[0], mi[1], mi[2], mi[3]);
+                *reinterpret_cast<uint4 *>(to + 2 * kC * L::kQ) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+        }
+
+        // ---- scores of this warp's 16 rows.  Against earlier blocks of 16 tokens the decay is a row factor, from the block's
+        // front c_ref on, times a column factor up to it (both at most 1); inside the own block it is one per pair.
         uint32_t aq[KS][4];
 #pragma unroll
         for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + (w * 16 + (lane & 15)) * L::kQ + s * 32 + (lane >> 4) * 16);
-        const float c0 = cs[w * 16 + lr], c1 = cs[w * 16 + lr + 8];
+        const float c0 = cs[w * 16 + lr], c1 = cs[w * 16 + lr + 8], cref = w ? cs[w * 16 - 1] : 0.f;
+        auto score = [&](int j, float (&x)[2][4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[0][i] = x[1][i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                uint32_t b[4];
+                ldsm4(b, sk + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
+                T::mma(x[0], aq[s], b[0], b[1]);
+                T::mma(x[1], aq[s], b[2], b[3]);
+            }
+        };
+        auto weigh = [&](const uint32_t (&pa)[4], int j, float (&o)[NV][4]) {
+#pragma unroll
+            for (int n = 0; n < NV / 2; ++n) {
+                uint32_t b[4];
+                ldsm4_t(b, sv + (j * 16 + (lane & 15)) * L::kV + n * 32 + (lane >> 4) * 16);
+                T::mma(o[2 * n], pa, b[0], b[1]);
+                T::mma(o[2 * n + 1], pa, b[2], b[3]);
+            }
+        };
+        auto row_scale = [&](float m0, float m1, float &s0, float &s1) {      // fp16: scores of a row brought to 2^13
+#pragma unroll
+            for (int x = 1; x < 4; x <<= 1) {
+                m0 = fmaxf(m0, __shfl_xor_sync(0xFFFFFFFFu, m0, x));
+                m1 = fmaxf(m1, __shfl_xor_sync(0xFFFFFFFFu, m1, x));
+            }
+            s0 = pow2_to_2_13(m0); s1 = pow2_to_2_13(m1);
+        };
         float o[NV][4];
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
-        float inv0 = 1.f, inv1 = 1.f;
+        uint32_t own[4];                               // weights of the own block
+        float so0 = 1.f, so1 = 1.f, sd0 = 1.f, sd1 = 1.f;
         {
-            float sc[8][4];
+            float x[2][4], m0 = 0.f, m1 = 0.f;
+            score(w, x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {           // 16 tokens at a time
-                if (j > w) continue;
+            for (int h = 0; h < 2; ++h) {
+                const int t = h * 8 + lc;
+                const float2 ct = *reinterpret_cast<const float2 *>(cs + w * 16 + t);
+                x[h][0] = t <= lr ? x[h][0] * exp2_approx(c0 - ct.x) : 0.f;
+                x[h][1] = t + 1 <= lr ? x[h][1] * exp2_approx(c0 - ct.y) : 0.f;
+                x[h][2] = t <= lr + 8 ? x[h][2] * exp2_approx(c1 - ct.x) : 0.f;
+                x[h][3] = t + 1 <= lr + 8 ? x[h][3] * exp2_approx(c1 - ct.y) : 0.f;
+                if (T::kF16) { m0 = fmaxf(m0, fmaxf(fabsf(x[h][0]), fabsf(x[h][1]))); m1 = fmaxf(m1, fmaxf(fabsf(x[h][2]), fabsf(x[h][3]))); }
+            }
+            if (T::kF16) row_scale(m0, m1, sd0, sd1);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[2 * j][i] = sc[2 * j + 1][i] = 0.f;
+            for (int h = 0; h < 2; ++h) { own[2 * h] = T::pack(x[h][0] * sd0, x[h][1] * sd0); own[2 * h + 1] = T::pack(x[h][2] * sd1, x[h][3] * sd1); }
+        }
+        {
+            float x[3][2][4], m0 = 0.f, m1 = 0.f;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    uint32_t b[4];
-                    ldsm4(b, sk + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
-                    T::mma(sc[2 * j], aq[s], b[0], b[1]);
-                    T::mma(sc[2 * j + 1], aq[s], b[2], b[3]);
-                }
+            for (int j = 0; j < 3; ++j) {
+                if (j >= w) continue;
+                score(j, x[j]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int t = j * 16 + h * 8 + lc;
-                    const float2 ct = *reinterpret_cast<const float2 *>(cs + t);
-                    float *x = sc[2 * j + h];
-                    const int i0 = w * 16 + lr, i1 = i0 + 8;
-                    x[0] = t <= i0 ? x[0] * exp2_approx(c0 - ct.x) : 0.f;
-                    x[1] = t + 1 <= i0 ? x[1] * exp2_approx(c0 - ct.y) : 0.f;
-                    x[2] = t <= i1 ? x[2] * exp2_approx(c1 - ct.x) : 0.f;
-                    x[3] = t + 1 <= i1 ? x[3] * exp2_approx(c1 - ct.y) : 0.f;
+                    const float2 ct = *reinterpret_cast<const float2 *>(cs + j * 16 + h * 8 + lc);
+                    const float f0 = exp2_approx(cref - ct.x), f1 = exp2_approx(cref - ct.y);
+                    x[j][h][0] *= f0; x[j][h][1] *= f1; x[j][h][2] *= f0; x[j][h][3] *= f1;
+                    if (T::kF16) { m0 = fmaxf(m0, fmaxf(fabsf(x[j][h][0]), fabsf(x[j][h][1]))); m1 = fmaxf(m1, fmaxf(fabsf(x[j][h][2]), fabsf(x[j][h][3]))); }
                 }
             }
-            float s0 = 1.f, s1 = 1.f;
-            if (T::kF16) {
-                float m0 = 0.f, m1 = 0.f;
+            if (T::kF16) row_scale(m0, m1, so0, so1);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j <= 2 * w + 1) {
-                        m0 = fmaxf(m0, fmaxf(fabsf(sc[j][0]), fabsf(sc[j][1])));
-                        m1 = fmaxf(m1, fmaxf(fabsf(sc[j][2]), fabsf(sc[j][3])));
-                    }
-#pragma unroll
-                for (int x = 1; x < 4; x <<= 1) {
-                    m0 = fmaxf(m0, __shfl_xor_sync(0xFFFFFFFFu, m0, x));
-                    m1 = fmaxf(m1, __shfl_xor_sync(0xFFFFFFFFu, m1, x));
-                }
-                s0 = pow2_to_2_13(m0); s1 = pow2_to_2_13(m1);
-                inv0 = 1.f / s0; inv1 = 1.f / s1;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j > w) continue;
-                const uint32_t pa[4] = {T::pack(sc[2 * j][0] * s0, sc[2 * j][1] * s0), T::pack(sc[2 * j][2] * s1, sc[2 * j][3] * s1),
-                                        T::pack(sc[2 * j + 1][0] * s0, sc[2 * j + 1][1] * s0), T::pack(sc[2 * j + 1][2] * s1, sc[2 * j + 1][3] * s1)};
-#pragma unroll
-                for (int n = 0; n < NV / 2; ++n) {
-                    uint32_t b[4];
-                    ldsm4_t(b, sv + (j * 16 + (lane & 15)) * L::kV + n * 32 + (lane >> 4) * 16);
-                    T::mma(o[2 * n], pa, b[0], b[1]);
-                    T::mma(o[2 * n + 1], pa, b[2], b[3]);
-                }
+            for (int j = 0; j < 3; ++j) {
+                if (j >= w) continue;
+                const uint32_t pa[4] = {T::pack(x[j][0][0] * so0, x[j][0][1] * so0), T::pack(x[j][0][2] * so1, x[j][0][3] * so1),
+                                        T::pack(x[j][1][0] * so0, x[j][1][1] * so0), T::pack(x[j][1][2] * so1, x[j][1][3] * so1)};
+                weigh(pa, j, o);
             }
         }
+        if (kFoldK) bar_sync(kTeamBar + team, 128);    // the weighted keys are written
 
         // ---- this piece's own contribution to the state (16 rows of dv per owning warp)
         float ds[ND][4];
@@ -350,6 +403,22 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ds[n][i] = 0.f;
             float xs = 1.f;
+            if (kFoldK) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v[4];
+                    ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
+#pragma unroll
+                    for (int n = 0; n < ND / 2; ++n)
+#pragma unroll
+                        for (int y = 0; y < 3; ++y) {
+                            uint32_t b[4];
+                            ldsm4_t(b, smem_u32(parts) + y * kC * L::kQ + (j * 16 + (lane & 15)) * L::kQ + n * 32 + (lane >> 4) * 16);
+                            T::mma(ds[2 * n], v, b[0], b[1]);
+                            T::mma(ds[2 * n + 1], v, b[2], b[3]);
+                        }
+                }
+            }
             if (T::kF16) {
                 float m = 0.f;
 #pragma unroll
@@ -367,7 +436,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
                 dinv = 1.f / xs;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < (kFoldK ? 0 : 4); ++j) {
                 uint32_t v[4], hi[4], lo[4], lo2[4];
                 ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
@@ -416,7 +485,9 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         if (p + 1 < pieces) bar_arrive(1 + (team + 1) % NT, 256);
 
         // ---- what the earlier pieces add to the outputs
-        const float e0 = exp2_approx(c0), e1 = exp2_approx(c1);
+        // r * (earlier blocks + e^c_ref Q S^T), then the own block on top
+        const float r0 = exp2_approx(c0 - cref), r1 = exp2_approx(c1 - cref), er = exp2_approx(cref);
+        const float z0 = r0 * sd0 / so0, z1 = r1 * sd1 / so1, y0 = r0 * sd0 * er, y1 = r1 * sd1 * er;
         const uint32_t sb = smem_u32(smem + L::oS + (p % L::kRing) * L::kS);
 #pragma unroll
         for (int n = 0; n < NV / 2; ++n) {
@@ -431,12 +502,17 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
             const float sc = T::kF16 ? sscale[(p % L::kRing) * 4 + n] : 1.f;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float *y = o[2 * n + h];
-                const float z0 = e0 * sc, z1 = e1 * sc;
                 // a cleared state adds nothing, whatever it held
-                y[0] = y[0] * inv0 + (e0 == 0.f ? 0.f : x[h][0] * z0); y[1] = y[1] * inv0 + (e0 == 0.f ? 0.f : x[h][1] * z0);
-                y[2] = y[2] * inv1 + (e1 == 0.f ? 0.f : x[h][2] * z1); y[3] = y[3] * inv1 + (e1 == 0.f ? 0.f : x[h][3] * z1);
+                float *y = o[2 * n + h];
+                y[0] = fmaf(y[0], z0, y0 == 0.f ? 0.f : x[h][0] * (y0 * sc)); y[1] = fmaf(y[1], z0, y0 == 0.f ? 0.f : x[h][1] * (y0 * sc));
+                y[2] = fmaf(y[2], z1, y1 == 0.f ? 0.f : x[h][2] * (y1 * sc)); y[3] = fmaf(y[3], z1, y1 == 0.f ? 0.f : x[h][3] * (y1 * sc));
             }
+        }
+        weigh(own, w, o);
+        if (T::kF16) {
+            const float i0 = 1.f / sd0, i1 = 1.f / sd1;
+#pragma unroll
+            for (int n = 0; n < NV; ++n) { o[n][0] *= i0; o[n][1] *= i0; o[n][2] *= i1; o[n][3] *= i1; }
         }
         // ---- rows out, whole 16-byte units
         uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
@@ -447,12 +523,12 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         }
         __syncwarp();
 #pragma unroll
-        for (int i = lane; i < 16 * NV; i += 32) {
-            const uint32_t t = p * kC + w * 16 + i / NV, c = i % NV;
-            if (t < len)
-                *reinterpret_cast<uint4 *>(og + (unsigned long long)(row0 + t) * a.os + c * 16) =
-                    *reinterpret_cast<const uint4 *>(so + (i / NV) * L::kV + c * 16);
+        for (int i = 0; i < 16 * CV / 32; ++i) {
+            const uint32_t t = lane / CV + i * (32 / CV);
+            if (p * kC + w * 16 + t < len)
+                *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
         }
+        og += (unsigned long long)NT * kC * a.os;
         if (L::kBufs == 2) buf ^= 1;
         bar_sync(kTeamBar + team, 128);             // the stage may be filled again, cs and wt rewritten
         if (L::kBufs == 1) load(p + NT, 0);
@@ -474,7 +550,7 @@ cudaError_t step_dk(const Geom &g, const SsmArgs &a, const Launch &l)
 template <class T, int DK, int DVT, int NT>
 cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
 {
-    using L = PromptSmem<DK, DVT, NT>;
+    using L = PromptSmem<DK, DVT, NT, !T::kF16 && DK < 64>;
     static_assert(L::kTotal <= 227 * 1024, "shared memory of one CTA");
     auto kernel = ssm_prompt_kernel<T, DK, DVT, NT>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
