@@ -330,7 +330,7 @@ AVMP_API int avmp_scatter_ssm_layers(avmp_ctx *ctx, uint32_t first_layer, uint32
  * are those kernels, reading pages and blocks where they lie, so a step touches its cache once.
  * All rows ("tokens") of a batch are packed; a row stride of 0 in a descriptor means densely packed
  * rows.  Pointers to rows must be 16-byte aligned and row strides multiples of 16 bytes (decays: 4).
- * Outputs must not overlap inputs.  Nothing is allocated: where a call needs scratch it takes a caller's
+ * Outputs must not overlap inputs.  The context's device must be current.  Nothing is allocated: where a call needs scratch it takes a caller's
  * buffer, whose content need not be preserved and which two calls may share if they cannot overlap
  * on the GPU.  An item that only the device can see to be wrong (see each call) is skipped, its output
  * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST. */

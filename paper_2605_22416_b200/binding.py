@@ -179,7 +179,8 @@ def _ptr(x) -> Optional[int]:
 
 def _stream(s) -> Optional[int]:
     if s is None:
-        return torch.cuda.current_stream().cuda_stream or None
+        # the raw handle: building a torch.cuda.Stream costs 3 us, as much as a launch
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
     if isinstance(s, torch.cuda.Stream):
         return s.cuda_stream or None
     return int(s) or None

@@ -84,6 +84,13 @@ void fill_stats(const avmp_ctx *c, const DevState &d, avmp_stats *o)
     o->step_ns_migration_plan = (uint64_t)(d.cyc_mig * ns_per_cycle);
 }
 
+// The compute calls check that the context's device is the current one (the stream and the launch belong to it).
+inline bool device_ok(const avmp_ctx *c)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
 bool attn_desc_ok(const avmp_ctx *c, const avmp_attn_desc *d)
 {
     if (!d || d->type > AVMP_TYPE_F16 || d->rsvd || !std::isfinite(d->scale)) return false;
@@ -561,7 +568,7 @@ int avmp_attn_prompt(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, co
                      const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out, float *d_lse, void *d_workspace,
                      size_t workspace_bytes, void *stream)
 {
-    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
     if (n == 0) return AVMP_OK;
     if (!d_reqs || !d_cu_q || (((uintptr_t)d_reqs | (uintptr_t)d_cu_q | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
     if (total_q && (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15))) return AVMP_EINVAL;
@@ -580,7 +587,7 @@ int avmp_attn_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, co
                      uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes,
                      void *stream)
 {
-    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
     if (n == 0) return AVMP_OK;
     if (!d_reqs || (((uintptr_t)d_reqs | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
     if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return AVMP_EINVAL;
@@ -601,7 +608,7 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
                     const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume, const void *d_q, const void *d_k,
                     const void *d_v, const float *d_log_decay, void *d_out, void *, size_t, void *stream)
 {
-    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
     if (n == 0) return AVMP_OK;
     if (!d_reqs || !d_cu || (((uintptr_t)d_reqs | (uintptr_t)d_cu | (uintptr_t)d_resume) & 3)) return AVMP_EINVAL;
     if (total_tokens && !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
@@ -615,7 +622,7 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
 int avmp_ssm_step(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n, const void *d_q,
                   const void *d_k, const void *d_v, const float *d_log_decay, void *d_out, void *stream)
 {
-    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc)) return AVMP_EINVAL;
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
     if (n == 0) return AVMP_OK;
     if (!d_reqs || ((uintptr_t)d_reqs & 3) || !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
     if ((uint64_t)n * ((c->spec.ssm_state_elems + 1023u) / 1024u) >= (1ull << 31)) return AVMP_EINVAL;

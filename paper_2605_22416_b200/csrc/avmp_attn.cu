@@ -521,10 +521,9 @@ cudaError_t decode_launch(const Geom &g, const DecodeArgs &d, const CUtensorMap 
         *launched += 1;
     }
     const size_t smem = 1024 + d.s.stages * d.s.stage_bytes + (d.a.n <= kLocalPlanMax ? 3 * ((size_t)d.a.n + 1) * 4 : 0);
-    auto kernel = attn_decode_kernel<T, D>;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + kRingBytes + 3 * (kLocalPlanMax + 1) * 4);
+    e = allow_smem<attn_decode_kernel<T, D>>(l.device, 1024 + kRingBytes + 3 * (kLocalPlanMax + 1) * 4);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kernel, dim3(d.s.ctas, d.s.head_groups), dim3(kThreads), smem, l.stream, g, d, map);
+    e = launch_pdl(attn_decode_kernel<T, D>, dim3(d.s.ctas, d.s.head_groups), dim3(kThreads), smem, l.stream, g, d, map);
     if (e != cudaSuccess) return e;
     *launched += 1;
     const uint32_t jobs = d.a.prefix == kInvalid ? d.s.ctas - 1 : d.a.n;

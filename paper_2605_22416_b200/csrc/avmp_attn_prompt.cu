@@ -627,15 +627,14 @@ cudaError_t tile_launch(const Geom &g, const PromptArgs &p, uint32_t grid, const
 {
     CUtensorMap map;
     if (!row_map(&map, g, p.a.head_dim, p.box_tokens)) return cudaErrorNotSupported;
-    auto kernel = attn_tile_kernel<T, D, PREFIX>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kTotal);
+    const cudaError_t e = allow_smem<attn_tile_kernel<T, D, PREFIX>>(l.device, Smem<D>::kTotal);
     if (e != cudaSuccess) return e;
     CUtensorMap q_map = {};
     PromptArgs a = p;
     const uint32_t rows = PREFIX ? p.a.n : p.a.total_q;
     a.q_boxes = (p.group & (p.group - 1)) == 0 && rows &&
                 query_map(&q_map, p.a.q, p.a.head_dim, p.a.q_heads, rows, p.a.qs, 128 / p.group, p.group);
-    return launch_pdl(kernel, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, a, map, q_map);
+    return launch_pdl(attn_tile_kernel<T, D, PREFIX>, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, a, map, q_map);
 }
 template <bool PREFIX>
 cudaError_t tile_type(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)

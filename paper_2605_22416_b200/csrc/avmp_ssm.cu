@@ -11,30 +11,37 @@ namespace avmp {
 
 namespace {
 
-// The block of d_reqs[k]'s layer, or null (dead slot, or named by an earlier entry of the list: two entries would
-// update one state at the same time).  Whole CTA; `report` tells which CTA of an item counts the error.
-__device__ __forceinline__ float *ssm_item(const Geom &g, const SsmArgs &a, uint32_t k, bool report)
+// The block of d_reqs[k]'s layer, or null where the slot is dead.
+__device__ __forceinline__ float *ssm_block(const Geom &g, const SsmArgs &a, uint32_t r)
 {
-    const uint32_t r = a.reqs[k];
     uint32_t slot = kInvalid;
     if (r < g.R) {
         const uint32_t state = g.r_state[r], h = g.r_ssm[(unsigned long long)r * g.ns + a.layer];
         if (state == AVMP_REQ_LIVE && h != kInvalid) slot = g.VT[1][h & 0x7FFFFFFFu];
     }
+    return slot == kInvalid ? nullptr : reinterpret_cast<float *>(unit_ptr(g, AVMP_POOL_SSM, slot));
+}
+// Whether an earlier entry of the list names the same slot (two entries would update one state at the same time).  Whole CTA.
+__device__ __forceinline__ bool ssm_repeated(const SsmArgs &a, uint32_t k, uint32_t r)
+{
     bool dup = false;
     for (uint32_t j = threadIdx.x; j < k; j += blockDim.x) dup |= a.reqs[j] == r;
-    dup = __syncthreads_or(dup);
-    if (slot == kInvalid || dup) {
-        if (report && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
-        return nullptr;
-    }
-    return reinterpret_cast<float *>(unit_ptr(g, AVMP_POOL_SSM, slot));
+    return __syncthreads_or(dup);
+}
+// Both; `report` tells which CTA of an item counts the error.
+__device__ __forceinline__ float *ssm_item(const Geom &g, const SsmArgs &a, uint32_t k, bool report)
+{
+    const uint32_t r = a.reqs[k];
+    float *S = ssm_block(g, a, r);
+    if (ssm_repeated(a, k, r)) S = nullptr;
+    if (!S && report && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+    return S;
 }
 
 // ---------------------------------------------------------------- one token
 constexpr int kStepCta = 256;
 constexpr uint32_t kStepTile = kStepCta * 4;      // state elements a CTA touches per round (a float4 per thread)
-constexpr int kStepRounds = 4;                    // rounds whose loads are in flight together
+constexpr int kStepRounds = 2;                    // rounds whose loads are in flight together (1 GB of state: 415 us with 1, 401 with 2, 441 with 4)
 
 template <class T, int DK>
 __global__ void __launch_bounds__(kStepCta)
@@ -43,25 +50,33 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
     constexpr int LANES = DK / 4;                 // lanes that share a state row
     pdl_prologue();
     const uint32_t k = blockIdx.x / parts, part = blockIdx.x % parts;
-    float *S = ssm_item(g, a, k, part == 0);
-    if (!S) return;
+    const uint32_t r = a.reqs[k];
+    float *S = ssm_block(g, a, r);
     const uint32_t elems = a.heads * a.dv * DK, rep = a.heads / a.groups;
-    const uint32_t end = min(elems, (part + 1) * part_elems);
+    const uint32_t end = min(elems, (part + 1) * part_elems), own = threadIdx.x * 4;
     const uint8_t *qrow = a.q + k * a.qs, *krow = a.k + k * a.ks;
     const uint16_t *vrow = reinterpret_cast<const uint16_t *>(a.v + k * a.vs);
     const float *grow = reinterpret_cast<const float *>(a.g + k * a.gs);
     uint16_t *orow = reinterpret_cast<uint16_t *>(a.out + k * a.os);
-    const uint32_t col = (threadIdx.x * 4) % DK;
-    for (uint32_t e0 = part * part_elems + threadIdx.x * 4; e0 - threadIdx.x * 4 < end; e0 += kStepTile * kStepRounds) {
+    const uint32_t col = own % DK;
+    bool checked = false;
+    for (uint32_t e0 = part * part_elems; e0 < end; e0 += kStepTile * kStepRounds) {
         float4 s[kStepRounds];
 #pragma unroll
         for (int u = 0; u < kStepRounds; ++u) {
-            const uint32_t e = e0 + u * kStepTile;
-            if (e < end) s[u] = __ldcs(reinterpret_cast<const float4 *>(S + e));
+            const uint32_t e = e0 + own + u * kStepTile;
+            if (S && e < end) s[u] = *reinterpret_cast<const float4 *>(S + e);
+        }
+        if (!checked) {      // while the first loads are on their way
+            if (ssm_repeated(a, k, r) || !S) {
+                if (part == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+                return;
+            }
+            checked = true;
         }
 #pragma unroll
         for (int u = 0; u < kStepRounds; ++u) {
-            const uint32_t e = e0 + u * kStepTile;
+            const uint32_t e = e0 + own + u * kStepTile;
             float acc = 0.f;
             uint32_t row = 0;
             if (e < end) {
@@ -76,7 +91,7 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
                 s[u].y = w == 0.f ? v * k0.y : fmaf(w, s[u].y, v * k0.y);
                 s[u].z = w == 0.f ? v * k1.x : fmaf(w, s[u].z, v * k1.x);
                 s[u].w = w == 0.f ? v * k1.y : fmaf(w, s[u].w, v * k1.y);
-                __stcs(reinterpret_cast<float4 *>(S + e), s[u]);
+                *reinterpret_cast<float4 *>(S + e) = s[u];
                 acc = s[u].x * q0.x + s[u].y * q0.y + s[u].z * q1.x + s[u].w * q1.y;
             }
 #pragma unroll
@@ -552,11 +567,10 @@ cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
 {
     using L = PromptSmem<DK, DVT, NT, !T::kF16 && DK < 64>;
     static_assert(L::kTotal <= 227 * 1024, "shared memory of one CTA");
-    auto kernel = ssm_prompt_kernel<T, DK, DVT, NT>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
+    const cudaError_t e = allow_smem<ssm_prompt_kernel<T, DK, DVT, NT>>(l.device, L::kTotal);
     if (e != cudaSuccess) return e;
     const uint32_t tiles = a.dv / DVT;
-    return launch_pdl(kernel, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles);
+    return launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles);
 }
 template <class T, int DVT>
 cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l)
