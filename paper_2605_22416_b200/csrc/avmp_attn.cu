@@ -89,17 +89,15 @@ __device__ __forceinline__ uint32_t busy_ctas(const Split &s, unsigned long long
     return total < s.ctas ? (uint32_t)total : s.ctas;
 }
 
-__device__ __forceinline__ uint32_t held(const Geom &g, uint32_t r) { return r < g.R && g.r_state[r] != AVMP_REQ_EMPTY ? g.r_len[r] : 0u; }
-
 // The step list, by the whole CTA.  Bad entries own no step.
 __device__ __forceinline__ void make_plan(const Geom &g, const DecodeArgs &d, const Plan &to, unsigned long long *tmp, bool lead)
 {
     const uint32_t n = d.a.n, step = 16 * d.s.shares;
-    const bool dead = d.a.prefix != kInvalid && held(g, d.a.prefix) == 0;
+    const bool dead = d.a.prefix != kInvalid && held_tokens(g, d.a.prefix) == 0;
     const uint32_t per = (n + blockDim.x - 1) / blockDim.x, k0 = min(n, threadIdx.x * per), k1 = min(n, k0 + per);
     unsigned long long mine = 0, tot;
     for (uint32_t k = k0; k < k1; ++k) {
-        const uint32_t r = d.a.reqs[k], len = dead ? 0u : held(g, r);
+        const uint32_t r = d.a.reqs[k], own = held_tokens(g, r), len = dead ? 0u : own;
         if (lead && len == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
         to.req[k] = r; to.len[k] = len;
         mine += (len + step - 1) / step;

@@ -20,6 +20,7 @@ constexpr int kRows = 256;                    // query rows per tile
 constexpr int kKv = 128;                      // KV tokens per round
 constexpr int kCta = 384;
 constexpr int kAnnounce = 64;                 // the first 64 tokens' weights are announced behind the weights from here
+constexpr uint32_t kAhead = 2;                // rounds ahead that the prefix pass calls rows into L2
 constexpr int kPoly = 0x08;                   // which of 8 pairs of exponentials go to the multiply-add pipe
 
 struct Tile { uint32_t k, b; };                          // list entry, row block
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(kStepThreads) prompt_plan_kernel(const Geom g,
         Item it = {};
         if (k < p.a.n) {
             const uint32_t r = p.a.reqs[k], c0 = p.a.cu[k], c1 = p.a.cu[k + 1];
-            const uint32_t len = r < g.R && g.r_state[r] != AVMP_REQ_EMPTY ? g.r_len[r] : 0u;
+            const uint32_t len = held_tokens(g, r);
             it = Item{r, len, c0, c1 - c0};
             if (len && c1 >= c0 && c1 <= p.a.total_q && it.nq <= len) blocks = ((unsigned long long)it.nq * p.group + kRows - 1) / kRows;
             else record_error(g.st, AVMP_DEV_BAD_REQUEST);
@@ -117,7 +118,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
     const uint32_t lane = threadIdx.x % 32, per = p.a.kv_heads * p.splits;
     Work w = {};
     if (PREFIX) {
-        const uint32_t r = p.a.prefix, held = r < g.R && g.r_state[r] != AVMP_REQ_EMPTY ? g.r_len[r] : 0u;
+        const uint32_t r = p.a.prefix, held = held_tokens(g, r);
         for (uint32_t n = 0, i; (i = nth_tile(n)) < p.prefix_blocks * per; ++n)
             if (!give(make_work(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
     } else if (p.tiles) {
@@ -132,7 +133,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
         if (lane < p.a.n) {
             req = p.a.reqs[lane]; q0 = p.a.cu[lane];
             const uint32_t q1 = p.a.cu[lane + 1];
-            held = req < g.R && g.r_state[req] != AVMP_REQ_EMPTY ? g.r_len[req] : 0u;
+            held = held_tokens(g, req);
             if (held && q1 >= q0 && q1 <= p.a.total_q && q1 - q0 <= held) {
                 nq = q1 - q0;
                 blocks = (uint32_t)(((unsigned long long)nq * p.group + kRows - 1) / kRows);
@@ -279,6 +280,17 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         if (tok >= g.T) tok = 0;
                     }
                     next = look(j + 1);
+                    if (PREFIX) {
+                        // every row of the prefix is read once and comes from HBM: the round behind the ring is called into L2 now
+                        const uint32_t far = look(j + kAhead), n_far = __popc(__ballot_sync(0xFFFFFFFFu, far != kInvalid));
+                        uint32_t tok_far = ((j + kAhead) * kKv) % g.T;
+                        for (uint32_t b = 0; b < n_far; ++b) {
+                            const uint32_t page = __shfl_sync(0xFFFFFFFFu, far, b);
+                            if (elect_one()) tma_prefetch_rows(&map, tok_far / 8, page * page_rows + part_row);
+                            tok_far += p.box_tokens;
+                            if (tok_far >= g.T) tok_far = 0;
+                        }
+                    }
                 }
             }
             if (*(volatile uint32_t *)&gave_up) {      // copies in flight land before this CTA's memory is given away

@@ -7,6 +7,8 @@
 #include "avmp_dev.cuh"
 #include "avmp_mma.cuh"
 
+#include <type_traits>
+
 namespace avmp {
 
 namespace {
@@ -114,7 +116,7 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
 // fp16 has little range: its scores (per row) and states and updates (per 16 rows of S) carry a power of two each.
 constexpr int kC = 64;                            // tokens per piece
 
-template <int DK, int DVT, int NT, bool FOLD_K>
+template <int DK, int DVT, int NT>
 struct PromptSmem {
     static constexpr int kQ = DK * 2 + 16;        // row strides: an odd number of 16-byte units, no bank conflicts
     static constexpr int kV = DVT * 2 + 16;
@@ -126,15 +128,13 @@ struct PromptSmem {
     static constexpr int kO = kC * kV;            // output staging
     static constexpr int kF = DVT * DK * 4;       // the state in 32 bits, thread-private places
     static constexpr int kW = kC * 2 * 4;         // running decays and tail weights
-    static constexpr int kParts = FOLD_K ? 3 * kC * kQ : 0;     // weighted keys in three parts
     static constexpr int oStage = 0;
     static constexpr int oS = oStage + NT * kBufs * kStage;
     static constexpr int oO = oS + kRing * kS;
     static constexpr int oF = oO + NT * kO;
     static constexpr int oW = oF + kF;
     static constexpr int oScale = oW + NT * kW;
-    static constexpr int oParts = (oScale + kRing * 4 * 4 + 15) / 16 * 16;
-    static constexpr int kTotal = oParts + NT * kParts;
+    static constexpr int kTotal = oScale + kRing * 4 * 4;
 };
 
 // A power of two that brings `m` (>= 0) to about 2^13; 1 for zero.
@@ -150,10 +150,7 @@ template <class T, int DK, int DVT, int NT>
 __global__ void __launch_bounds__(NT * 128, 1)
 ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 {
-    // The weights of the update go to the keys where those are the fewer numbers (done once per team); for fp16, whose range
-    // needs a scale over all tokens, and for long keys to the values (16 columns a warp).
-    constexpr bool kFoldK = !T::kF16 && DK < 64;
-    using L = PromptSmem<DK, DVT, NT, kFoldK>;
+    using L = PromptSmem<DK, DVT, NT>;
     constexpr int KS = DK / 16;                   // k-steps of a product over dk
     constexpr int NV = DVT / 8;                   // 8-column tiles of the output
     constexpr int ND = DK / 8;                    // 8-column tiles of the state
@@ -298,34 +295,6 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         }
         bar_sync(kTeamBar + team, 128);
 
-        uint8_t *parts = smem + L::oParts + team * L::kParts;
-        if (kFoldK) {
-            // keys times their tail weights, in three 16-bit parts
-#pragma unroll
-            for (int i = 0; i < kC / kRowsQ; ++i) {
-                const int t = tid / CK + i * kRowsQ;
-                const uint4 x = *reinterpret_cast<const uint4 *>(st + L::kStageK + dq + i * kRowsQ * L::kQ);
-                const float wj = wt[t];
-                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-                uint32_t hi[4], mi[4], lo[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    float2 f = T::unpack(in[y]);
-                    f.x *= wj; f.y *= wj;
-                    hi[y] = T::pack(f.x, f.y);
-                    float2 z = T::unpack(hi[y]);
-                    f.x -= z.x; f.y -= z.y;
-                    mi[y] = T::pack(f.x, f.y);
-                    z = T::unpack(mi[y]);
-                    lo[y] = T::pack(f.x - z.x, f.y - z.y);
-                }
-                uint8_t *to = parts + dq + i * kRowsQ * L::kQ;
-                *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4 *>(to + kC * L::kQ) = make_uint4(mi[0], mi[1], mi[2], mi[3]);
-                *reinterpret_cast<uint4 *>(to + 2 * kC * L::kQ) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            }
-        }
-
         // ---- scores of this warp's 16 rows.  Against earlier blocks of 16 tokens the decay is a row factor, from the block's
         // front c_ref on, times a column factor up to it (both at most 1); inside the own block it is one per pair.
         uint32_t aq[KS][4];
@@ -367,73 +336,53 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
             for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
         uint32_t own[4];                               // weights of the own block
         float so0 = 1.f, so1 = 1.f, sd0 = 1.f, sd1 = 1.f;
-        {
-            float x[2][4], m0 = 0.f, m1 = 0.f;
-            score(w, x);
+        // (compiled for each warp of the team on its own: as a loop up to w its blocks ran one after the other)
+        auto scores = [&](auto which) {
+            constexpr int W = decltype(which)::value;
+            float x[W + 1][2][4], m0 = 0.f, m1 = 0.f, d0 = 0.f, d1 = 0.f;
+#pragma unroll
+            for (int j = 0; j <= W; ++j) score(j, x[j]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int t = h * 8 + lc;
-                const float2 ct = *reinterpret_cast<const float2 *>(cs + w * 16 + t);
-                x[h][0] = t <= lr ? x[h][0] * exp2_approx(c0 - ct.x) : 0.f;
-                x[h][1] = t + 1 <= lr ? x[h][1] * exp2_approx(c0 - ct.y) : 0.f;
-                x[h][2] = t <= lr + 8 ? x[h][2] * exp2_approx(c1 - ct.x) : 0.f;
-                x[h][3] = t + 1 <= lr + 8 ? x[h][3] * exp2_approx(c1 - ct.y) : 0.f;
-                if (T::kF16) { m0 = fmaxf(m0, fmaxf(fabsf(x[h][0]), fabsf(x[h][1]))); m1 = fmaxf(m1, fmaxf(fabsf(x[h][2]), fabsf(x[h][3]))); }
+                float *y = x[W][h];
+                const float2 ct = *reinterpret_cast<const float2 *>(cs + W * 16 + t);
+                y[0] = t <= lr ? y[0] * exp2_approx(c0 - ct.x) : 0.f;
+                y[1] = t + 1 <= lr ? y[1] * exp2_approx(c0 - ct.y) : 0.f;
+                y[2] = t <= lr + 8 ? y[2] * exp2_approx(c1 - ct.x) : 0.f;
+                y[3] = t + 1 <= lr + 8 ? y[3] * exp2_approx(c1 - ct.y) : 0.f;
+                if (T::kF16) { d0 = fmaxf(d0, fmaxf(fabsf(y[0]), fabsf(y[1]))); d1 = fmaxf(d1, fmaxf(fabsf(y[2]), fabsf(y[3]))); }
             }
-            if (T::kF16) row_scale(m0, m1, sd0, sd1);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) { own[2 * h] = T::pack(x[h][0] * sd0, x[h][1] * sd0); own[2 * h + 1] = T::pack(x[h][2] * sd1, x[h][3] * sd1); }
-        }
-        {
-            float x[3][2][4], m0 = 0.f, m1 = 0.f;
-#pragma unroll
-            for (int j = 0; j < 3; ++j) {
-                if (j >= w) continue;
-                score(j, x[j]);
+            for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float2 ct = *reinterpret_cast<const float2 *>(cs + j * 16 + h * 8 + lc);
                     const float f0 = exp2_approx(cref - ct.x), f1 = exp2_approx(cref - ct.y);
-                    x[j][h][0] *= f0; x[j][h][1] *= f1; x[j][h][2] *= f0; x[j][h][3] *= f1;
-                    if (T::kF16) { m0 = fmaxf(m0, fmaxf(fabsf(x[j][h][0]), fabsf(x[j][h][1]))); m1 = fmaxf(m1, fmaxf(fabsf(x[j][h][2]), fabsf(x[j][h][3]))); }
+                    float *y = x[j][h];
+                    y[0] *= f0; y[1] *= f1; y[2] *= f0; y[3] *= f1;
+                    if (T::kF16) { m0 = fmaxf(m0, fmaxf(fabsf(y[0]), fabsf(y[1]))); m1 = fmaxf(m1, fmaxf(fabsf(y[2]), fabsf(y[3]))); }
                 }
-            }
-            if (T::kF16) row_scale(m0, m1, so0, so1);
+            if (T::kF16) { row_scale(d0, d1, sd0, sd1); if (W) row_scale(m0, m1, so0, so1); }
 #pragma unroll
-            for (int j = 0; j < 3; ++j) {
-                if (j >= w) continue;
+            for (int h = 0; h < 2; ++h) { own[2 * h] = T::pack(x[W][h][0] * sd0, x[W][h][1] * sd0); own[2 * h + 1] = T::pack(x[W][h][2] * sd1, x[W][h][3] * sd1); }
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
                 const uint32_t pa[4] = {T::pack(x[j][0][0] * so0, x[j][0][1] * so0), T::pack(x[j][0][2] * so1, x[j][0][3] * so1),
                                         T::pack(x[j][1][0] * so0, x[j][1][1] * so0), T::pack(x[j][1][2] * so1, x[j][1][3] * so1)};
                 weigh(pa, j, o);
             }
-        }
-        if (kFoldK) bar_sync(kTeamBar + team, 128);    // the weighted keys are written
+        };
+        if (w == 0) scores(std::integral_constant<int, 0>{});
+        else if (w == 1) scores(std::integral_constant<int, 1>{});
+        else if (w == 2) scores(std::integral_constant<int, 2>{});
+        else scores(std::integral_constant<int, 3>{});
 
         // ---- this piece's own contribution to the state (16 rows of dv per owning warp)
         float ds[ND][4];
         float dinv = 1.f;
         if (w < WM) {
-#pragma unroll
-            for (int n = 0; n < ND; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ds[n][i] = 0.f;
             float xs = 1.f;
-            if (kFoldK) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t v[4];
-                    ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
-#pragma unroll
-                    for (int n = 0; n < ND / 2; ++n)
-#pragma unroll
-                        for (int y = 0; y < 3; ++y) {
-                            uint32_t b[4];
-                            ldsm4_t(b, smem_u32(parts) + y * kC * L::kQ + (j * 16 + (lane & 15)) * L::kQ + n * 32 + (lane >> 4) * 16);
-                            T::mma(ds[2 * n], v, b[0], b[1]);
-                            T::mma(ds[2 * n + 1], v, b[2], b[3]);
-                        }
-                }
-            }
             if (T::kF16) {
                 float m = 0.f;
 #pragma unroll
@@ -450,36 +399,50 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
                 xs = pow2_to_2_13(m);
                 dinv = 1.f / xs;
             }
+            // the parts' products are summed apart (short dependent chains) where registers allow it
+            constexpr int kSums = ND <= 4 ? (T::kF16 ? 2 : 3) : 1;
+            float part[kSums][ND][4];
 #pragma unroll
-            for (int j = 0; j < (kFoldK ? 0 : 4); ++j) {
-                uint32_t v[4], hi[4], lo[4], lo2[4];
+            for (int y = 0; y < kSums; ++y)
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) part[y][n][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t v[4], x3[3][4];
                 ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float2 x = T::unpack(v[i]);
                     const float2 y = *reinterpret_cast<const float2 *>(wt + j * 16 + (i >> 1) * 8 + lc);
                     x.x *= y.x * xs; x.y *= y.y * xs;
-                    hi[i] = T::pack(x.x, x.y);
-                    const float2 h = T::unpack(hi[i]);
+                    x3[0][i] = T::pack(x.x, x.y);
+                    const float2 h = T::unpack(x3[0][i]);
                     x.x -= h.x; x.y -= h.y;
-                    lo[i] = T::pack(x.x, x.y);
-                    const float2 m = T::unpack(lo[i]);
-                    lo2[i] = T::pack(x.x - m.x, x.y - m.y);
+                    x3[1][i] = T::pack(x.x, x.y);
+                    const float2 m = T::unpack(x3[1][i]);
+                    x3[2][i] = T::pack(x.x - m.x, x.y - m.y);
                 }
 #pragma unroll
                 for (int n = 0; n < ND / 2; ++n) {
                     uint32_t b[4];
                     ldsm4_t(b, sk + (j * 16 + (lane & 15)) * L::kQ + n * 32 + (lane >> 4) * 16);
-                    T::mma(ds[2 * n], hi, b[0], b[1]);
-                    T::mma(ds[2 * n + 1], hi, b[2], b[3]);
-                    T::mma(ds[2 * n], lo, b[0], b[1]);
-                    T::mma(ds[2 * n + 1], lo, b[2], b[3]);
-                    if (!T::kF16) {
-                        T::mma(ds[2 * n], lo2, b[0], b[1]);
-                        T::mma(ds[2 * n + 1], lo2, b[2], b[3]);
+#pragma unroll
+                    for (int y = 0; y < (T::kF16 ? 2 : 3); ++y) {
+                        T::mma(part[y % kSums][2 * n], x3[y], b[0], b[1]);
+                        T::mma(part[y % kSums][2 * n + 1], x3[y], b[2], b[3]);
                     }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ds[n][i] = part[kSums - 1][n][i];
+#pragma unroll
+                    for (int y = kSums - 2; y >= 0; --y) ds[n][i] += part[y][n][i];
+                }
         }
 
         // ---- hand-over: wait for the state in front of this piece, pass the one behind it on at once
@@ -565,7 +528,7 @@ cudaError_t step_dk(const Geom &g, const SsmArgs &a, const Launch &l)
 template <class T, int DK, int DVT, int NT>
 cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
 {
-    using L = PromptSmem<DK, DVT, NT, !T::kF16 && DK < 64>;
+    using L = PromptSmem<DK, DVT, NT>;
     static_assert(L::kTotal <= 227 * 1024, "shared memory of one CTA");
     const cudaError_t e = allow_smem<ssm_prompt_kernel<T, DK, DVT, NT>>(l.device, L::kTotal);
     if (e != cudaSuccess) return e;

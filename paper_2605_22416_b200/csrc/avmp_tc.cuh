@@ -225,10 +225,21 @@ __device__ __forceinline__ void tma_load_query(uint32_t dst, const CUtensorMap *
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(head), "r"(token) : "memory");
 }
+__device__ __forceinline__ void tma_prefetch_rows(const CUtensorMap *map, int group, int row)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global.tile [%0, {%3, %3, %3, %1, %2}];" :: "l"(map), "r"(group), "r"(row), "r"(0) : "memory");
+}
 __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *map, uint32_t bar, int group, int row)
 {
     asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%5, %5, %5, %3, %4}], [%2];"
                  :: "r"(dst), "l"(map), "r"(bar), "r"(group), "r"(row), "r"(0) : "memory");
+}
+
+// Tokens that a slot's chain holds; 0 for a slot that is empty or out of range.  Both tables are read at once.
+__device__ __forceinline__ uint32_t held_tokens(const Geom &g, uint32_t r)
+{
+    const uint32_t i = r < g.R ? r : 0u, state = g.r_state[i], len = g.r_len[i];
+    return r < g.R && state != AVMP_REQ_EMPTY ? len : 0u;
 }
 
 // What the parts of an attention call leave for the joining pass: sums over part of the tokens, not yet divided.
