@@ -387,7 +387,7 @@ AVMP_API size_t avmp_ssm_workspace_bytes(const avmp_ctx *ctx, const avmp_ssm_des
  * of them is left in its block.  d_resume[k] != 0: start from the state in the block; 0, or d_resume NULL:
  * from zero (a fresh block holds leftovers), so that a request without rows gets a zero state.
  * Skipped items: a slot that is not LIVE, a slot that an earlier entry of the list names, offsets that
- * decrease or pass total_tokens.  n_reqs <= max_requests. */
+ * decrease or pass total_tokens.  n_reqs <= max_requests; total_tokens < 2^31. */
 AVMP_API int avmp_ssm_prompt(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs,
                              uint32_t n_reqs, const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume,
                              const void *d_q, const void *d_k, const void *d_v, const float *d_log_decay, void *d_out,

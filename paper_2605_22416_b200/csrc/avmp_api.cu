@@ -612,7 +612,7 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
     if (n == 0) return AVMP_OK;
     if (!d_reqs || !d_cu || (((uintptr_t)d_reqs | (uintptr_t)d_cu | (uintptr_t)d_resume) & 3)) return AVMP_EINVAL;
     if (total_tokens && !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
-    if ((uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
+    if (total_tokens >= (1u << 31) || (uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
     SsmArgs a = ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out);
     a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
     c->launches += 1;

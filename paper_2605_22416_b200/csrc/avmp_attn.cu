@@ -15,7 +15,8 @@ namespace avmp {
 namespace {
 
 template <int N>
-bool encode(CUtensorMap *map, const void *base, const cuuint64_t (&dims)[N], const cuuint64_t (&strides)[N - 1], const cuuint32_t (&box)[N])
+bool encode(CUtensorMap *map, const void *base, const cuuint64_t (&dims)[N], const cuuint64_t (&strides)[N - 1], const cuuint32_t (&box)[N],
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -30,7 +31,7 @@ bool encode(CUtensorMap *map, const void *base, const cuuint64_t (&dims)[N], con
     }();
     const cuuint32_t one[5] = {1, 1, 1, 1, 1};
     return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, N, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                    swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -46,6 +47,12 @@ bool row_map(CUtensorMap *map, const Geom &g, uint32_t head_dim, uint32_t box_to
     const uint64_t row = head_dim * 2ull;
     return encode<5>(map, g.arena, {64, 8, head_dim / 64, g.T / 8, g.V[0] * (g.U[0] / row)}, {g.row_bytes, 128, 8 * g.row_bytes, row},
                   {64, 8, head_dim / 64, box_tokens / 8, 1});
+}
+
+bool rows_map(CUtensorMap *map, const void *p, uint32_t row_elems, uint32_t n_rows, unsigned long long stride, uint32_t columns, uint32_t rows)
+{
+    return encode<2>(map, p, {row_elems, n_rows}, {stride}, {columns, rows},
+                     columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : columns == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
 }
 
 bool query_map(CUtensorMap *map, const void *q, uint32_t head_dim, uint32_t q_heads, uint32_t rows, unsigned long long stride,

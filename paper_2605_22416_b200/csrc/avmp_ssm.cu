@@ -4,8 +4,7 @@
 // ssm_step_kernel     one token per request: every state element is read once and written once, bound by HBM.
 // ssm_prompt_kernel   whole prompts by pieces of 64 tokens: inside a piece the recurrence is two triangular
 //                     products, between pieces only the state is carried.
-#include "avmp_dev.cuh"
-#include "avmp_mma.cuh"
+#include "avmp_tc.cuh"
 
 #include <type_traits>
 
@@ -118,11 +117,14 @@ constexpr int kC = 64;                            // tokens per piece
 
 template <int DK, int DVT, int NT>
 struct PromptSmem {
-    static constexpr int kQ = DK * 2 + 16;        // row strides: an odd number of 16-byte units, no bank conflicts
-    static constexpr int kV = DVT * 2 + 16;
-    static constexpr int kStageQ = 0, kStageK = kC * kQ, kStageV = 2 * kC * kQ, kStageG = kStageV + kC * kV;
-    static constexpr int kStage = kStageG + kC * 4;
-    static constexpr int kBufs = DK == 128 ? 1 : 2;          // loads run one piece ahead where the memory allows it
+    // A stage holds the rows as tiled copies leave them, their 16-byte units permuted against bank conflicts (see `unit`);
+    // everything else has rows of an odd number of 16-byte units.
+    static constexpr int kRowK = DK < 64 ? DK * 2 : 128, kBlocksK = DK == 128 ? 2 : 1;   // 128 columns: two blocks of 64
+    static constexpr int kRowV = DVT * 2;
+    static constexpr int kStageV = 0, kStageQ = kC * kRowV, kStageK = kStageQ + kC * DK * 2, kStageG = kStageK + kC * DK * 2;
+    static constexpr int kStage = (kStageG + kC * 4 + 1023) / 1024 * 1024;
+    static constexpr int kQ = DK * 2 + 16, kV = DVT * 2 + 16;
+    static constexpr int kBufs = DK == 128 ? 1 : 2;          // loads run a team's next piece ahead where the memory allows it
     static constexpr int kRing = NT + 2;          // copies of the state in 16 bits: see the hand-over
     static constexpr int kS = DVT * kQ;
     static constexpr int kO = kC * kV;            // output staging
@@ -134,8 +136,17 @@ struct PromptSmem {
     static constexpr int oF = oO + NT * kO;
     static constexpr int oW = oF + kF;
     static constexpr int oScale = oW + NT * kW;
-    static constexpr int kTotal = oScale + kRing * 4 * 4;
+    static constexpr int oBars = oScale + kRing * 4 * 4;
+    static constexpr int kTotal = oBars + NT * kBufs * 8 + 1024;
 };
+
+// Place of 16-byte unit c of row r where rows of ROW bytes were copied with the swizzle of that width.
+template <int ROW>
+__device__ __forceinline__ uint32_t unit(uint32_t r, uint32_t c)
+{
+    const uint32_t x = ROW == 128 ? r & 7 : ROW == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+    return r * ROW + ((c ^ x) << 4);
+}
 
 // A power of two that brings `m` (>= 0) to about 2^13; 1 for zero.
 __device__ __forceinline__ float pow2_to_2_13(float m)
@@ -147,15 +158,23 @@ __device__ __forceinline__ float pow2_to_2_13(float m)
 }
 
 template <class T, int DK, int DVT, int NT>
-__global__ void __launch_bounds__(NT * 128, 1)
-ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
+__global__ void __launch_bounds__(NT * 128, NT == 2 && DK == 16 ? 2 : 1)
+ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_constant__ CUtensorMap q_map,
+                  const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     using L = PromptSmem<DK, DVT, NT>;
     constexpr int KS = DK / 16;                   // k-steps of a product over dk
     constexpr int NV = DVT / 8;                   // 8-column tiles of the output
     constexpr int ND = DK / 8;                    // 8-column tiles of the state
     constexpr int WM = DVT / 16;                  // warps of a team that own 16 rows of the state each
-    extern __shared__ __align__(128) uint8_t smem[];
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t gave_up;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < NT * L::kBufs; ++i) mbar_init(smem_u32(smem + L::oBars) + 8 * i, 1);
+        mbar_fence_init();
+    }
     pdl_prologue();
     const uint32_t per_req = a.heads * tiles;
     const uint32_t k = blockIdx.x / per_req, head = (blockIdx.x % per_req) / tiles, tile = blockIdx.x % tiles;
@@ -178,43 +197,39 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
     float *sscale = reinterpret_cast<float *>(smem + L::oScale);
     S += ((unsigned long long)head * a.dv + tile * DVT) * DK;
 
-    // Loads by running pointers: a thread copies the same 16-byte column of rows that are kRowsQ (kRowsV) apart.
-    constexpr int CK = DK / 8, CV = DVT / 8;               // 16-byte units per row
-    constexpr int kRowsQ = 128 / CK, kRowsV = 128 / CV;
+    constexpr int CV = DVT / 8;                            // 16-byte units per row of the output
     const unsigned long long own_row = row0 + (unsigned long long)team * kC;
-    const uint8_t *qg = a.q + (own_row + tid / CK) * a.qs + grp * DK * 2 + tid % CK * 16;
-    const uint8_t *kg = a.k + (own_row + tid / CK) * a.ks + grp * DK * 2 + tid % CK * 16;
-    const uint8_t *vg = a.v + (own_row + tid / CV) * a.vs + ((unsigned long long)head * a.dv + tile * DVT) * 2 + tid % CV * 16;
     const uint8_t *gg = a.g + (own_row + tid % kC) * a.gs + head * 4;
     uint8_t *og = a.out + (own_row + w * 16 + lane / CV) * a.os + ((unsigned long long)head * a.dv + tile * DVT) * 2 + lane % CV * 16;
-    const unsigned long long q_next = (unsigned long long)NT * kC * a.qs, k_next = (unsigned long long)NT * kC * a.ks,
-                             v_next = (unsigned long long)NT * kC * a.vs, g_next = (unsigned long long)NT * kC * a.gs;
-    const uint32_t dq = tid / CK * L::kQ + tid % CK * 16, dvv = L::kStageV + tid / CV * L::kV + tid % CV * 16;
+    const unsigned long long g_next = (unsigned long long)NT * kC * a.gs;
+    const uint32_t bars = smem_u32(smem + L::oBars) + 8 * team * L::kBufs;
 
-    // Piece p of this team (called for p = team, team + NT, ... in turn).
+    // Piece p of this team (called for p = team, team + NT, ... in turn): rows by tiled copies, decays by small ones.  Rows behind
+    // the request's last are the next request's, or zeros behind the last of all: see the last piece.
     auto load = [&](uint32_t p, int buf) {
         if (p < pieces) {
-            const uint32_t base = smem_u32(stage0 + buf * L::kStage), left = len - p * kC;
+            const uint32_t base = smem_u32(stage0 + buf * L::kStage), left = len - p * kC, row = row0 + p * kC;
+            if (tid == 0) {
+                mbar_expect(bars + 8 * buf, kC * (DVT + 2 * DK) * 2);
+                tma_load_tile(base + L::kStageV, &v_map, bars + 8 * buf, head * a.dv + tile * DVT, row);
 #pragma unroll
-            for (int i = 0; i < kC / kRowsQ; ++i) {
-                const bool ok = (uint32_t)(tid / CK + i * kRowsQ) < left;
-                cp_async16(base + L::kStageQ + dq + i * kRowsQ * L::kQ, ok ? qg + i * kRowsQ * a.qs : a.q, ok);
-                cp_async16(base + L::kStageK + dq + i * kRowsQ * L::kQ, ok ? kg + i * kRowsQ * a.ks : a.k, ok);
-            }
-#pragma unroll
-            for (int i = 0; i < kC / kRowsV; ++i) {
-                const bool ok = (uint32_t)(tid / CV + i * kRowsV) < left;
-                cp_async16(base + dvv + i * kRowsV * L::kV, ok ? vg + i * kRowsV * a.vs : a.v, ok);
+                for (int x = 0; x < L::kBlocksK; ++x) {
+                    tma_load_tile(base + L::kStageQ + x * kC * 128, &q_map, bars + 8 * buf, grp * DK + x * 64, row);
+                    tma_load_tile(base + L::kStageK + x * kC * 128, &k_map, bars + 8 * buf, grp * DK + x * 64, row);
+                }
             }
             if (tid < kC) {
                 const bool ok = (uint32_t)tid < left;
                 cp_async4(base + L::kStageG + tid * 4, ok ? gg : a.g, ok);
             }
-            qg += q_next; kg += k_next; vg += v_next; gg += g_next;
+            gg += g_next;
         }
         cp_async_commit();
     };
 
+    auto place_k = [](uint32_t r, uint32_t c) {             // 16-byte unit c of a row of Q or K
+        return DK == 128 ? (c >> 3) * (kC * 128) + unit<128>(r, c & 7) : unit<L::kRowK>(r, c);
+    };
     // Publishes a state fragment as the 16-bit operand of piece p.
     auto publish = [&](const float (&f)[ND][4], uint32_t p) {
         const uint32_t slot = p % L::kRing;
@@ -244,7 +259,8 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         }
     };
 
-    load(team, 0);
+    __syncthreads();
+    for (int i = 0; i < (L::kBufs > 1 ? L::kBufs - 1 : 1); ++i) load(team + i * NT, i);
     if (team == 0 && w < WM) {
         float f[ND][4];
 #pragma unroll
@@ -266,10 +282,26 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
     static_assert(NT >= 2, "the hand-over goes from one team to another");
     constexpr int kTeamBar = 1 + NT;
     int buf = 0;
-    for (uint32_t p = team; p < pieces; p += NT) {
-        if (L::kBufs == 2) { load(p + NT, buf ^ 1); cp_async_wait<1>(); } else cp_async_wait<0>();
+    uint32_t round = 0;
+    for (uint32_t p = team; p < pieces; p += NT, ++round) {
+        if (L::kBufs > 1) load(p + (L::kBufs - 1) * NT, (buf + L::kBufs - 1) % L::kBufs);
+        cp_async_wait<L::kBufs - 1>();
         uint8_t *st = stage0 + buf * L::kStage;
         const uint32_t sq = smem_u32(st + L::kStageQ), sk = smem_u32(st + L::kStageK), sv = smem_u32(st + L::kStageV);
+        // a copy that never lands is reported and not waited for again; the barriers between the teams are still kept
+        if (!mbar_wait(bars + 8 * buf, round / L::kBufs & 1, &gave_up) && tid == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
+        if (len - p * kC < kC) {
+            // behind the request's last row: zeros, as a weight of zero does not silence a NaN
+            constexpr int C = (L::kRowV + 2 * DK * 2) / 16;
+            const uint32_t gone = kC - (len - p * kC);
+            for (uint32_t i = tid; i < gone * C; i += 128) {
+                const uint32_t r = len - p * kC + i / C, c = i % C;
+                // (whole rows are cleared, so the order of their units does not matter)
+                uint8_t *to = c < L::kRowV / 16 ? st + L::kStageV + r * L::kRowV + c * 16
+                                                : st + L::kStageQ + (c - L::kRowV / 16) / (L::kRowK / 16) * (kC * L::kRowK) + r * L::kRowK + (c - L::kRowV / 16) % (L::kRowK / 16) * 16;
+                *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+            }
+        }
         bar_sync(kTeamBar + team, 128);
         if (w == 0) {
             // running sums in units of log2: from the front for the decays, from the back for the tail weights
@@ -299,7 +331,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
         // front c_ref on, times a column factor up to it (both at most 1); inside the own block it is one per pair.
         uint32_t aq[KS][4];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + (w * 16 + (lane & 15)) * L::kQ + s * 32 + (lane >> 4) * 16);
+        for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + place_k(w * 16 + (lane & 15), s * 2 + (lane >> 4)));
         const float c0 = cs[w * 16 + lr], c1 = cs[w * 16 + lr + 8], cref = w ? cs[w * 16 - 1] : 0.f;
         auto score = [&](int j, float (&x)[2][4]) {
 #pragma unroll
@@ -307,7 +339,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 uint32_t b[4];
-                ldsm4(b, sk + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
+                ldsm4(b, sk + place_k(j * 16 + (lane & 7) + ((lane >> 4) << 3), s * 2 + ((lane >> 3) & 1)));
                 T::mma(x[0], aq[s], b[0], b[1]);
                 T::mma(x[1], aq[s], b[2], b[3]);
             }
@@ -316,7 +348,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
             for (int n = 0; n < NV / 2; ++n) {
                 uint32_t b[4];
-                ldsm4_t(b, sv + (j * 16 + (lane & 15)) * L::kV + n * 32 + (lane >> 4) * 16);
+                ldsm4_t(b, sv + unit<L::kRowV>(j * 16 + (lane & 15), n * 2 + (lane >> 4)));
                 T::mma(o[2 * n], pa, b[0], b[1]);
                 T::mma(o[2 * n + 1], pa, b[2], b[3]);
             }
@@ -388,7 +420,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t v[4];
-                    ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
+                    ldsm4_t(v, sv + unit<L::kRowV>(j * 16 + (lane & 7) + ((lane >> 4) << 3), w * 2 + ((lane >> 3) & 1)));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float2 x = T::unpack(v[i]), y = *reinterpret_cast<const float2 *>(wt + j * 16 + (i >> 1) * 8 + lc);
@@ -411,7 +443,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t v[4], x3[3][4];
-                ldsm4_t(v, sv + (j * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kV + w * 32 + ((lane >> 3) & 1) * 16);
+                ldsm4_t(v, sv + unit<L::kRowV>(j * 16 + (lane & 7) + ((lane >> 4) << 3), w * 2 + ((lane >> 3) & 1)));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float2 x = T::unpack(v[i]);
@@ -427,7 +459,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
 #pragma unroll
                 for (int n = 0; n < ND / 2; ++n) {
                     uint32_t b[4];
-                    ldsm4_t(b, sk + (j * 16 + (lane & 15)) * L::kQ + n * 32 + (lane >> 4) * 16);
+                    ldsm4_t(b, sk + place_k(j * 16 + (lane & 15), n * 2 + (lane >> 4)));
 #pragma unroll
                     for (int y = 0; y < (T::kF16 ? 2 : 3); ++y) {
                         T::mma(part[y % kSums][2 * n], x3[y], b[0], b[1]);
@@ -507,11 +539,16 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles)
                 *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
         }
         og += (unsigned long long)NT * kC * a.os;
-        if (L::kBufs == 2) buf ^= 1;
+        buf = (buf + 1) % L::kBufs;
         bar_sync(kTeamBar + team, 128);             // the stage may be filled again, cs and wt rewritten
         if (L::kBufs == 1) load(p + NT, 0);
     }
     cp_async_wait<0>();
+    if (*(volatile uint32_t *)&gave_up) {
+        // copies in flight land, or have their time, before this CTA's memory is given away
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 1000000ull) {}
+    }
 }
 
 template <class T, int DK>
@@ -533,13 +570,22 @@ cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
     const cudaError_t e = allow_smem<ssm_prompt_kernel<T, DK, DVT, NT>>(l.device, L::kTotal);
     if (e != cudaSuccess) return e;
     const uint32_t tiles = a.dv / DVT;
-    return launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles);
+    CUtensorMap q = {}, k = {}, v = {};
+    if (a.total && !(rows_map(&q, a.q, a.groups * DK, a.total, a.qs, DK < 64 ? DK : 64, kC) &&
+                     rows_map(&k, a.k, a.groups * DK, a.total, a.ks, DK < 64 ? DK : 64, kC) &&
+                     rows_map(&v, a.v, a.heads * a.dv, a.total, a.vs, DVT, kC)))
+        return cudaErrorNotSupported;
+    return launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles, q, k, v);
 }
 template <class T, int DVT>
 cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l)
 {
+    // Short keys: two CTAs of two teams on an SM overlap their beginnings and ends (32 prompts of 272 tokens: 36 against 45 us;
+    // 16 of 2048: 394 against 423), one of four teams walks a long prompt faster (65 521 tokens: 823 against 1697).  Only
+    // the mean length is known here.
+    const bool small = a.total / a.n < 1024u && (unsigned long long)a.n * a.heads * (a.dv / DVT) >= 2ull * l.n_sms;
     switch (a.dk) {
-    case 16: return prompt_launch<T, 16, DVT, 4>(g, a, l);
+    case 16: return small ? prompt_launch<T, 16, DVT, 2>(g, a, l) : prompt_launch<T, 16, DVT, 4>(g, a, l);
     case 32: return prompt_launch<T, 32, DVT, 3>(g, a, l);
     case 64: return prompt_launch<T, 64, DVT, 2>(g, a, l);
     default: return prompt_launch<T, 128, DVT, 2>(g, a, l);

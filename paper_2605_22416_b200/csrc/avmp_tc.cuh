@@ -225,6 +225,13 @@ __device__ __forceinline__ void tma_load_query(uint32_t dst, const CUtensorMap *
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(head), "r"(token) : "memory");
 }
+// Packed rows of 16-bit numbers, boxes of `rows` x `columns` (16, 32 or 64) with the swizzle of that width; rows behind the last are zeros.
+bool rows_map(CUtensorMap *map, const void *p, uint32_t row_elems, uint32_t n_rows, unsigned long long stride, uint32_t columns, uint32_t rows);
+__device__ __forceinline__ void tma_load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int row)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(row) : "memory");
+}
 __device__ __forceinline__ void tma_prefetch_rows(const CUtensorMap *map, int group, int row)
 {
     asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global.tile [%0, {%3, %3, %3, %1, %2}];" :: "l"(map), "r"(group), "r"(row), "r"(0) : "memory");
