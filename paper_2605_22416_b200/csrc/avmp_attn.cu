@@ -124,23 +124,6 @@ __global__ void __launch_bounds__(kStepThreads) attn_plan_kernel(const Geom g, c
     make_plan(g, d, d.ws, tmp, true);
 }
 
-// Four 8-column tiles of an accumulator row, two columns a lane: afterwards the lane holds the eight columns of tile `lane & 3`
-// (a 4 x 4 transpose inside the quad), so that rows are stored in 16-byte units.
-__device__ __forceinline__ void quad_transpose(uint32_t (&a)[4])
-{
-    const bool o1 = threadIdx.x & 1, o2 = threadIdx.x & 2;
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o1 ? a[i] : a[i + 1], 1);
-        if (o1) a[i] = y; else a[i + 1] = y;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o2 ? a[i] : a[i + 2], 2);
-        if (o2) a[i] = y; else a[i + 2] = y;
-    }
-}
-
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUtensorMap map)
@@ -385,7 +368,7 @@ drain:
                         uint32_t v[4];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) v[x] = T::pack(o[i + x][2 * r] * (r ? i1 : i0), o[i + x][2 * r + 1] * (r ? i1 : i0));
-                        quad_transpose(v);
+                        quad_transpose(v);      // the lane then holds the eight columns of tile `lane & 3`: rows go out in 16-byte units
                         if (r ? row1 : row0)
                             *reinterpret_cast<uint4 *>(out + ((unsigned long long)(r ? qh1 : qh0) * D + (i + (lane & 3)) * 8) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
                     }

@@ -548,26 +548,40 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
             if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top, sum);
             if (d.j0 < d.j1) {
                 const float inv = 1.f / sum;
-                uint8_t *out = p.a.out + (unsigned long long)(d.q0 + token) * p.a.os + (unsigned long long)qh * D * 2;
+                // A thread holds a row, and a store of 32 rows costs a cycle each (4000 a tile).  Quads of lanes swap 16-byte units
+                // first: a store then covers 64 bytes of 8 rows.
+                const bool whole = !PREFIX && p.splits == 1;
+                const unsigned long long mine_at = !mine ? 0ull : whole
+                    ? reinterpret_cast<unsigned long long>(p.a.out + (unsigned long long)(d.q0 + token) * p.a.os + (unsigned long long)qh * D * 2)
+                    : reinterpret_cast<unsigned long long>(p.parts.o + at * D);
+                uint8_t *rows[4];                      // of the quad's four lanes, at this lane's unit; null: no such row
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const unsigned long long x = __shfl_sync(0xFFFFFFFFu, mine_at, (lane & ~3) + r);
+                    rows[r] = x ? reinterpret_cast<uint8_t *>(x) + (lane & 3) * 16 : nullptr;
+                }
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld32(o, to + c);
                     tmem_wait_ld();
-                    if (mine && (PREFIX || p.splits > 1)) {
+                    if (whole) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4 *>(p.parts.o + at * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                    } else if (mine) {
+                        for (int e = 0; e < 32; e += 2) o[e / 2] = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                    }
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint4 v;
-                            v.x = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                            v.y = T::pack(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                            v.z = T::pack(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                            v.w = T::pack(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                            *reinterpret_cast<uint4 *>(out + (c + e) * 2) = v;
+                    for (int h = 0; h < 2; ++h) {
+                        if (whole && h) break;
+                        uint32_t v[4][4];              // [word][row]
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) v[k][x] = o[h * 16 + x * 4 + k];
+                            quad_transpose(v[k]);
                         }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (rows[r]) *reinterpret_cast<uint4 *>(rows[r] + (whole ? c * 2 : (c + h * 16) * 4)) = make_uint4(v[0][r], v[1][r], v[2][r], v[3][r]);
                     }
                     __syncwarp();
                 }

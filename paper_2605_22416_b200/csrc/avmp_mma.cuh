@@ -72,6 +72,22 @@ __device__ __forceinline__ float exp2_approx(float x)
     return y;
 }
 
+// 4 x 4 transpose inside each quad of lanes: afterwards a[i] is what lane i of the quad held as a[lane & 3].
+__device__ __forceinline__ void quad_transpose(uint32_t (&a)[4])
+{
+    const bool o1 = threadIdx.x & 1, o2 = threadIdx.x & 2;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o1 ? a[i] : a[i + 1], 1);
+        if (o1) a[i] = y; else a[i + 1] = y;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, o2 ? a[i] : a[i + 2], 2);
+        if (o2) a[i] = y; else a[i + 2] = y;
+    }
+}
+
 // Named barriers: `n` threads in all; an arrival does not wait.
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "r"(n) : "memory"); }
