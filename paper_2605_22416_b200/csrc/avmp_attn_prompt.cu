@@ -100,8 +100,12 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
     w.tok0 = w.row0 / p.group; w.rem0 = w.row0 - w.tok0 * p.group;
     w.len = causal ? past + (w.row0 + w.rows - 1) / p.group + 1 : held;
     const uint32_t rounds = (w.len + kKv - 1) / kKv;
-    w.j0 = (uint32_t)((unsigned long long)rounds * split / p.splits);
-    w.j1 = (uint32_t)((unsigned long long)rounds * (split + 1) / p.splits);
+    w.j0 = 0; w.j1 = rounds;
+    if (p.splits > 1) {      // shares of whole rounds: the first `rest` get one more
+        const uint32_t each = rounds / p.splits, rest = rounds - each * p.splits;
+        w.j0 = split * each + min(split, rest);
+        w.j1 = w.j0 + each + (split < rest ? 1u : 0u);
+    }
     return w;
 }
 
@@ -136,7 +140,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
             held = held_tokens(g, req);
             if (held && q1 >= q0 && q1 <= p.a.total_q && q1 - q0 <= held) {
                 nq = q1 - q0;
-                blocks = (uint32_t)(((unsigned long long)nq * p.group + kRows - 1) / kRows);
+                blocks = (nq * p.group + kRows - 1) / kRows;      // total_q * q_heads < 2^31
                 if (nq) top = (held + kKv - 1) / kKv;
             } else if (blockIdx.x == 0) {
                 record_error(g.st, AVMP_DEV_BAD_REQUEST);
@@ -147,22 +151,28 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
         auto first = [&](uint32_t R) {
             const uint32_t x = (R - 1) * kKv;            // its last token stands at position x or later
             if (x <= past) return 0u;
-            return x - past >= nq ? blocks : min(blocks, (uint32_t)((unsigned long long)(x - past) * p.group / kRows));
+            return x - past >= nq ? blocks : min(blocks, (x - past) * p.group / kRows);
         };
-        for (uint32_t n = 0, i; (i = nth_tile(n)) < all * per; ++n) {
-            const uint32_t e = i / per;
+        for (uint32_t n = 0, i; (i = nth_tile(n)) < all * p.a.kv_heads; ++n) {
+            const uint32_t e = i / p.a.kv_heads;
             uint32_t lo = 1, hi = most + 1;              // count(lo) > e >= count(hi)
             while (lo + 1 < hi) {
                 const uint32_t mid = (lo + hi) >> 1;
                 if (__reduce_add_sync(0xFFFFFFFFu, blocks - first(mid)) > e) lo = mid; else hi = mid;
             }
             const uint32_t f0 = first(lo), f1 = first(lo + 1), mine = f1 - f0;      // blocks with exactly lo rounds
-            const uint32_t incl = (uint32_t)warp_incl_scan(mine), at = e - __reduce_add_sync(0xFFFFFFFFu, blocks - f1);
+            uint32_t incl = mine;
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, incl, x);
+                if (lane >= x) incl += y;
+            }
+            const uint32_t at = e - __reduce_add_sync(0xFFFFFFFFu, blocks - f1);
             const uint32_t owner = __ffs(__ballot_sync(0xFFFFFFFFu, incl > at)) - 1;
             const uint32_t block = __shfl_sync(0xFFFFFFFFu, f0 + at - (incl - mine), owner);
             if (!give(make_work(p, owner, __shfl_sync(0xFFFFFFFFu, req, owner), __shfl_sync(0xFFFFFFFFu, held, owner),
                                 __shfl_sync(0xFFFFFFFFu, past, owner), __shfl_sync(0xFFFFFFFFu, q0, owner),
-                                __shfl_sync(0xFFFFFFFFu, nq, owner) * p.group, block, i % per / p.splits, i % p.splits, true))) return;
+                                __shfl_sync(0xFFFFFFFFu, nq, owner) * p.group, block, i - e * p.a.kv_heads, 0, true))) return;
         }
     }
     give(w);
@@ -223,7 +233,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     }
 
     if (w >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         if (w == 8 || w == 10) {
             // ---------------- loads: K by one warp, V by another.  The lanes look the pages up a round ahead; one thread issues.
             const uint32_t v = w == 8 ? 0 : 1, page_rows = (uint32_t)(g.U[0] / (D * 2));
@@ -391,7 +401,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
             });
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ---------------- softmax: warpgroup m, one row per thread
         const uint32_t m = w >> 2, tid = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(w & 3) << 21;                 // this warp's quarter of the lanes
