@@ -129,13 +129,13 @@ struct PromptSmem {
     static constexpr int kS = DVT * kQ;
     static constexpr int kO = kC * kV;            // output staging
     static constexpr int kF = DVT * DK * 4;       // the state in 32 bits, thread-private places
-    static constexpr int kW = kC * 2 * 4;         // running decays and tail weights
+    static constexpr int kW = kC * 2 * 4;         // running decays and tail weights, of this piece and the team's next
     static constexpr int oStage = 0;
     static constexpr int oS = oStage + NT * kBufs * kStage;
     static constexpr int oO = oS + kRing * kS;
     static constexpr int oF = oO + NT * kO;
     static constexpr int oW = oF + kF;
-    static constexpr int oScale = oW + NT * kW;
+    static constexpr int oScale = oW + NT * 2 * kW;
     static constexpr int oBars = oScale + kRing * 4 * 4;
     static constexpr int kTotal = oBars + NT * kBufs * 8 + 1024;
 };
@@ -193,13 +193,13 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
     const int lr = lane >> 2, lc = (lane & 3) * 2;
     uint8_t *stage0 = smem + L::oStage + team * L::kBufs * L::kStage;
     float *F = reinterpret_cast<float *>(smem + L::oF);
-    float *cs = reinterpret_cast<float *>(smem + L::oW + team * L::kW), *wt = cs + kC;
+    float *decays = reinterpret_cast<float *>(smem + L::oW + team * 2 * L::kW);
     float *sscale = reinterpret_cast<float *>(smem + L::oScale);
     S += ((unsigned long long)head * a.dv + tile * DVT) * DK;
 
     constexpr int CV = DVT / 8;                            // 16-byte units per row of the output
     const unsigned long long own_row = row0 + (unsigned long long)team * kC;
-    const uint8_t *gg = a.g + (own_row + tid % kC) * a.gs + head * 4;
+    const uint8_t *gg = a.g + (own_row + 2 * lane) * a.gs + head * 4;       // two decays a lane of the first warp
     uint8_t *og = a.out + (own_row + w * 16 + lane / CV) * a.os + ((unsigned long long)head * a.dv + tile * DVT) * 2 + lane % CV * 16;
     const unsigned long long g_next = (unsigned long long)NT * kC * a.gs;
     const uint32_t bars = smem_u32(smem + L::oBars) + 8 * team * L::kBufs;
@@ -218,10 +218,12 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
                     tma_load_tile(base + L::kStageK + x * kC * 128, &k_map, bars + 8 * buf, grp * DK + x * 64, row);
                 }
             }
-            if (tid < kC) {
-                const bool ok = (uint32_t)tid < left;
-                cp_async4(base + L::kStageG + tid * 4, ok ? gg : a.g, ok);
-            }
+            if (w == 0)
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const bool ok = 2 * lane + i < left;
+                    cp_async4(base + L::kStageG + (2 * lane + i) * 4, ok ? gg + i * a.gs : a.g, ok);
+                }
             gg += g_next;
         }
         cp_async_commit();
@@ -229,6 +231,28 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
 
     auto place_k = [](uint32_t r, uint32_t c) {             // 16-byte unit c of a row of Q or K
         return DK == 128 ? (c >> 3) * (kC * 128) + unit<128>(r, c & 7) : unit<L::kRowK>(r, c);
+    };
+    // First warp: running sums in units of log2, from the front for the decays, from the back for the tail weights (the weights
+    // of the state keep their relative precision that way).
+    auto scan = [&](const float *gs, float *cs) {
+        float *wt = cs + kC;
+        constexpr float kLog2e = 1.4426950408889634f;
+        float g0 = gs[2 * lane] * kLog2e, g1 = gs[2 * lane + 1] * kLog2e;
+        // 2^-300 is 0 in 32 bits; -inf itself would make differences of sums undefined
+        g0 = g0 < -300.f ? -300.f : g0; g1 = g1 < -300.f ? -300.f : g1;
+        float f = g0 + g1, b = f;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const float x = __shfl_up_sync(0xFFFFFFFFu, f, o), y = __shfl_down_sync(0xFFFFFFFFu, b, o);
+            if (lane >= o) f += x;
+            if (lane + o < 32) b += y;
+        }
+        float b_next = __shfl_down_sync(0xFFFFFFFFu, b, 1);
+        if (lane == 31) b_next = 0.f;
+        float f_prev = __shfl_up_sync(0xFFFFFFFFu, f, 1);
+        if (lane == 0) f_prev = 0.f;
+        cs[2 * lane] = f_prev + g0; cs[2 * lane + 1] = f;
+        wt[2 * lane] = exp2_approx(b_next + g1); wt[2 * lane + 1] = exp2_approx(b_next);
     };
     // Publishes a state fragment as the 16-bit operand of piece p.
     auto publish = [&](const float (&f)[ND][4], uint32_t p) {
@@ -277,6 +301,11 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
         publish(f, 0);
         if (pieces == 0 && !resume) store_state(f);
     }
+    if (L::kBufs > 1 && w == 0) {          // the first piece's decays; later ones are worked out a piece ahead
+        cp_async_wait<0>();
+        __syncwarp();
+        scan(reinterpret_cast<const float *>(stage0 + L::kStageG), decays);
+    }
     __syncthreads();
 
     static_assert(NT >= 2, "the hand-over goes from one team to another");
@@ -285,7 +314,6 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
     uint32_t round = 0;
     for (uint32_t p = team; p < pieces; p += NT, ++round) {
         if (L::kBufs > 1) load(p + (L::kBufs - 1) * NT, (buf + L::kBufs - 1) % L::kBufs);
-        cp_async_wait<L::kBufs - 1>();
         uint8_t *st = stage0 + buf * L::kStage;
         const uint32_t sq = smem_u32(st + L::kStageQ), sk = smem_u32(st + L::kStageK), sv = smem_u32(st + L::kStageV);
         // a copy that never lands is reported and not waited for again; the barriers between the teams are still kept
@@ -302,30 +330,13 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
                 *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
             }
         }
-        bar_sync(kTeamBar + team, 128);
-        if (w == 0) {
-            // running sums in units of log2: from the front for the decays, from the back for the tail weights
-            // (the weights of the state keep their relative precision that way)
-            const float *gs = reinterpret_cast<const float *>(st + L::kStageG);
-            constexpr float kLog2e = 1.4426950408889634f;
-            float g0 = gs[2 * lane] * kLog2e, g1 = gs[2 * lane + 1] * kLog2e;
-            // 2^-300 is 0 in 32 bits; -inf itself would make differences of sums undefined
-            g0 = g0 < -300.f ? -300.f : g0; g1 = g1 < -300.f ? -300.f : g1;
-            float f = g0 + g1, b = f;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const float x = __shfl_up_sync(0xFFFFFFFFu, f, o), y = __shfl_down_sync(0xFFFFFFFFu, b, o);
-                if (lane >= o) f += x;
-                if (lane + o < 32) b += y;
-            }
-            float b_next = __shfl_down_sync(0xFFFFFFFFu, b, 1);
-            if (lane == 31) b_next = 0.f;
-            float f_prev = __shfl_up_sync(0xFFFFFFFFu, f, 1);
-            if (lane == 0) f_prev = 0.f;
-            cs[2 * lane] = f_prev + g0; cs[2 * lane + 1] = f;
-            wt[2 * lane] = exp2_approx(b_next + g1); wt[2 * lane + 1] = exp2_approx(b_next);
+        float *cs = decays + (L::kBufs > 1 ? (round & 1) * 2 * kC : 0), *wt = cs + kC;
+        if (L::kBufs == 1 && w == 0) {
+            cp_async_wait<0>();
+            __syncwarp();
+            scan(reinterpret_cast<const float *>(st + L::kStageG), cs);
         }
-        bar_sync(kTeamBar + team, 128);
+        if (L::kBufs == 1 || len - p * kC < kC) bar_sync(kTeamBar + team, 128);
 
         // ---- scores of this warp's 16 rows.  Against earlier blocks of 16 tokens the decay is a row factor, from the block's
         // front c_ref on, times a column factor up to it (both at most 1); inside the own block it is one per pair.
@@ -477,6 +488,12 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
                 }
         }
 
+        if (L::kBufs > 1 && w == 0 && p + NT < pieces) {      // the team's next piece, while the other warps have more rows to see
+            cp_async_wait<0>();
+            __syncwarp();
+            scan(reinterpret_cast<const float *>(stage0 + (buf ^ 1) * L::kStage + L::kStageG), decays + ((round + 1) & 1) * 2 * kC);
+        }
+
         // ---- hand-over: wait for the state in front of this piece, pass the one behind it on at once
         if (p > 0) bar_sync(1 + team, 256);
         if (w < WM) {
@@ -540,7 +557,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
         }
         og += (unsigned long long)NT * kC * a.os;
         buf = (buf + 1) % L::kBufs;
-        bar_sync(kTeamBar + team, 128);             // the stage may be filled again, cs and wt rewritten
+        bar_sync(kTeamBar + team, 128);             // the stage may be filled again, the next decays are there
         if (L::kBufs == 1) load(p + NT, 0);
     }
     cp_async_wait<0>();
