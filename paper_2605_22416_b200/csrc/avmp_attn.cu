@@ -104,7 +104,7 @@ __device__ __forceinline__ void make_plan(const Geom &g, const DecodeArgs &d, co
     const uint32_t per = (n + blockDim.x - 1) / blockDim.x, k0 = min(n, threadIdx.x * per), k1 = min(n, k0 + per);
     unsigned long long mine = 0, tot;
     for (uint32_t k = k0; k < k1; ++k) {
-        const uint32_t r = d.a.reqs[k], own = held_tokens(g, r), len = dead ? 0u : own;
+        const uint32_t r = __ldcg(d.a.reqs + k), own = held_tokens(g, r), len = dead ? 0u : own;
         if (lead && len == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
         to.req[k] = r; to.len[k] = len;
         mine += (len + step - 1) / step;
@@ -185,8 +185,8 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
                 while (p.cu[kk + 1] <= st) ++kk;
                 const uint32_t t = (st - p.cu[kk]) * step_tokens + (lane % per_step) * s.box_tokens;
                 if (t < p.len[kk]) {
-                    const uint32_t h = g.r_chain[(unsigned long long)p.req[kk] * g.max_pages + t / g.T];
-                    slot = g.VT[0][h & 0x7FFFFFFFu];
+                    const uint32_t h = __ldcg(g.r_chain + ((unsigned long long)p.req[kk] * g.max_pages + t / g.T));
+                    slot = __ldcg(g.VT[0] + (h & 0x7FFFFFFFu));
                     tok = t % g.T;
                 }
             }
@@ -245,10 +245,10 @@ drain:
             const uint8_t *q0 = d.a.q + k * d.a.qs + (unsigned long long)qh0 * D * 2, *q1 = d.a.q + k * d.a.qs + (unsigned long long)qh1 * D * 2;
 #pragma unroll
             for (int x = 0; x < KS; ++x) {
-                q[x][0] = row0 ? *reinterpret_cast<const uint32_t *>(q0 + (x * 16 + lc) * 2) : 0u;
-                q[x][1] = row1 ? *reinterpret_cast<const uint32_t *>(q1 + (x * 16 + lc) * 2) : 0u;
-                q[x][2] = row0 ? *reinterpret_cast<const uint32_t *>(q0 + (x * 16 + 8 + lc) * 2) : 0u;
-                q[x][3] = row1 ? *reinterpret_cast<const uint32_t *>(q1 + (x * 16 + 8 + lc) * 2) : 0u;
+                q[x][0] = row0 ? __ldcg(reinterpret_cast<const uint32_t *>(q0 + (x * 16 + lc) * 2)) : 0u;
+                q[x][1] = row1 ? __ldcg(reinterpret_cast<const uint32_t *>(q1 + (x * 16 + lc) * 2)) : 0u;
+                q[x][2] = row0 ? __ldcg(reinterpret_cast<const uint32_t *>(q0 + (x * 16 + 8 + lc) * 2)) : 0u;
+                q[x][3] = row1 ? __ldcg(reinterpret_cast<const uint32_t *>(q1 + (x * 16 + 8 + lc) * 2)) : 0u;
             }
         }
         float o[ND][4];
@@ -259,7 +259,9 @@ drain:
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         for (uint32_t c = st; c < seg_end; ++c, ++it) {
             const uint32_t stage = it % s.stages;
-            if (!mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, &gave_up)) return;      // (the loading warp still waits for the pass in front)
+            // A copy that never lands is reported by the loading warp and not waited for again: the warps of this CTA keep their
+            // barriers with each other, and the results are not to be used.
+            mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, &gave_up);
             const uint32_t base = ring + stage * s.stage_bytes;
             const uint32_t t0 = (c - begin) * step_tokens + share * 16;
             if (works && t0 < len) {

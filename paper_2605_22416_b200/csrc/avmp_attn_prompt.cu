@@ -655,7 +655,7 @@ uint32_t box_of(uint32_t T)
     return b;
 }
 
-// Rows of partial sums that a call may leave: splitting stops where the SMs are busy.
+// Rows of partial sums that a call may leave.  Splits x row blocks x KV heads never pass the SMs, and a row block has 256 rows.
 size_t part_rows(size_t rows, int n_sms) { const size_t full = (size_t)n_sms * kRows; return rows > full ? rows : full; }
 
 template <class T, int D, bool PREFIX>
@@ -724,8 +724,9 @@ cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l
     p.group = a.q_heads / a.kv_heads;
     p.box_tokens = box_of(g.T);
     const unsigned long long full = (unsigned long long)a.n * (((unsigned long long)g.max_pages * g.T * p.group + kRows - 1) / kRows);
-    p.cap = (uint32_t)min(full, (unsigned long long)a.total_q * p.group / kRows + a.n);
-    p.splits = split_of((unsigned long long)p.cap * a.kv_heads, l.n_sms);
+    const unsigned long long most = (unsigned long long)a.total_q * p.group / kRows + a.n;      // row blocks of the buffers' rows
+    p.cap = (uint32_t)min(full, most);
+    p.splits = split_of(most * a.kv_heads, l.n_sms);           // (parts lie by row of the buffers: see part_rows)
     uint8_t *w = a.ws;
     p.n_tiles = reinterpret_cast<uint32_t *>(w); w += 256;
     p.tiles = reinterpret_cast<Tile *>(w); w += up256((size_t)full * sizeof(Tile));

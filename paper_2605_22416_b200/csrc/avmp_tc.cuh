@@ -242,10 +242,11 @@ __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *m
                  :: "r"(dst), "l"(map), "r"(bar), "r"(group), "r"(row), "r"(0) : "memory");
 }
 
-// Tokens that a slot's chain holds; 0 for a slot that is empty or out of range.  Both tables are read at once.
+// Tokens that a slot's chain holds; 0 for a slot that is empty or out of range.  Both tables are read at once, and past the
+// L1 cache (a kernel that starts without waiting has nothing else to tell it that its lines are new).
 __device__ __forceinline__ uint32_t held_tokens(const Geom &g, uint32_t r)
 {
-    const uint32_t i = r < g.R ? r : 0u, state = g.r_state[i], len = g.r_len[i];
+    const uint32_t i = r < g.R ? r : 0u, state = __ldcg(g.r_state + i), len = __ldcg(g.r_len + i);
     return r < g.R && state != AVMP_REQ_EMPTY ? len : 0u;
 }
 

@@ -278,6 +278,27 @@ def test_prompt_of_many_requests():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("total", [6, 700, 9000])
+def test_buffers_larger_than_the_rows_in_them(total):
+    """A padded batch: far more rows in the buffers than the requests can hold tokens, at widths where the tokens are split
+    over the SMs and where they are not; nothing outside the workspace is written."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    c = Cache([300, 6], 1, 64, 16, "bfloat16", seed=12)
+    desc = B.attn_desc(q_heads=4, dtype=c.dt, scale=0.125)
+    size = c.ctx.attn_workspace_bytes(desc, 2)
+    ws = torch.full((size + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    q, _ = c.queries(total, 4)
+    out, lse = torch.full((total, 4, 64), 7.0, dtype=c.dt, device="cuda"), torch.full((total, 4), 7.0, device="cuda")
+    c.ctx.attn_prompt(c.layer, desc, _i32([0, 1]), 2, _i32([0, 2, 6]), total, q, out, lse, ws, size)
+    for r, a, b in ((0, 0, 2), (1, 2, 6)):
+        want, want_lse = _exact(q[a:b], c.rows[r], 0.125, [300, 6][r] - (b - a))
+        _check(out[a:b], lse[a:b], want, want_lse, f"slot {r}")
+    assert (out[6:] == 7).all() and (lse[6:] == 7).all() and (ws[size:] == 0x5A).all()
+    c.ctx.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("lists", ["short", "long"])
 def test_bad_items_are_skipped(lists):
     import torch
