@@ -130,6 +130,43 @@ def test_single_tokens(dtype, heads, groups, dk, dv):
     ctx.close()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("n,heads,groups,dk,dv", [(120, 128, 8, 16, 128), (67, 37, 1, 128, 96), (330, 20, 4, 64, 64)])
+def test_single_tokens_of_large_states(dtype, n, heads, groups, dk, dv):
+    """Batches of many CTAs per request, with ends of blocks inside a CTA's part and skipped entries in the list; twice."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt = getattr(torch, dtype)
+    m = _model(heads, dk, dv, layers=1, conv=20)
+    slots = n + 5
+    ctx = _ctx(m, slots, list(range(n)))
+    gen = torch.Generator("cuda").manual_seed(n)
+    order = np.random.default_rng(n).permutation(n)
+    reqs = list(order[: n - 3]) + [order[0], n + 2, 0xFFFFFFFF]           # named before, empty, out of range
+    first, conv = _fill_state(ctx, 0, order, m, gen)
+    q, k = ((torch.randn(n, groups, dk, device="cuda", generator=gen) * 0.2).to(dt) for _ in range(2))
+    v = (torch.randn(n, heads, dv, device="cuda", generator=gen)).to(dt)
+    g = -torch.rand(n, heads, device="cuda", generator=gen)
+    g[5, 0] = -math.inf
+    out = torch.full((n, heads, dv), 7.0, dtype=dt, device="cuda")
+    desc = B.ssm_desc(heads=heads, groups=groups, dk=dk, dv=dv, dtype=dt)
+    for step in range(2):
+        ctx.ssm_step(0, desc, _i32(reqs), n, q, k, v, g, out)
+        assert ctx.stats()["error_count"] == 3 * (step + 1)
+    st, cv = _states(ctx, 0, order, m)
+    S = first.view(n, heads, dv, dk)[: n - 3].double()
+    rep = heads // groups
+    kk, qq = (x[: n - 3].double().repeat_interleave(rep, 1)[:, :, None, :] for x in (k, q))
+    w = g[: n - 3].double().exp()[:, :, None, None]
+    for _ in range(2):
+        S = torch.where(w == 0, torch.zeros_like(S), S * w) + v[: n - 3].double()[..., None] * kk
+    _check(st.view(n, heads, dv, dk)[: n - 3], S, 2.0 ** -20, "states")
+    _check(out[: n - 3], (S * qq).sum(-1), torch.finfo(dt).eps / 2, "out")
+    assert torch.equal(st[n - 3:], first[n - 3:]) and (out[n - 3:] == 7).all() and torch.equal(cv, conv)
+    ctx.close()
+
+
 PROMPTS = [
     # heads, groups, dk, dv, lengths, resume
     (1, 1, 16, 32, [1], [0]),
