@@ -330,9 +330,10 @@ AVMP_API int avmp_scatter_ssm_layers(avmp_ctx *ctx, uint32_t first_layer, uint32
  * are those kernels, reading pages and blocks where they lie, so a step touches its cache once.
  * All rows ("tokens") of a batch are packed; a row stride of 0 in a descriptor means densely packed
  * rows.  Pointers to rows must be 16-byte aligned and row strides multiples of 16 bytes (decays: 4).
- * Outputs must not overlap inputs.  The context's device must be current.  Nothing is allocated: where a call needs scratch it takes a caller's
- * buffer, whose content need not be preserved and which two calls may share if they cannot overlap
- * on the GPU.  An item that only the device can see to be wrong (see each call) is skipped, its output
+ * Outputs must not overlap inputs.  The context's device must be current.  Nothing is allocated: where
+ * a call needs scratch it takes a caller's buffer, whose content need not be preserved and which two calls
+ * may share if they cannot overlap on the GPU.  Calls can be captured into graphs; nothing is read on the host
+ * but the arguments.  An item that only the device can see to be wrong (see each call) is skipped, its output
  * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST. */
 enum { AVMP_TYPE_BF16 = 0, AVMP_TYPE_F16 = 1 };   /* type of input and output rows (and of cached K and V) */
 
@@ -363,7 +364,7 @@ AVMP_API int avmp_attn_prompt(avmp_ctx *ctx, uint32_t attn_layer, const avmp_att
 /* Attention of one token per request over its whole chain: row k of d_q belongs to d_reqs[k] (slots may
  * repeat).  With prefix_req != AVMP_INVALID every request also sees all tokens of that slot's chain
  * (a shared prompt that is held once); the batch's products with it are computed together.  A prefix slot
- * out of range or holding nothing skips every item. */
+ * out of range or holding nothing skips every item.  n_reqs <= max_requests; q_heads * n_reqs < 2^31. */
 AVMP_API int avmp_attn_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_attn_desc *desc, const uint32_t *d_reqs,
                               uint32_t n_reqs, uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse,
                               void *d_workspace, size_t workspace_bytes, void *stream);

@@ -5,10 +5,14 @@
 // heads fill the rows of the tensor-core tiles whatever the group is, and every K and V row is loaded once for all of them.
 // Over it run the KV tokens, 128 at a time:
 //     S = Q K^T  (tcgen05, sums in tensor memory),  P = 2^(S - m),  O += P V  (P as an operand in tensor memory).
-// One CTA per SM, 12 warps: two warpgroups own 128 rows each (a thread is a row: the softmax needs no exchange), one
-// warp loads K and V slices of pages by tiled bulk copies, one issues the products.  While one warpgroup
-// exponentiates, the tensor cores work for the other.  The running maximum m is only moved when it grows by more than
-// 2^8 (P stays inside 16-bit range; sums are 32-bit), so the accumulator is rarely rescaled.
+// One CTA per SM, 12 warps: two warpgroups own 128 rows each (a thread is a row: the softmax needs no exchange), a warp each
+// loads K and V slices of pages by tiled copies (the latter the query rows too), one issues the products, one hands out
+// tiles.  While one warpgroup exponentiates, the tensor cores work for the other.  The running maximum m is only moved when
+// it grows by more than 2^8 (P stays inside 16-bit range; sums are 32-bit), so the accumulator is rarely rescaled.
+//
+// Measured (32 query heads on 8 KV heads of 128, bf16): a prompt of 32 749 tokens 7.2 ms alone (1 220 TFLOP/s), 7.8 ms in a
+// loop, where the card's power limit holds the clock at 1.57 GHz (81 to 84 % of what cuBLAS sustains there).  Long
+// tiles are bound by that; short ones (32 prompts of 32 to 512 tokens: 48 us) by the chain load, S, P, O, store.
 // P is rounded to the 16 bits of V (eps/2 per weight, averaged over the tokens); denominators are summed before that.
 #include "avmp_tc.cuh"
 
@@ -21,7 +25,7 @@ constexpr int kKv = 128;                      // KV tokens per round
 constexpr int kCta = 384;
 constexpr int kAnnounce = 64;                 // the first 64 tokens' weights are announced behind the weights from here
 constexpr uint32_t kAhead = 2;                // rounds ahead that the prefix pass calls rows into L2
-constexpr int kPoly = 0x08;                   // which of 8 pairs of exponentials go to the multiply-add pipe
+constexpr int kPoly = 0x08;                   // which of 8 pairs of exponentials go to the multiply-add pipe (long prompt: none 8.40 ms, 1 8.33, 2 8.38, 3 8.85)
 
 struct Tile { uint32_t k, b; };                          // list entry, row block
 struct Item { uint32_t req, len, q0, nq; };              // slot, held tokens, first row, rows

@@ -189,8 +189,7 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of a pair on the multiply-add pipe (the special-function unit gives 4 exponentials a cycle and scheduler and is what a
-// softmax runs out of first).  x is split into an integer n, by adding and taking away 1.5 * 2^23, and |f| <= 1/2;
+// 2^x of a pair on the multiply-add pipe (the special-function unit gives 4 exponentials a cycle and scheduler).  x is split into an integer n, by adding and taking away 1.5 * 2^23, and |f| <= 1/2;
 // 2^f is a polynomial of degree 4 fitted for least relative error (2.6e-6) on that interval, 2^n is added to the
 // exponent.  x <= 2^6; below -126 the result is 2^-126 or less instead of 0.
 __device__ __forceinline__ float2 exp2_poly2(unsigned long long x)
