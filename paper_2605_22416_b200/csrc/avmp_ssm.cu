@@ -2,7 +2,7 @@
 //     S_t = exp(g_t) S_{t-1} + v_t k_t^T,   o_t = S_t q_t        (S: [dv][dk], fp32, one per request and head)
 //
 // ssm_step_kernel     one token per request: every state element is read once and written once, bound by HBM (1 GB of state:
-//                     387 to 416 us, 82 to 88 % of the measured copy rate).
+//                     372 us, 91 % of the measured copy rate).
 // ssm_prompt_kernel   whole prompts by pieces of 64 tokens: inside a piece the recurrence is two triangular
 //                     products, between pieces only the state is carried (65 521 tokens of 128 heads, dv 64, dk 16: 816 us,
 //                     2.7 TB/s of rows and state; bound by the latency of four warps per scheduler, not by HBM).
@@ -42,20 +42,36 @@ __device__ __forceinline__ float *ssm_item(const Geom &g, const SsmArgs &a, uint
 }
 
 // ---------------------------------------------------------------- one token
-constexpr int kStepCta = 256;
+// Division by a number known at launch: a multiply and two shifts (round-up method of Granlund and Montgomery, exact for 32 bits).
+struct Divider {
+    uint32_t mul, shift, one;      // one: the divisor is 1
+    static Divider of(uint32_t d)
+    {
+        uint32_t l = 0;
+        while (l < 32 && (1ull << l) < d) ++l;
+        return Divider{(uint32_t)((((1ull << l) - d) << 32) / d + 1), l ? l - 1 : 0, d == 1};
+    }
+    __device__ uint32_t operator()(uint32_t n) const
+    {
+        const uint32_t t = __umulhi(mul, n);
+        return one ? n : (t + ((n - t) >> 1)) >> shift;
+    }
+};
+
+constexpr int kStepCta = 128;                     // (256 threads: 391 us, 512: 423)
 constexpr uint32_t kStepTile = kStepCta * 4;      // state elements a CTA touches per round (a float4 per thread)
-constexpr int kStepRounds = 2;                    // rounds whose loads are in flight together (1 GB of state: 415 us with 1, 401 with 2, 441 with 4)
+constexpr int kStepRounds = 2;                    // rounds whose loads are in flight together (1 GB of state: 380 us with 1, 372 with 2, 456 with 4)
 
 template <class T, int DK>
 __global__ void __launch_bounds__(kStepCta)
-ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_elems)
+ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_elems, const Divider by_dv, const Divider by_rep)
 {
     constexpr int LANES = DK / 4;                 // lanes that share a state row
     pdl_prologue();
     const uint32_t k = blockIdx.x / parts, part = blockIdx.x % parts;
     const uint32_t r = a.reqs[k];
     float *S = ssm_block(g, a, r);
-    const uint32_t elems = a.heads * a.dv * DK, rep = a.heads / a.groups;
+    const uint32_t elems = a.heads * a.dv * DK;
     const uint32_t end = min(elems, (part + 1) * part_elems), own = threadIdx.x * 4;
     const uint8_t *qrow = a.q + k * a.qs, *krow = a.k + k * a.ks;
     const uint16_t *vrow = reinterpret_cast<const uint16_t *>(a.v + k * a.vs);
@@ -84,11 +100,11 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
             uint32_t row = 0;
             if (e < end) {
                 row = e / DK;
-                const uint32_t head = row / a.dv, grp = head / rep;
+                const uint32_t head = by_dv(row), grp = by_rep(head);
                 const uint2 kk = *reinterpret_cast<const uint2 *>(krow + (grp * DK + col) * 2);
                 const uint2 qq = *reinterpret_cast<const uint2 *>(qrow + (grp * DK + col) * 2);
                 const float2 k0 = T::unpack(kk.x), k1 = T::unpack(kk.y), q0 = T::unpack(qq.x), q1 = T::unpack(qq.y);
-                const float v = T::unpack(vrow[row]).x, w = expf(grow[head]);
+                const float v = T::unpack(vrow[row]).x, w = exp2_approx(grow[head] * 1.4426950408889634f);
                 // w == 0 clears the state, whatever it held
                 s[u].x = w == 0.f ? v * k0.x : fmaf(w, s[u].x, v * k0.x);
                 s[u].y = w == 0.f ? v * k0.y : fmaf(w, s[u].y, v * k0.y);
@@ -578,7 +594,8 @@ cudaError_t step_dk(const Geom &g, const SsmArgs &a, const Launch &l)
     uint32_t part = kStepTile * 16;
     while (part > kStepTile && (unsigned long long)a.n * ((elems + part - 1) / part) < 8ull * l.n_sms) part >>= 1;
     const uint32_t parts = (elems + part - 1) / part;
-    return launch_pdl(ssm_step_kernel<T, DK>, dim3(a.n * parts), dim3(kStepCta), 0, l.stream, g, a, parts, part);
+    return launch_pdl(ssm_step_kernel<T, DK>, dim3(a.n * parts), dim3(kStepCta), 0, l.stream, g, a, parts, part, Divider::of(a.dv),
+                      Divider::of(a.heads / a.groups));
 }
 
 template <class T, int DK, int DVT, int NT>
