@@ -312,6 +312,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     const unsigned long long t0 = global_ns();
                     while (!mbar_try(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1) && global_ns() - t0 < kWaitLimitNs) {}
                 }
+                const unsigned long long t0 = global_ns();      // and so do query rows
+                while (global_ns() - t0 < 1000000ull) {}
                 if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
             }
         } else if (w == 9) {

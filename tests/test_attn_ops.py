@@ -291,6 +291,8 @@ def test_buffers_larger_than_the_rows_in_them(total):
     q, _ = c.queries(total, 4)
     out, lse = torch.full((total, 4, 64), 7.0, dtype=c.dt, device="cuda"), torch.full((total, 4), 7.0, device="cuda")
     c.ctx.attn_prompt(c.layer, desc, _i32([0, 1]), 2, _i32([0, 2, 6]), total, q, out, lse, ws, size)
+    c.ctx.attn_prompt(c.layer, desc, _i32([0, 1]), 2, _i32([0, 0, 0]), 0, None, None, None, ws, size)      # no rows, no buffers
+    assert c.ctx.stats()["error_count"] == 0
     for r, a, b in ((0, 0, 2), (1, 2, 6)):
         want, want_lse = _exact(q[a:b], c.rows[r], 0.125, [300, 6][r] - (b - a))
         _check(out[a:b], lse[a:b], want, want_lse, f"slot {r}")

@@ -360,6 +360,23 @@ def test_graph_replay_other_stream_and_empty_lists():
     ctx.close()
 
 
+@pytest.mark.gpu
+def test_no_tokens_at_all():
+    """A list whose requests bring no rows: states are cleared, or kept where they are resumed; the row buffers may be absent."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    heads, dk, dv = 2, 64, 64
+    m = _model(heads, dk, dv)
+    ctx = _ctx(m, 4, [0, 1, 2])
+    gen = torch.Generator("cuda").manual_seed(4)
+    before, _ = _fill_state(ctx, 1, [0, 1, 2], m, gen)
+    desc = B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=torch.bfloat16)
+    ctx.ssm_prompt(1, desc, _i32([2, 0]), 2, _i32([0, 0, 0]), 0, _i32([0, 1]), None, None, None, None, None)
+    after, _ = _states(ctx, 1, [0, 1, 2], m)
+    assert torch.equal(after[:2], before[:2]) and (after[2] == 0).all() and ctx.stats()["error_count"] == 0
+    ctx.close()
+
+
 def test_refusals_on_the_host():
     """Arguments are checked before anything is launched (a made-up context on host memory: never dereferenced)."""
     import ctypes
