@@ -602,11 +602,16 @@ int avmp_attn_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, co
     return cu(e);
 }
 
-size_t avmp_ssm_workspace_bytes(const avmp_ctx *, const avmp_ssm_desc *, uint32_t, uint32_t) { return 0; }
+size_t avmp_ssm_workspace_bytes(const avmp_ctx *c, const avmp_ssm_desc *desc, uint32_t n, uint32_t total_tokens)
+{
+    if (!c || !ssm_desc_ok(c, desc) || n == 0) return 0;
+    const uint32_t shares = ssm_shares(n, desc->heads, desc->dv, total_tokens, c->n_sms);
+    return shares < 2 ? 0 : (size_t)n * shares * ((size_t)desc->heads * desc->dv * desc->dk + (size_t)desc->heads * (desc->dv / 32)) * 4;
+}
 
 int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n,
                     const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume, const void *d_q, const void *d_k,
-                    const void *d_v, const float *d_log_decay, void *d_out, void *, size_t, void *stream)
+                    const void *d_v, const float *d_log_decay, void *d_out, void *d_workspace, size_t workspace_bytes, void *stream)
 {
     if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !ssm_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
     if (n == 0) return AVMP_OK;
@@ -615,8 +620,15 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
     if (total_tokens >= (1u << 31) || (uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
     SsmArgs a = ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out);
     a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
-    c->launches += 1;
-    return cu(launch_ssm_prompt(c->g, a, L(c, stream)));
+    if (const size_t need = avmp_ssm_workspace_bytes(c, desc, n, total_tokens)) {
+        if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
+        if (workspace_bytes < need) return AVMP_ENOSPC;
+        a.ws = static_cast<float *>(d_workspace);
+    }
+    uint32_t launched = 0;
+    const cudaError_t e = launch_ssm_prompt(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
 }
 
 int avmp_ssm_step(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n, const void *d_q,

@@ -223,9 +223,11 @@ struct SsmArgs {
     const uint8_t *g;
     uint8_t *out;
     unsigned long long qs, ks, vs, gs, os;     // row strides in bytes
+    float *ws;                                 // prompts: states and decays of shares of a long prompt
 };
+uint32_t ssm_shares(uint32_t n, uint32_t heads, uint32_t dv, uint32_t total, int n_sms);
 cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l);
-cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l);
+cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *n_launched);
 // Attention over KV chains (avmp_attn.cu, avmp_attn_prompt.cu).
 struct AttnArgs {
     uint32_t layer, n, q_heads, kv_heads, head_dim, total_q;

@@ -130,6 +130,9 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
 // What is rounded to 16 bits: the scores after their decay and the state as an operand of Q S^T (both enter an output
 // that is rounded to 16 bits itself).  The state's own update keeps 32 bits: e^(..) v_j is split into
 // 16-bit parts, two for fp16 and three for bf16 (k_j has 16 bits to begin with), 2^-23 relative, and summed in 32 bits.
+// Where requests, heads and columns leave SMs idle, each prompt is cut into `shares` runs of pieces. A first pass works out
+// each run's final state from zero (the first run's from the state in the block) and its whole decay, a second one starts
+// every run from the states of those before it.
 // fp16 has little range: its scores (per row) and states and updates (per 16 rows of S) carry a power of two each.
 constexpr int kC = 64;                            // tokens per piece
 
@@ -177,7 +180,7 @@ __device__ __forceinline__ float pow2_to_2_13(float m)
 
 template <class T, int DK, int DVT, int NT>
 __global__ void __launch_bounds__(NT * 128, NT == 2 && DK == 16 ? 2 : 1)
-ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_constant__ CUtensorMap q_map,
+ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares, bool locals, const __grid_constant__ CUtensorMap q_map,
                   const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     using L = PromptSmem<DK, DVT, NT>;
@@ -187,24 +190,36 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
     constexpr int WM = DVT / 16;                  // warps of a team that own 16 rows of the state each
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t gave_up;
+    __shared__ float decayed;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     if (threadIdx.x == 0) {
         gave_up = 0;
+        decayed = 1.f;
         for (int i = 0; i < NT * L::kBufs; ++i) mbar_init(smem_u32(smem + L::oBars) + 8 * i, 1);
         mbar_fence_init();
     }
     pdl_prologue();
     const uint32_t per_req = a.heads * tiles;
-    const uint32_t k = blockIdx.x / per_req, head = (blockIdx.x % per_req) / tiles, tile = blockIdx.x % tiles;
-    const bool lead = blockIdx.x % per_req == 0;
+    // the first pass needs no last run
+    const uint32_t runs = locals ? shares - 1 : shares, run = blockIdx.x % runs, item = blockIdx.x / runs;
+    const uint32_t k = item / per_req, head = (item % per_req) / tiles, tile = item % tiles;
+    const bool lead = item % per_req == 0 && run == 0 && !locals;
     float *S = ssm_item(g, a, k, lead);
     if (!S) return;
-    const uint32_t row0 = a.cu[k], row1 = a.cu[k + 1];
+    uint32_t row0 = a.cu[k];
+    const uint32_t row1 = a.cu[k + 1];
     if (row1 < row0 || row1 > a.total) {
         if (lead && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
         return;
     }
-    const uint32_t len = row1 - row0, pieces = (len + kC - 1) / kC;
+    uint32_t len = row1 - row0, pieces = (len + kC - 1) / kC;
+    const bool last = run + 1 == shares;
+    if (shares > 1) {
+        const uint32_t p0 = (uint32_t)((unsigned long long)pieces * run / shares), p1 = (uint32_t)((unsigned long long)pieces * (run + 1) / shares);
+        row0 += p0 * kC;
+        len = min(len - p0 * kC, (p1 - p0) * kC);
+        pieces = p1 - p0;
+    }
     const bool resume = a.resume && a.resume[k];
     const uint32_t grp = head / (a.heads / a.groups);
     const int team = threadIdx.x / 128, tid = threadIdx.x % 128, w = tid / 32, lane = tid % 32;
@@ -214,6 +229,11 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
     float *decays = reinterpret_cast<float *>(smem + L::oW + team * 2 * L::kW);
     float *sscale = reinterpret_cast<float *>(smem + L::oScale);
     S += ((unsigned long long)head * a.dv + tile * DVT) * DK;
+    // workspace: [item][share] states, then decays.  The last share's place keeps the state that the first run starts from (the
+    // last run of the second pass may replace the block's before the first one reads it).
+    float *place = a.ws + (unsigned long long)item * shares * DVT * DK;
+    float *decays_out = a.ws + (unsigned long long)(gridDim.x / runs) * shares * DVT * DK + (unsigned long long)item * shares;
+    float *to = locals ? place + run * DVT * DK : last ? S : nullptr;
 
     constexpr int CV = DVT / 8;                            // 16-byte units per row of the output
     const unsigned long long own_row = row0 + (unsigned long long)team * kC;
@@ -293,12 +313,24 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
             *reinterpret_cast<uint32_t *>(sb + (w * 16 + lr + 8) * L::kQ + (n * 8 + lc) * 2) = T::pack(f[n][2] * sc, f[n][3] * sc);
         }
     };
-    auto store_state = [&](const float (&f)[ND][4]) {
+    auto put = [&](float *to, const float (&f)[ND][4]) {
 #pragma unroll
         for (int n = 0; n < ND; ++n) {
-            *reinterpret_cast<float2 *>(S + (w * 16 + lr) * DK + n * 8 + lc) = make_float2(f[n][0], f[n][1]);
-            *reinterpret_cast<float2 *>(S + (w * 16 + lr + 8) * DK + n * 8 + lc) = make_float2(f[n][2], f[n][3]);
+            *reinterpret_cast<float2 *>(to + (w * 16 + lr) * DK + n * 8 + lc) = make_float2(f[n][0], f[n][1]);
+            *reinterpret_cast<float2 *>(to + (w * 16 + lr + 8) * DK + n * 8 + lc) = make_float2(f[n][2], f[n][3]);
         }
+    };
+    auto get = [&](const float *from, float (&f)[ND][4]) {
+#pragma unroll
+        for (int n = 0; n < ND; ++n) {
+            const float2 x = *reinterpret_cast<const float2 *>(from + (w * 16 + lr) * DK + n * 8 + lc);
+            const float2 y = *reinterpret_cast<const float2 *>(from + (w * 16 + lr + 8) * DK + n * 8 + lc);
+            f[n][0] = x.x; f[n][1] = x.y; f[n][2] = y.x; f[n][3] = y.y;
+        }
+    };
+    auto store_state = [&](const float (&f)[ND][4]) {
+        if (to) put(to, f);
+        if (locals && w == 0 && lane == 0) decays_out[run] = decayed;
     };
 
     __syncthreads();
@@ -306,18 +338,30 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
     if (team == 0 && w < WM) {
         float f[ND][4];
 #pragma unroll
-        for (int n = 0; n < ND; ++n) {
-            float2 x = make_float2(0.f, 0.f), y = x;
-            if (resume) {
-                x = *reinterpret_cast<const float2 *>(S + (w * 16 + lr) * DK + n * 8 + lc);
-                y = *reinterpret_cast<const float2 *>(S + (w * 16 + lr + 8) * DK + n * 8 + lc);
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[n][i] = 0.f;
+        if (shares == 1 || locals) {
+            if (resume && run == 0) get(S, f);
+            if (locals && run == 0) put(place + (shares - 1) * DVT * DK, f);
+        } else {
+            get(place + (run ? 0 : shares - 1) * DVT * DK, f);
+            for (uint32_t j = 1; j < run; ++j) {
+                float x[ND][4];
+                get(place + j * DVT * DK, x);
+                const float d = decays_out[j];
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[n][i] = d == 0.f ? x[n][i] : fmaf(d, f[n][i], x[n][i]);
             }
-            f[n][0] = x.x; f[n][1] = x.y; f[n][2] = y.x; f[n][3] = y.y;
+        }
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) F[(n * 4 + i) * (WM * 32) + tid] = f[n][i];
-        }
         publish(f, 0);
-        if (pieces == 0 && !resume) store_state(f);
+        if (pieces == 0) store_state(f);
     }
     if (L::kBufs > 1 && w == 0) {          // the first piece's decays; later ones are worked out a piece ahead
         cp_async_wait<0>();
@@ -434,7 +478,8 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
                 weigh(pa, j, o);
             }
         };
-        if (w == 0) scores(std::integral_constant<int, 0>{});
+        if (locals) {}                             // states alone are wanted
+        else if (w == 0) scores(std::integral_constant<int, 0>{});
         else if (w == 1) scores(std::integral_constant<int, 1>{});
         else if (w == 2) scores(std::integral_constant<int, 2>{});
         else scores(std::integral_constant<int, 3>{});
@@ -516,6 +561,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
         if (p > 0) bar_sync(1 + team, 256);
         if (w < WM) {
             const float dec = exp2_approx(cs[kC - 1]);
+            if (locals && w == 0 && lane == 0) decayed *= dec;
 #pragma unroll
             for (int n = 0; n < ND; ++n)
 #pragma unroll
@@ -529,6 +575,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
         }
         if (p + 1 < pieces) bar_arrive(1 + (team + 1) % NT, 256);
 
+        if (!locals) {
         // ---- what the earlier pieces add to the outputs
         // r * (earlier blocks + e^c_ref Q S^T), then the own block on top
         const float r0 = exp2_approx(c0 - cref), r1 = exp2_approx(c1 - cref), er = exp2_approx(cref);
@@ -574,6 +621,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, const __grid_co
                 *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
         }
         og += (unsigned long long)NT * kC * a.os;
+        }
         buf = (buf + 1) % L::kBufs;
         bar_sync(kTeamBar + team, 128);             // the stage may be filled again, the next decays are there
         if (L::kBufs == 1) load(p + NT, 0);
@@ -599,7 +647,7 @@ cudaError_t step_dk(const Geom &g, const SsmArgs &a, const Launch &l)
 }
 
 template <class T, int DK, int DVT, int NT>
-cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
+cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *launched)
 {
     using L = PromptSmem<DK, DVT, NT>;
     static_assert(L::kTotal <= 227 * 1024, "shared memory of one CTA");
@@ -611,20 +659,28 @@ cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l)
                      rows_map(&k, a.k, a.groups * DK, a.total, a.ks, DK < 64 ? DK : 64, kC) &&
                      rows_map(&v, a.v, a.heads * a.dv, a.total, a.vs, DVT, kC)))
         return cudaErrorNotSupported;
-    return launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(a.n * a.heads * tiles), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles, q, k, v);
+    const uint32_t shares = ssm_shares(a.n, a.heads, a.dv, a.total, l.n_sms), items = a.n * a.heads * tiles;
+    if (shares > 1) {
+        const cudaError_t f = launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(items * (shares - 1)), dim3(NT * 128), L::kTotal, l.stream, g, a,
+                                         tiles, shares, true, q, k, v);
+        if (f != cudaSuccess) return f;
+        *launched += 1;
+    }
+    *launched += 1;
+    return launch_pdl(ssm_prompt_kernel<T, DK, DVT, NT>, dim3(items * shares), dim3(NT * 128), L::kTotal, l.stream, g, a, tiles, shares, false, q, k, v);
 }
 template <class T, int DVT>
-cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l)
+cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *launched)
 {
     // Short keys: two CTAs of two teams on an SM overlap their beginnings and ends (32 prompts of 272 tokens: 36 against 45 us;
     // 16 of 2048: 394 against 423), one of four teams walks a long prompt faster (65 521 tokens: 823 against 1697).  Only
     // the mean length is known here.
     const bool small = a.total / a.n < 1024u && (unsigned long long)a.n * a.heads * (a.dv / DVT) >= 2ull * l.n_sms;
     switch (a.dk) {
-    case 16: return small ? prompt_launch<T, 16, DVT, 2>(g, a, l) : prompt_launch<T, 16, DVT, 4>(g, a, l);
-    case 32: return prompt_launch<T, 32, DVT, 3>(g, a, l);
-    case 64: return prompt_launch<T, 64, DVT, 2>(g, a, l);
-    default: return prompt_launch<T, 128, DVT, 2>(g, a, l);
+    case 16: return small ? prompt_launch<T, 16, DVT, 2>(g, a, l, launched) : prompt_launch<T, 16, DVT, 4>(g, a, l, launched);
+    case 32: return prompt_launch<T, 32, DVT, 3>(g, a, l, launched);
+    case 64: return prompt_launch<T, 64, DVT, 2>(g, a, l, launched);
+    default: return prompt_launch<T, 128, DVT, 2>(g, a, l, launched);
     }
 }
 template <class T>
@@ -644,10 +700,20 @@ cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l)
 {
     return a.f16 ? step_type<F16>(g, a, l) : step_type<Bf16>(g, a, l);
 }
-cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l)
+cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *launched)
 {
-    if (a.dv % 64 == 0) return a.f16 ? prompt_dv<F16, 64>(g, a, l) : prompt_dv<Bf16, 64>(g, a, l);
-    return a.f16 ? prompt_dv<F16, 32>(g, a, l) : prompt_dv<Bf16, 32>(g, a, l);
+    if (a.dv % 64 == 0) return a.f16 ? prompt_dv<F16, 64>(g, a, l, launched) : prompt_dv<Bf16, 64>(g, a, l, launched);
+    return a.f16 ? prompt_dv<F16, 32>(g, a, l, launched) : prompt_dv<Bf16, 32>(g, a, l, launched);
+}
+// Runs that each prompt is cut into: as many as leave no SM without one, of 8 pieces or more on the mean; 1 where the first pass
+// would cost more than it gives (it reads keys and values once more).  65 536 tokens of 1 head 58 us against 789 in one run,
+// of 8 heads 93 against 797, of 48 468 against 805; 16 384 tokens of 32 heads of 64 keys 174 against 389.
+uint32_t ssm_shares(uint32_t n, uint32_t heads, uint32_t dv, uint32_t total, int n_sms)
+{
+    const unsigned long long items = (unsigned long long)n * heads * (dv % 64 ? dv / 32 : dv / 64);
+    unsigned long long s = (unsigned long long)n_sms / items;
+    if (s > total / n / (8 * kC)) s = total / n / (8 * kC);
+    return s < 3 ? 1u : (uint32_t)(s < 32 ? s : 32);
 }
 
 }  // namespace avmp

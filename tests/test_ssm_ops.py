@@ -225,6 +225,49 @@ def test_prompts(dtype, case):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,heads,dk,dv,lens,resume", [("bfloat16", 1, 16, 64, [9001], [1]), ("float16", 2, 64, 32, [20, 0, 6000], [1, 1, 0]),
+                                                           ("bfloat16", 3, 128, 64, [4097, 65], [0, 1]), ("bfloat16", 1, 32, 32, [2048], [0])])
+def test_long_prompts_of_few_heads(dtype, heads, dk, dv, lens, resume):
+    """Prompts that are cut into runs over the SMs: same state and outputs; short and empty requests beside them; a reset inside."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt = getattr(torch, dtype)
+    m = _model(heads, dk, dv)
+    n, tot = len(lens), sum(lens)
+    ctx = _ctx(m, 6, list(range(n)))
+    gen = torch.Generator("cuda").manual_seed(dk)
+    first, conv = _fill_state(ctx, 1, list(range(n)), m, gen)
+    q, k = ((torch.randn(tot, 1, dk, device="cuda", generator=gen) * 0.2).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) ** 6 * 0.2
+    g[tot // 2, 0] = -math.inf
+    desc = B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=dt)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    size = ctx.ssm_workspace_bytes(desc, n, tot)
+    assert size > 0
+    with pytest.raises(B.AvmpError, match="invalid argument"):
+        ctx.ssm_prompt(1, desc, _i32(range(n)), n, _i32(cu), tot, _i32(resume), q, k, v, g, v)
+    ws = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    with pytest.raises(B.AvmpError, match="workspace too small"):
+        ctx.ssm_prompt(1, desc, _i32(range(n)), n, _i32(cu), tot, _i32(resume), q, k, v, g, v, ws, size - 16)
+    for rep in range(2):
+        ctx.scatter_ssm(1, _i32(range(n)), n, first, conv)
+        out = torch.zeros_like(v)
+        ctx.ssm_prompt(1, desc, _i32(range(n)), n, _i32(cu), tot, _i32(resume), q, k, v, g, out, ws, size)
+    st, cv = _states(ctx, 1, list(range(n)), m)
+    for i in range(n):
+        a, b = cu[i], cu[i + 1]
+        S, o = _recurrence(first[i].view(heads, dv, dk).double() * resume[i], q[a:b], k[a:b], v[a:b], g[a:b], heads)
+        if lens[i]:
+            _check(st[i].view(heads, dv, dk), S, STATE_TOL, f"state {i}")
+            _check(out[a:b], o, _out_tol(dt), f"out {i}")
+        else:
+            assert torch.equal(st[i].view(heads, dv, dk), S.float())
+    assert (ws[size:] == 0xFF).all() and torch.equal(cv, conv) and ctx.stats()["error_count"] == 0
+    ctx.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [2.0 ** -12, 2.0 ** 9])
 def test_half_precision_inputs_of_extreme_size(scale):
     """fp16 rows near the ends of their range: scores and states pass 65504 and fall below 2^-14."""
