@@ -576,51 +576,51 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
         if (p + 1 < pieces) bar_arrive(1 + (team + 1) % NT, 256);
 
         if (!locals) {
-        // ---- what the earlier pieces add to the outputs
-        // r * (earlier blocks + e^c_ref Q S^T), then the own block on top
-        const float r0 = exp2_approx(c0 - cref), r1 = exp2_approx(c1 - cref), er = exp2_approx(cref);
-        const float z0 = r0 * sd0 / so0, z1 = r1 * sd1 / so1, y0 = r0 * sd0 * er, y1 = r1 * sd1 * er;
-        const uint32_t sb = smem_u32(smem + L::oS + (p % L::kRing) * L::kS);
+            // ---- what the earlier pieces add to the outputs
+            // r * (earlier blocks + e^c_ref Q S^T), then the own block on top
+            const float r0 = exp2_approx(c0 - cref), r1 = exp2_approx(c1 - cref), er = exp2_approx(cref);
+            const float z0 = r0 * sd0 / so0, z1 = r1 * sd1 / so1, y0 = r0 * sd0 * er, y1 = r1 * sd1 * er;
+            const uint32_t sb = smem_u32(smem + L::oS + (p % L::kRing) * L::kS);
 #pragma unroll
-        for (int n = 0; n < NV / 2; ++n) {
-            float x[2][4] = {};
+            for (int n = 0; n < NV / 2; ++n) {
+                float x[2][4] = {};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                uint32_t b[4];
-                ldsm4(b, sb + (n * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
-                T::mma(x[0], aq[s], b[0], b[1]);
-                T::mma(x[1], aq[s], b[2], b[3]);
+                for (int s = 0; s < KS; ++s) {
+                    uint32_t b[4];
+                    ldsm4(b, sb + (n * 16 + (lane & 7) + ((lane >> 4) << 3)) * L::kQ + s * 32 + ((lane >> 3) & 1) * 16);
+                    T::mma(x[0], aq[s], b[0], b[1]);
+                    T::mma(x[1], aq[s], b[2], b[3]);
+                }
+                const float sc = T::kF16 ? sscale[(p % L::kRing) * 4 + n] : 1.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // a cleared state adds nothing, whatever it held
+                    float *y = o[2 * n + h];
+                    y[0] = fmaf(y[0], z0, y0 == 0.f ? 0.f : x[h][0] * (y0 * sc)); y[1] = fmaf(y[1], z0, y0 == 0.f ? 0.f : x[h][1] * (y0 * sc));
+                    y[2] = fmaf(y[2], z1, y1 == 0.f ? 0.f : x[h][2] * (y1 * sc)); y[3] = fmaf(y[3], z1, y1 == 0.f ? 0.f : x[h][3] * (y1 * sc));
+                }
             }
-            const float sc = T::kF16 ? sscale[(p % L::kRing) * 4 + n] : 1.f;
+            weigh(own, w, o);
+            if (T::kF16) {
+                const float i0 = 1.f / sd0, i1 = 1.f / sd1;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // a cleared state adds nothing, whatever it held
-                float *y = o[2 * n + h];
-                y[0] = fmaf(y[0], z0, y0 == 0.f ? 0.f : x[h][0] * (y0 * sc)); y[1] = fmaf(y[1], z0, y0 == 0.f ? 0.f : x[h][1] * (y0 * sc));
-                y[2] = fmaf(y[2], z1, y1 == 0.f ? 0.f : x[h][2] * (y1 * sc)); y[3] = fmaf(y[3], z1, y1 == 0.f ? 0.f : x[h][3] * (y1 * sc));
+                for (int n = 0; n < NV; ++n) { o[n][0] *= i0; o[n][1] *= i0; o[n][2] *= i1; o[n][3] *= i1; }
             }
-        }
-        weigh(own, w, o);
-        if (T::kF16) {
-            const float i0 = 1.f / sd0, i1 = 1.f / sd1;
+            // ---- rows out, whole 16-byte units
+            uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
 #pragma unroll
-            for (int n = 0; n < NV; ++n) { o[n][0] *= i0; o[n][1] *= i0; o[n][2] *= i1; o[n][3] *= i1; }
-        }
-        // ---- rows out, whole 16-byte units
-        uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
+            for (int n = 0; n < NV; ++n) {
+                *reinterpret_cast<uint32_t *>(so + lr * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][0], o[n][1]);
+                *reinterpret_cast<uint32_t *>(so + (lr + 8) * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][2], o[n][3]);
+            }
+            __syncwarp();
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            *reinterpret_cast<uint32_t *>(so + lr * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][0], o[n][1]);
-            *reinterpret_cast<uint32_t *>(so + (lr + 8) * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][2], o[n][3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 16 * CV / 32; ++i) {
-            const uint32_t t = lane / CV + i * (32 / CV);
-            if (p * kC + w * 16 + t < len)
-                *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
-        }
-        og += (unsigned long long)NT * kC * a.os;
+            for (int i = 0; i < 16 * CV / 32; ++i) {
+                const uint32_t t = lane / CV + i * (32 / CV);
+                if (p * kC + w * 16 + t < len)
+                    *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
+            }
+            og += (unsigned long long)NT * kC * a.os;
         }
         buf = (buf + 1) % L::kBufs;
         bar_sync(kTeamBar + team, 128);             // the stage may be filled again, the next decays are there
