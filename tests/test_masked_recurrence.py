@@ -1,0 +1,104 @@
+"""The recurrence on the SSM state blocks where rows must not count (tokens behind a row, tokens in front of a reset), bounds
+entry by entry, and states that are carried over the runs that a long prompt is cut into.
+
+Tolerances.  An output is sum over tokens and dk of terms e^(..) v k q.  Rounded to 16 bits are the decayed scores, the carried
+state as an operand, and the output: 3 * eps/2 of the sum of the terms' absolute values (which the same recurrence on absolute
+values gives); exponents of up to 600 in log2 units are good to 2^-15, and that with the 32-bit sums stays inside a quarter
+of eps/2.  The state: e^(..) v enters with 22 bits (fp16, two parts) or 24 (bf16, three), exponentials are good to 2^-22, one to a
+term and one more for each piece of 64 tokens it is carried over: (pieces + 2) * 2^-22 norm-wise."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+from test_ssm_ops import _ctx, _fill_state, _i32, _model, _states
+
+
+def _recurrence(S, q, k, v, g, rep):
+    """64 bits, token by token: state, outputs, and the outputs of the absolute values.  S [heads, dv, dk]."""
+    import torch
+    out = torch.zeros(v.shape, dtype=torch.float64, device=v.device)
+    size, A = torch.zeros_like(out), S.abs()
+    q, k = (x.double().repeat_interleave(rep, 1) for x in (q, k))
+    v, g = v.double(), g.double()
+    for t in range(v.shape[0]):
+        w = g[t].exp()[:, None, None]
+        vk = v[t][:, :, None] * k[t][:, None, :]
+        S = torch.where(w == 0, vk, S * w + vk)
+        A = torch.where(w == 0, vk.abs(), A * w + vk.abs())
+        out[t] = (S * q[t][:, None, :]).sum(-1)
+        size[t] = (A * q[t][:, None, :].abs()).sum(-1)
+    return S, out, size
+
+
+def _near(out, want, size, what):
+    """Finite where the definition is, and close there."""
+    import torch
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(out), fin), f"{what}: {int((torch.isfinite(out) != fin).sum())} entries finite or not where they should be"
+    d = ((out.double() - want).abs() - 3.25 * torch.finfo(out.dtype).eps / 2 * size)[fin]
+    assert d.numel() == 0 or float(d.max()) <= 0, f"{what}: {float(d.max()):.3g} too far off"
+
+
+def _near_state(got, want, pieces, what):
+    import torch
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fin), f"{what}: {int((torch.isfinite(got) != fin).sum())} entries finite or not where they should be"
+    err = float(((got.double() - want)[fin]).norm() / want[fin].norm().clamp(min=1e-300))
+    assert err <= (pieces + 2) * 2.0 ** -22, f"{what}: relative error {err:.3g}"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,groups,dk,dv,lens", [(4, 2, 16, 64, [300, 17]), (2, 1, 32, 96, [250]), (2, 1, 64, 64, [200, 65]), (2, 2, 128, 32, [130])])
+def test_entry_by_entry(dtype, heads, groups, dk, dv, lens):
+    """Finite rows: every output by itself, and states to the precision that three (two) 16-bit parts of e^(..) v give."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, m, n, tot = getattr(torch, dtype), _model(heads, dk, dv), len(lens), sum(lens)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    ctx = _ctx(m, 4, list(range(n)))
+    gen = torch.Generator("cuda").manual_seed(dk + dv)
+    q, k = ((torch.randn(tot, groups, dk, device="cuda", generator=gen) * 0.3).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) ** 4 * 0.2
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(0, B.ssm_desc(heads=heads, groups=groups, dk=dk, dv=dv, dtype=dt), _i32(range(n)), n, _i32(cu), tot, None, q, k, v, g, out)
+    st, _ = _states(ctx, 0, list(range(n)), m)
+    for r in range(n):
+        a, b = cu[r], cu[r + 1]
+        S, o, size = _recurrence(torch.zeros(heads, dv, dk, dtype=torch.float64, device="cuda"), q[a:b], k[a:b], v[a:b], g[a:b], heads // groups)
+        _near(out[a:b], o, size, f"request {r}")
+        _near_state(st[r].view(heads, dv, dk), S, -(-lens[r] // 64), f"state {r}")
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,heads,dk,dv,lens", [("bfloat16", 1, 16, 64, [4000]), ("float16", 2, 64, 32, [33, 6000]), ("bfloat16", 3, 128, 64, [4097])])
+def test_states_carried_over_the_runs_of_a_cut_prompt(dtype, heads, dk, dv, lens):
+    """Decays so gentle that the state in the block and every earlier run count visibly in the last one."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, m, n, tot = getattr(torch, dtype), _model(heads, dk, dv), len(lens), sum(lens)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    ctx = _ctx(m, 4, list(range(n)))
+    gen = torch.Generator("cuda").manual_seed(dk)
+    first, _ = _fill_state(ctx, 1, list(range(n)), m, gen, scale=30.0)
+    q, k = ((torch.randn(tot, 1, dk, device="cuda", generator=gen) * 0.2).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) * 2e-4
+    desc = B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=dt)
+    size = ctx.ssm_workspace_bytes(desc, n, tot)
+    assert size > 0
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(1, desc, _i32(range(n)), n, _i32(cu), tot, _i32([1] * n), q, k, v, g, out, ws, size)
+    st, _ = _states(ctx, 1, list(range(n)), m)
+    for r in range(n):
+        a, b = cu[r], cu[r + 1]
+        S, o, mass = _recurrence(first[r].view(heads, dv, dk).double(), q[a:b], k[a:b], v[a:b], g[a:b], heads)
+        _near(out[a:b], o, mass, f"request {r}")
+        _near_state(st[r].view(heads, dv, dk), S, -(-lens[r] // 64), f"state {r}")
+    ctx.close()
