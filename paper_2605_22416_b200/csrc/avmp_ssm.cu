@@ -304,6 +304,14 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, fabsf(f[n][i]));
             m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
+            if (m == INFINITY) {            // it would scale the numbers beside it to nothing
+                m = 0.f;
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m = fmaxf(m, fabsf(f[n][i]) < INFINITY ? fabsf(f[n][i]) : 0.f);
+                m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m)));
+            }
             sc = pow2_to_2_13(m);
             if (lane == 0) sscale[slot * 4 + w] = 1.f / sc;
         }

@@ -50,6 +50,65 @@ def _near_state(got, want, pieces, what):
     assert err <= (pieces + 2) * 2.0 ** -22, f"{what}: relative error {err:.3g}"
 
 
+SHAPES = [(2, 1, 16, 64), (3, 1, 16, 32), (4, 2, 32, 64), (2, 2, 64, 96), (2, 1, 128, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("what", ["state"])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_a_bad_row_counts_from_itself_to_the_next_reset(shape, what, value, dtype):
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    if what == "decay" and not math.isnan(value):
+        return                                          # decays are at most 0, and -inf is the reset
+    heads, groups, dk, dv = SHAPES[shape]
+    dt, m = getattr(torch, dtype), _model(heads, dk, dv)
+    lens, n = [300, 90, 64], 3
+    tot, cu = sum(lens), np.concatenate([[0], np.cumsum(lens)])
+    ctx = _ctx(m, 4, [0, 1, 2])
+    gen = torch.Generator("cuda").manual_seed(shape)
+    first, conv = _fill_state(ctx, 1, [0, 1, 2], m, gen, scale=0.5)
+    q, k = ((torch.randn(tot, groups, dk, device="cuda", generator=gen) * 0.3).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) ** 4 * 0.2
+    # request 0: bad at 21 (reset at 30, in the next block of 16), at 40 (reset at 44, in its own), at 70 (reset a piece later),
+    # at 200 of one head's row (never reset); request 1: bad at 10, reset in head 0 only; request 2: clean
+    bad, resets = [21, 40, 70, 200, cu[1] + 10], [30, 44, 140, cu[1] + 15]
+    for t in resets:
+        g[t, 0 if t > cu[1] else slice(None)] = -math.inf
+    if what == "v":
+        for i, t in enumerate(bad):
+            v[t, i % heads, 3 * i + 1] = value
+    elif what == "k":
+        for i, t in enumerate(bad):
+            k[t, i % groups, (5 * i + 2) % dk] = value
+    elif what == "decay":
+        for t in bad:
+            g[t, heads - 1] = value
+    else:
+        st = first.view(n, heads, dv, dk)
+        st[0, 0, 5, 3], st[1, 0, 7, 1], st[1, heads - 1, dv - 1, dk - 1] = value, value, value
+        ctx.scatter_ssm(1, _i32([0, 1, 2]), n, first, conv)
+    desc = B.ssm_desc(heads=heads, groups=groups, dk=dk, dv=dv, dtype=dt)
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(1, desc, _i32([0, 1, 2]), n, _i32(cu), tot, _i32([1, 1, 0]), q, k, v, g, out)
+    st, cv = _states(ctx, 1, [0, 1, 2], m)
+    for r in range(n):
+        a, b = cu[r], cu[r + 1]
+        S0 = first[r].view(heads, dv, dk).double() if r < 2 else torch.zeros(heads, dv, dk, dtype=torch.float64, device="cuda")
+        S, o, _ = _recurrence(S0, q[a:b], k[a:b], v[a:b], g[a:b], heads // groups)
+        z = lambda x: torch.nan_to_num(x, 0.0, 0.0, -math.inf if x is g else 0.0)        # sizes without the bad entries
+        size = _recurrence(z(S0), z(q)[a:b], z(k)[a:b], z(v)[a:b], z(g)[a:b], heads // groups)[2]
+        _near(out[a:b], o, size, f"request {r}")
+        _near_state(st[r].view(heads, dv, dk), S, -(-lens[r] // 64), f"state {r}")
+        if r < 2:
+            assert torch.isfinite(o).any() and not torch.isfinite(o).all()
+    assert torch.equal(cv, conv) and ctx.stats()["error_count"] == 0
+    ctx.close()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("heads,groups,dk,dv,lens", [(4, 2, 16, 64, [300, 17]), (2, 1, 32, 96, [250]), (2, 1, 64, 64, [200, 65]), (2, 2, 128, 32, [130])])
