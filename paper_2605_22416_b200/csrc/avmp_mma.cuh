@@ -88,8 +88,17 @@ __device__ __forceinline__ void quad_transpose(uint32_t (&a)[4])
     }
 }
 
-// Named barriers: `n` threads in all; an arrival does not wait.
+// Named barriers: `n` threads in all; an arrival does not wait; bar_or tells whether any thread brought true.
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "r"(n) : "memory"); }
+
+__device__ __forceinline__ bool bar_or(int id, int n, bool v)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\t"
+                 "barrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)v) : "memory");
+    return r != 0;
+}
 
 }  // namespace avmp

@@ -4,8 +4,8 @@
 // ssm_step_kernel     one token per request: every state element is read once and written once, bound by HBM (1 GB of state:
 //                     372 us, 91 % of the measured copy rate).
 // ssm_prompt_kernel   whole prompts by pieces of 64 tokens: inside a piece the recurrence is two triangular
-//                     products, between pieces only the state is carried (65 521 tokens of 128 heads, dv 64, dk 16: 816 us,
-//                     2.7 TB/s of rows and state; bound by the latency of four warps per scheduler, not by HBM).
+//                     products, between pieces only the state is carried (65 521 tokens of 128 heads, dv 64, dk 16: 875 us,
+//                     2.6 TB/s of rows and state; bound by the latency of four warps per scheduler, not by HBM).
 #include "avmp_tc.cuh"
 
 #include <type_traits>
@@ -134,6 +134,10 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
 // each run's final state from zero (the first run's from the state in the block) and its whole decay, a second one starts
 // every run from the states of those before it.
 // fp16 has little range: its scores (per row) and states and updates (per 16 rows of S) carry a power of two each.
+// A product takes in rows that count for nothing with a weight of zero, and 0 x NaN and 0 x inf are NaN; the parts of an infinite
+// e^(..) v are inf - inf.  Every row of V and K enters some warp's update, so an update that is not finite shows a piece with such a
+// row: its update and its output rows are then worked out again token by token, as the recurrence is written (walk_state, walk_rows).
+// The look at the updates costs 5 % (the prompt above: 826 us without).
 constexpr int kC = 64;                            // tokens per piece
 
 template <int DK, int DVT, int NT>
@@ -176,6 +180,77 @@ __device__ __forceinline__ float pow2_to_2_13(float m)
     if (m == 0.f) e = 13;
     e = max(-60, min(60, 13 - e));
     return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+template <int DK>
+__device__ __forceinline__ uint32_t place_k(uint32_t r, uint32_t c)        // 16-byte unit c of a row of Q or K in a stage
+{
+    constexpr int kRowK = DK < 64 ? DK * 2 : 128;
+    return DK == 128 ? (c >> 3) * (kC * 128) + unit<128>(r, c & 7) : unit<kRowK>(r, c);
+}
+
+// A piece's update token by token, for 16 rows of the state from `d` on: F (this thread's places in it, `pitch` apart) from the
+// state in front to the one behind.  Returns the decay over the piece.  Whole warp; not inlined, so that its registers cost nothing elsewhere.
+template <class T, class L, int DK, int DVT>
+__device__ __noinline__ float walk_state(const uint8_t *st, uint32_t tokens, uint32_t d, float *F, uint32_t pitch)
+{
+    const uint32_t lane = threadIdx.x % 32, lc = (lane & 3) * 2;
+    const float *g = reinterpret_cast<const float *>(st + L::kStageG);
+    float over = 1.f;
+    d += lane >> 2;
+    for (uint32_t t = 0; t < tokens; ++t) {
+        const float w = exp2_approx(g[t] * 1.4426950408889634f);
+        const uint8_t *row = st + L::kStageV + (d & 7) * 2;
+        const float v0 = T::unpack(*reinterpret_cast<const uint16_t *>(row + unit<L::kRowV>(t, d >> 3))).x;
+        const float v1 = T::unpack(*reinterpret_cast<const uint16_t *>(row + unit<L::kRowV>(t, (d >> 3) + 1))).x;
+#pragma unroll 1
+        for (uint32_t n = 0; n < DK / 8; ++n) {
+            const float2 k = T::unpack(*reinterpret_cast<const uint32_t *>(st + L::kStageK + place_k<DK>(t, n) + lc * 2));
+            const float add[4] = {v0 * k.x, v0 * k.y, v1 * k.x, v1 * k.y};
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                float *f = F + (n * 4 + i) * pitch;
+                *f = w == 0.f ? add[i] : fmaf(w, *f, add[i]);
+            }
+        }
+        over = w == 0.f ? 0.f : over * w;
+    }
+    return over;
+}
+
+// Output rows row0 .. row1 of a piece, each from the last token it sees backwards to a reset or to the state in front of the
+// piece (its 16-bit copy sb, with the factors sc); into `so`.  Whole warp.
+template <class T, class L, int DK, int DVT>
+__device__ __noinline__ void walk_rows(const uint8_t *st, const uint8_t *sb, const float *sc, uint32_t row0, uint32_t row1, uint8_t *so)
+{
+    const uint32_t lane = threadIdx.x % 32;
+    const float *g = reinterpret_cast<const float *>(st + L::kStageG);
+    auto number = [](const uint8_t *unit_at, uint32_t c) { return T::unpack(*reinterpret_cast<const uint16_t *>(unit_at + (c & 7) * 2)).x; };
+    for (uint32_t r = row0; r < row1; ++r, so += L::kV) {
+        float acc[DVT / 32] = {}, weight = 1.f;
+        for (int j = (int)r; j >= 0 && weight != 0.f; --j) {
+            float s = 0.f;
+            for (uint32_t c = lane; c < DK; c += 32)
+                s += number(st + L::kStageQ + place_k<DK>(r, c >> 3), c) * number(st + L::kStageK + place_k<DK>(j, c >> 3), c);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+#pragma unroll
+            for (uint32_t x = 0; x < DVT / 32; ++x)
+                acc[x] += s * weight * number(st + L::kStageV + unit<L::kRowV>(j, (lane + x * 32) >> 3), lane);
+            const float w = exp2_approx(g[j] * 1.4426950408889634f);
+            weight = w == 0.f ? 0.f : weight * w;
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < DVT / 32; ++x) {
+            const uint32_t d = lane + x * 32;
+            if (weight != 0.f) {
+                float s = 0.f;
+                for (uint32_t c = 0; c < DK; ++c) s += number(st + L::kStageQ + place_k<DK>(r, c >> 3), c) * number(sb + d * L::kQ + (c >> 3) * 16, c);
+                acc[x] += weight * s * (T::kF16 ? sc[d >> 4] : 1.f);
+            }
+            *reinterpret_cast<uint16_t *>(so + d * 2) = (uint16_t)T::pack(acc[x], 0.f);
+        }
+    }
 }
 
 template <class T, int DK, int DVT, int NT>
@@ -267,9 +342,6 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
         cp_async_commit();
     };
 
-    auto place_k = [](uint32_t r, uint32_t c) {             // 16-byte unit c of a row of Q or K
-        return DK == 128 ? (c >> 3) * (kC * 128) + unit<128>(r, c & 7) : unit<L::kRowK>(r, c);
-    };
     // First warp: running sums in units of log2, from the front for the decays, from the back for the tail weights (the weights
     // of the state keep their relative precision that way).
     auto scan = [&](const float *gs, float *cs) {
@@ -319,6 +391,15 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
         for (int n = 0; n < ND; ++n) {
             *reinterpret_cast<uint32_t *>(sb + (w * 16 + lr) * L::kQ + (n * 8 + lc) * 2) = T::pack(f[n][0] * sc, f[n][1] * sc);
             *reinterpret_cast<uint32_t *>(sb + (w * 16 + lr + 8) * L::kQ + (n * 8 + lc) * 2) = T::pack(f[n][2] * sc, f[n][3] * sc);
+        }
+    };
+    // This warp's rows of piece p, whole 16-byte units.
+    auto rows_out = [&](uint32_t p, const uint8_t *so) {
+#pragma unroll
+        for (int i = 0; i < 16 * CV / 32; ++i) {
+            const uint32_t t = lane / CV + i * (32 / CV);
+            if (p * kC + w * 16 + t < len)
+                *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
         }
     };
     auto put = [&](float *to, const float (&f)[ND][4]) {
@@ -412,7 +493,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
         // front c_ref on, times a column factor up to it (both at most 1); inside the own block it is one per pair.
         uint32_t aq[KS][4];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + place_k(w * 16 + (lane & 15), s * 2 + (lane >> 4)));
+        for (int s = 0; s < KS; ++s) ldsm4(aq[s], sq + place_k<DK>(w * 16 + (lane & 15), s * 2 + (lane >> 4)));
         const float c0 = cs[w * 16 + lr], c1 = cs[w * 16 + lr + 8], cref = w ? cs[w * 16 - 1] : 0.f;
         auto score = [&](int j, float (&x)[2][4]) {
 #pragma unroll
@@ -420,7 +501,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 uint32_t b[4];
-                ldsm4(b, sk + place_k(j * 16 + (lane & 7) + ((lane >> 4) << 3), s * 2 + ((lane >> 3) & 1)));
+                ldsm4(b, sk + place_k<DK>(j * 16 + (lane & 7) + ((lane >> 4) << 3), s * 2 + ((lane >> 3) & 1)));
                 T::mma(x[0], aq[s], b[0], b[1]);
                 T::mma(x[1], aq[s], b[2], b[3]);
             }
@@ -541,7 +622,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
 #pragma unroll
                 for (int n = 0; n < ND / 2; ++n) {
                     uint32_t b[4];
-                    ldsm4_t(b, sk + place_k(j * 16 + (lane & 15), n * 2 + (lane >> 4)));
+                    ldsm4_t(b, sk + place_k<DK>(j * 16 + (lane & 15), n * 2 + (lane >> 4)));
 #pragma unroll
                     for (int y = 0; y < (T::kF16 ? 2 : 3); ++y) {
                         T::mma(part[y % kSums][2 * n], x3[y], b[0], b[1]);
@@ -567,9 +648,14 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
 
         // ---- hand-over: wait for the state in front of this piece, pass the one behind it on at once
         if (p > 0) bar_sync(1 + team, 256);
+        bool odd = false;                              // the update is not finite
         if (w < WM) {
-            const float dec = exp2_approx(cs[kC - 1]);
-            if (locals && w == 0 && lane == 0) decayed *= dec;
+            float dec = exp2_approx(cs[kC - 1]), mark = cs[kC - 1] * 0.f;        // 0, or NaN once a number is not finite
+#pragma unroll
+            for (int n = 0; n < ND; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mark = fmaf(ds[n][i], 0.f, mark);
+            odd = __any_sync(0xFFFFFFFFu, mark != 0.f);
 #pragma unroll
             for (int n = 0; n < ND; ++n)
 #pragma unroll
@@ -577,8 +663,16 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
                     float *f = F + (n * 4 + i) * (WM * 32) + tid;
                     const float add = T::kF16 ? ds[n][i] * dinv : ds[n][i];
                     ds[n][i] = dec == 0.f ? add : fmaf(dec, *f, add);
-                    *f = ds[n][i];
+                    if (!odd) *f = ds[n][i];
                 }
+            if (odd) {
+                dec = walk_state<T, L, DK, DVT>(st, min((uint32_t)kC, len - p * kC), w * 16, F + tid, WM * 32);
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ds[n][i] = F[(n * 4 + i) * (WM * 32) + tid];
+            }
+            if (locals && w == 0 && lane == 0) decayed = dec == 0.f ? 0.f : decayed * dec;
             if (p + 1 < pieces) publish(ds, p + 1); else store_state(ds);
         }
         if (p + 1 < pieces) bar_arrive(1 + (team + 1) % NT, 256);
@@ -614,7 +708,7 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
 #pragma unroll
                 for (int n = 0; n < NV; ++n) { o[n][0] *= i0; o[n][1] *= i0; o[n][2] *= i1; o[n][3] *= i1; }
             }
-            // ---- rows out, whole 16-byte units
+            // ---- rows out
             uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
@@ -622,16 +716,19 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
                 *reinterpret_cast<uint32_t *>(so + (lr + 8) * L::kV + (n * 8 + lc) * 2) = T::pack(o[n][2], o[n][3]);
             }
             __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 16 * CV / 32; ++i) {
-                const uint32_t t = lane / CV + i * (32 / CV);
-                if (p * kC + w * 16 + t < len)
-                    *reinterpret_cast<uint4 *>(og + i * (32 / CV) * a.os) = *reinterpret_cast<const uint4 *>(so + t * L::kV + lane % CV * 16);
-            }
-            og += (unsigned long long)NT * kC * a.os;
+            rows_out(p, so);
         }
+        if (bar_or(kTeamBar + team, 128, odd) && !locals) {
+            uint8_t *so = smem + L::oO + team * L::kO + w * 16 * L::kV;
+            walk_rows<T, L, DK, DVT>(st, smem + L::oS + (p % L::kRing) * L::kS, sscale + (p % L::kRing) * 4, w * 16,
+                                     min((uint32_t)w * 16 + 16, len - p * kC), so);
+            __syncwarp();
+            rows_out(p, so);
+            bar_sync(kTeamBar + team, 128);
+        }
+        // the stage may be filled again, the next decays are there
+        og += (unsigned long long)NT * kC * a.os;
         buf = (buf + 1) % L::kBufs;
-        bar_sync(kTeamBar + team, 128);             // the stage may be filled again, the next decays are there
         if (L::kBufs == 1) load(p + NT, 0);
     }
     cp_async_wait<0>();

@@ -56,7 +56,7 @@ SHAPES = [(2, 1, 16, 64), (3, 1, 16, 32), (4, 2, 32, 64), (2, 2, 64, 96), (2, 1,
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("what", ["state"])
+@pytest.mark.parametrize("what", ["v", "k", "state", "decay"])
 @pytest.mark.parametrize("shape", range(len(SHAPES)))
 def test_a_bad_row_counts_from_itself_to_the_next_reset(shape, what, value, dtype):
     import torch
