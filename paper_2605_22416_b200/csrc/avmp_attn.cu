@@ -133,6 +133,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUtensorMap map)
 {
     constexpr int KS = D / 16, ND = D / 8;
+    // Weights are relative to this much below the maximum: fp16 has subnormal numbers from 2^-14 down, and tens of thousands of weights of
+    // 2^-25 would be rounded to nothing.
+    constexpr float kBelow = T::kF16 ? 14.f : 0.f;
     extern __shared__ uint8_t smem_raw[];                  // ring (1024-byte rows groups of the swizzle), then the plan
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ unsigned long long bars[2 * kMaxStages], tmp[32];
@@ -291,6 +294,7 @@ drain:
                     n0 = fmaxf(n0, __shfl_xor_sync(0xFFFFFFFFu, n0, i));
                     n1 = fmaxf(n1, __shfl_xor_sync(0xFFFFFFFFu, n1, i));
                 }
+                n0 -= kBelow; n1 -= kBelow;
                 if (__any_sync(0xFFFFFFFFu, n0 > m0 || n1 > m1)) {
                     n0 = fmaxf(n0, m0); n1 = fmaxf(n1, m1);
                     const float f0 = m0 == n0 ? 1.f : exp2_approx(m0 - n0), f1 = m1 == n1 ? 1.f : exp2_approx(m1 - n1);

@@ -8,7 +8,8 @@
 // One CTA per SM, 12 warps: two warpgroups own 128 rows each (a thread is a row: the softmax needs no exchange), a warp each
 // loads K and V slices of pages by tiled copies (the latter the query rows too), one issues the products, one hands out
 // tiles.  While one warpgroup exponentiates, the tensor cores work for the other.  The running maximum m is only moved when
-// it grows by more than 2^8 (P stays inside 16-bit range; sums are 32-bit), so the accumulator is rarely rescaled.
+// it grows by more than 2^8 (sums are 32-bit), so the accumulator is rarely rescaled.  Weights of fp16 are taken times 2^7, to at
+// most 2^15: its subnormal numbers begin at 2^-14, and tens of thousands of weights of 2^-25 would be rounded to nothing.
 //
 // Measured (32 query heads on 8 KV heads of 128, bf16): a prompt of 32 749 tokens 7.2 ms alone (1 220 TFLOP/s), 7.8 ms in a
 // loop, where the card's power limit holds the clock at 1.57 GHz (81 to 84 % of what cuBLAS sustains there).  Long
@@ -193,6 +194,8 @@ struct Smem {
 
 enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_WORK = 31, B_TAKEN = 35, B_QFREE = 39, B_COUNT = 41 };
 constexpr uint32_t kWorks = 4;                // ring of work items
+
+template <class T> constexpr float kLift = T::kF16 ? 7.f : 0.f;         // weights are 2^(score - m + kLift), score - m at most 8
 
 template <class T, int D, bool PREFIX>
 __global__ void __launch_bounds__(kCta, 1)
@@ -513,7 +516,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     fence_async_smem();
                 }
                 // a NaN among the scores makes every weight one
-                const float sub = now != now ? now : top == -INFINITY ? 0.f : -top;
+                const float sub = now != now ? now : top == -INFINITY ? 0.f : kLift<T> - top;
                 const unsigned long long sub2 = pack2(sub, sub);
                 unsigned long long sum0 = 0, sum1 = 0;
                 // weights of 16 tokens at a time, rounded, to the first registers that are free again
@@ -561,7 +564,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 tiles += 1;
                 tc_fence_after();
             }
-            if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top, sum);
+            if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top - kLift<T>, sum);
             if (d.j0 < d.j1) {
                 const float inv = 1.f / sum;
                 // A thread holds a row, and a store of 32 rows costs a cycle each (4000 a tile).  Quads of lanes swap 16-byte units
@@ -602,7 +605,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     __syncwarp();
                 }
                 if (!PREFIX && p.splits == 1 && mine && p.a.lse)
-                    p.a.lse[(unsigned long long)(d.q0 + token) * p.a.q_heads + qh] = top * 0.6931471805599453f + logf(sum);
+                    p.a.lse[(unsigned long long)(d.q0 + token) * p.a.q_heads + qh] = (top - kLift<T>) * 0.6931471805599453f + logf(sum);
                 tc_fence_before();     // the accumulator has been read: the next weights let products overwrite it
             }
         }
