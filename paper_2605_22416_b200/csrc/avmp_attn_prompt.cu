@@ -8,8 +8,9 @@
 // One CTA per SM, 12 warps: two warpgroups own 128 rows each (a thread is a row: the softmax needs no exchange), a warp each
 // loads K and V slices of pages by tiled copies (the latter the query rows too), one issues the products, one hands out
 // tiles.  While one warpgroup exponentiates, the tensor cores work for the other.  The running maximum m is only moved when
-// it grows by more than 2^8 (sums are 32-bit), so the accumulator is rarely rescaled.  Weights of fp16 are taken times 2^7, to at
-// most 2^15: its subnormal numbers begin at 2^-14, and tens of thousands of weights of 2^-25 would be rounded to nothing.
+// it grows by more than 2^8 (sums are 32-bit), so the accumulator is rarely rescaled.  Weights are taken times a power of two that
+// puts them where their type has room: bf16 to at most 1 (a weight of 2^8 times a value of 2^120 would pass 32 bits), fp16 to at most
+// 2^15 (its subnormal numbers begin at 2^-14; tens of thousands of weights of 2^-25 would be rounded to nothing).
 //
 // Measured (32 query heads on 8 KV heads of 128, bf16): a prompt of 32 749 tokens 7.2 ms alone (1 220 TFLOP/s), 7.8 ms in a
 // loop, where the card's power limit holds the clock at 1.57 GHz (81 to 84 % of what cuBLAS sustains there).  Long
@@ -195,7 +196,7 @@ struct Smem {
 enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_WORK = 31, B_TAKEN = 35, B_QFREE = 39, B_COUNT = 41 };
 constexpr uint32_t kWorks = 4;                // ring of work items
 
-template <class T> constexpr float kLift = T::kF16 ? 7.f : 0.f;         // weights are 2^(score - m + kLift), score - m at most 8
+template <class T> constexpr float kLift = T::kF16 ? 7.f : -8.f;         // weights are 2^(score - m + kLift), score - m at most 8
 
 template <class T, int D, bool PREFIX>
 __global__ void __launch_bounds__(kCta, 1)

@@ -75,3 +75,27 @@ def test_many_small_weights_beside_a_large_one(call, dtype):
         assert torch.equal(out[:1].expand_as(out).isfinite(), out.isfinite()) and float((out.double() - want[:1]).abs().max()) < 1e-5
     _close(out[:rows], lse[:rows], want, want_lse, mass, call)
     c.ctx.close()
+
+
+@pytest.mark.gpu
+def test_values_near_the_largest():
+    """A score 7.5 (in log2 units) above those of the tokens before it, with a value of 2^126, in tiles that the running maximum stays
+    behind in: what the output is."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    L, dim, hk, hq = 300, 64, 8, 128              # more tiles than SMs: tokens are not split
+    c = Cache([L], hk, dim, 16, "bfloat16", seed=62)
+    kv = torch.zeros_like(c.rows[0])
+    kv[0, 200, :, 0] = 4.0
+    kv[1] = 1.0
+    kv[1, 200] = 2.0 ** 126
+    c.ctx.scatter_kv(c.layer, _i32([0]), None, 1, kv[0].contiguous(), kv[1].contiguous())
+    desc = B.attn_desc(q_heads=hq, dtype=c.dt, scale=7.5 * math.log(2) / 4)
+    ws, size = c.workspace(desc, 1)
+    q = torch.zeros(L, hq, dim, dtype=c.dt, device="cuda")
+    q[:, :, 0] = 1.0
+    out, lse = torch.zeros(L, hq, dim, dtype=c.dt, device="cuda"), torch.zeros(L, hq, device="cuda")
+    c.ctx.attn_prompt(c.layer, desc, _i32([0]), 1, _i32([0, L]), L, q, out, lse, ws, size)
+    want, want_lse, mass = _exact(q, kv, desc.scale, 0)
+    _close(out, lse, want, want_lse, mass, "prompt")
+    c.ctx.close()
