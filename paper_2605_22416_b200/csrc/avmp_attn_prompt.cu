@@ -516,7 +516,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     }
                     fence_async_smem();
                 }
-                // a NaN among the scores makes every weight one
+                // a NaN among the scores makes the weights NaN (but for those on the multiply-add pipe) and with them the whole row
                 const float sub = now != now ? now : top == -INFINITY ? 0.f : kLift<T> - top;
                 const unsigned long long sub2 = pack2(sub, sub);
                 unsigned long long sum0 = 0, sum1 = 0;

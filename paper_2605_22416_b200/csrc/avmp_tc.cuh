@@ -182,6 +182,12 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // Largest of three; a NaN wins.
 __device__ __forceinline__ float max3_nan(float a, float b, float c)
 {
@@ -190,12 +196,12 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     return r;
 }
 // 2^x of a pair on the multiply-add pipe (the special-function unit gives 4 exponentials a cycle and scheduler).  x is split into an integer n, by adding and taking away 1.5 * 2^23, and |f| <= 1/2;
-// 2^f is a polynomial of degree 4 fitted for least relative error (2.6e-6) on that interval, 2^n is added to the
-// exponent.  x <= 2^6; below -126 the result is 2^-126 or less instead of 0.
+// 2^f is a polynomial of degree 4 fitted for least relative error (2.6e-6) on that interval, 2^n is put together from
+// its exponent.  x <= 2^6; below -126.5 the result is 0 (a masked token's weight, which a large value would make visible otherwise).
 __device__ __forceinline__ float2 exp2_poly2(unsigned long long x)
 {
     float2 t = unpack2(x);
-    t.x = fmaxf(t.x, -126.f); t.y = fmaxf(t.y, -126.f);
+    t.x = fmaxf(t.x, -127.f); t.y = fmaxf(t.y, -127.f);
     const unsigned long long v = pack2(t.x, t.y);
     const unsigned long long n = add2(v, pack2(12582912.f, 12582912.f));
     const unsigned long long f = add2(v, fma2(n, pack2(-1.f, -1.f), pack2(12582912.f, 12582912.f)));
@@ -203,9 +209,8 @@ __device__ __forceinline__ float2 exp2_poly2(unsigned long long x)
     y = fma2(y, f, pack2(2.402474483e-01f, 2.402474483e-01f));
     y = fma2(y, f, pack2(6.931218147e-01f, 6.931218147e-01f));
     y = fma2(y, f, pack2(9.999992614e-01f, 9.999992614e-01f));
-    const float2 m = unpack2(n), z = unpack2(y);
-    return make_float2(__uint_as_float(__float_as_uint(z.x) + (__float_as_uint(m.x) << 23)),
-                       __uint_as_float(__float_as_uint(z.y) + (__float_as_uint(m.y) << 23)));
+    const float2 m = unpack2(n);      // an exponent field of 0 for n = -127
+    return unpack2(mul2(y, pack2(__uint_as_float((__float_as_uint(m.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(m.y) << 23) + 0x3F800000u))));
 }
 
 // The pages as a five-dimensional tensor [slot][layer, K or V][head][token][dim] with boxes of box_tokens x box_heads rows of

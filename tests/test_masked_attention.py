@@ -37,6 +37,101 @@ def _close(out, lse, want, want_lse, size, what, keep=None):
     assert float(((lse.double() - want_lse).abs() - 2.0 ** -20 * want_lse.abs()).max()) <= 2.0 ** -18, f"{what}: log-sum"
 
 
+SHAPES = [
+    # held, new, kv_heads, group, dim, page
+    ([300, 50], [300, 50], 2, 2, 64, 16),
+    ([700], [300], 1, 1, 128, 16),                    # tokens split over the SMs
+    ([300, 33], [300, 33], 8, 16, 64, 32),            # more tiles than SMs
+    ([260, 129], [129, 129], 2, 3, 128, 24),          # groups that do not divide a tile
+    ([90] * 40, [40] * 40, 2, 8, 128, 16),            # a list with a plan of its own
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("value", ["lowest"])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_a_value_counts_for_the_rows_that_see_it_and_no_others(case, value, dtype):
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    held, new, hk, group, dim, page = SHAPES[case]
+    c = Cache(held, hk, dim, page, dtype, seed=40 + case)
+    lowest = torch.finfo(c.dt).min
+    hq, scale, tot = hk * group, dim ** -0.5, sum(new)
+    cu = np.concatenate([[0], np.cumsum(new)])
+    planted = [(0, held[0] - x, i % hk, 5 * i + 1) for i, x in enumerate([1, 2, 17, 40, min(129, held[0] - 3), held[0]])]
+    planted += [(0, held[0] // 16 * 16 - x, x % hk, 30 + x) for x in (9, 10, 25)]           # tokens 7, 6 and 7 of 16
+    planted += [(len(held) - 1, held[-1] // 2, hk - 1, dim - 1)]
+    clean = {r: kv.clone() for r, kv in c.rows.items()}
+    for r, p, h, x in planted:
+        c.rows[r][1, p, h, x] = lowest if value == "lowest" else value
+        clean[r][1, p, h, x] = lowest if value == "lowest" else 0
+    for r in {p[0] for p in planted}:
+        c.ctx.scatter_kv(c.layer, _i32([r]), None, 1, c.rows[r][0].contiguous(), c.rows[r][1].contiguous())
+    q, _ = c.queries(tot, hq)
+    out, lse = torch.zeros(tot, hq, dim, dtype=c.dt, device="cuda"), torch.zeros(tot, hq, device="cuda")
+    desc = B.attn_desc(q_heads=hq, dtype=c.dt, scale=scale)
+    ws, size = c.workspace(desc, len(held))
+    c.ctx.attn_prompt(c.layer, desc, _i32(range(len(held))), len(held), _i32(cu), tot, q, out, lse, ws, size)
+    for r in range(len(held)):
+        a, b = cu[r], cu[r + 1]
+        past = held[r] - new[r]
+        want, want_lse, mass = _exact(q[a:b], clean[r], scale, past)
+        keep = torch.ones(b - a, hq, dim, dtype=torch.bool, device="cuda")
+        if value != "lowest":
+            for s, p, h, x in planted:
+                if s == r:
+                    rows = slice(max(0, p - past), b - a)
+                    heads = slice(h * group, (h + 1) * group)
+                    keep[rows, heads, x] = False
+                    got = out[a:b][rows, heads, x]
+                    assert (got.isnan() if math.isnan(value) else got == value).all(), f"slot {r}, token {p}: not seen"
+        _close(out[a:b], lse[a:b], want, want_lse, mass, f"slot {r}", keep)
+    assert c.ctx.stats()["error_count"] == 0
+    c.ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("call", ["prompt"])
+def test_scores_of_minus_infinity(call, dtype):
+    """Tokens whose score is -inf weigh nothing, wherever they stand; a row that sees no others has no average: NaN, and -inf
+    for its log-sum."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    held, dim, hq, scale = [300, 40, 100, 150], 64, 4, 0.125
+    c = Cache(held, 2, dim, 16, dtype, seed=60)
+    off = {0: (0, 140), 1: (0, 40), 2: (20, 90), 3: (0, 135)}            # slot 1: all of it
+    for r, (a, b) in off.items():
+        c.rows[r][0, a:b, :, 0] = -math.inf
+        c.ctx.scatter_kv(c.layer, _i32([r]), None, 1, c.rows[r][0].contiguous(), c.rows[r][1].contiguous())
+    desc = B.attn_desc(q_heads=hq, dtype=c.dt, scale=scale)
+    ws, size = c.workspace(desc, 4)
+    if call == "prompt":
+        n, cu = 3, [0, 300, 340, 440]
+        parts = [(cu[r], cu[r + 1], c.rows[r], 0) for r in range(3)]
+    else:
+        n = 3
+        parts = [(r, r + 1, torch.cat([c.rows[3], c.rows[r]], 1) if call == "prefix" else c.rows[r], None) for r in range(3)]
+    tot = parts[-1][1]
+    q, _ = c.queries(tot, hq)
+    q[:, :, 0] = 1
+    out, lse = torch.zeros(tot, hq, dim, dtype=c.dt, device="cuda"), torch.zeros(tot, hq, device="cuda")
+    if call == "prompt":
+        c.ctx.attn_prompt(c.layer, desc, _i32(range(3)), 3, _i32(cu), tot, q, out, lse, ws, size)
+    else:
+        c.ctx.attn_decode(c.layer, desc, _i32(range(3)), 3, 3 if call == "prefix" else NONE, q, out, lse, ws, size)
+    for r, (a, b, kv, past) in enumerate(parts):
+        want, want_lse, mass = _exact(q[a:b], kv, scale, kv.shape[1] - 1 if past is None else past)
+        none = want_lse == -math.inf
+        assert (out[a:b][none].isnan()).all() and (lse[a:b][none] == -math.inf).all(), f"slot {r}: rows that see nothing"
+        if (~none).any():
+            _close(out[a:b][~none], lse[a:b][~none], want[~none], want_lse[~none], mass[~none], f"slot {r}")
+    if call != "prefix":
+        assert lse[parts[1][0]:parts[1][1]].isinf().all()
+    c.ctx.close()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("call", ["prompt", "decode", "prefix"])
