@@ -302,10 +302,12 @@ drain:
 #pragma unroll
                     for (int i = 0; i < ND; ++i) { o[i][0] *= f0; o[i][1] *= f0; o[i][2] *= f1; o[i][3] *= f1; }
                 }
+                // a row that has seen nothing but scores of minus infinity so far: their weights are 0, not 2^(-inf + inf)
+                const float s0 = m0 == -INFINITY ? 0.f : m0, s1 = m1 == -INFINITY ? 0.f : m1;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    x[h][0] = exp2_approx(x[h][0] - m0); x[h][1] = exp2_approx(x[h][1] - m0);
-                    x[h][2] = exp2_approx(x[h][2] - m1); x[h][3] = exp2_approx(x[h][3] - m1);
+                    x[h][0] = exp2_approx(x[h][0] - s0); x[h][1] = exp2_approx(x[h][1] - s0);
+                    x[h][2] = exp2_approx(x[h][2] - s1); x[h][3] = exp2_approx(x[h][3] - s1);
                     l0 += x[h][0] + x[h][1]; l1 += x[h][2] + x[h][3];
                 }
                 const uint32_t pa[4] = {T::pack(x[0][0], x[0][1]), T::pack(x[0][2], x[0][3]), T::pack(x[1][0], x[1][1]), T::pack(x[1][2], x[1][3])};

@@ -93,7 +93,7 @@ def test_a_value_counts_for_the_rows_that_see_it_and_no_others(case, value, dtyp
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("call", ["prompt"])
+@pytest.mark.parametrize("call", ["prompt", "decode", "prefix"])
 def test_scores_of_minus_infinity(call, dtype):
     """Tokens whose score is -inf weigh nothing, wherever they stand; a row that sees no others has no average: NaN, and -inf
     for its log-sum."""
