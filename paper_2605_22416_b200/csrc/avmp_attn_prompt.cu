@@ -16,6 +16,10 @@
 // loop, where the card's power limit holds the clock at 1.57 GHz (81 to 84 % of what cuBLAS sustains there).  Long
 // tiles are bound by that; short ones (32 prompts of 32 to 512 tokens: 48 us) by the chain load, S, P, O, store.
 // P is rounded to the 16 bits of V (eps/2 per weight, averaged over the tokens); denominators are summed before that.
+// A weight of zero does not silence a NaN or an infinity in V, so one in a token that some rows of a tile do not see spoils those rows.
+// It shows when they are written out: such tiles are noted and done once more behind the others, with zeros in the place of what is not finite
+// in tokens that some row does not see, and with these values added, from the cache, to the rows that do see them.  (32 short
+// prompts: 48.1 us without, 50.6 so; 55 to 58 with V looked over in every tile beforehand.)
 #include "avmp_tc.cuh"
 
 namespace avmp {
@@ -81,6 +85,28 @@ __global__ void __launch_bounds__(kStepThreads) prompt_plan_kernel(const Geom g,
     if (threadIdx.x == 0) *p.n_tiles = base;
 }
 
+// Adds what is not finite among 16 columns of V, tokens t0 .. t1 of a chain, to a row's sums.  (For the few rows that have such values.)
+template <class T>
+__device__ __forceinline__ void add_not_finite(const Geom &g, const uint32_t *chain, uint32_t t0, uint32_t t1, unsigned long long in_page, uint32_t (&o)[16])
+{
+    for (uint32_t t = t0; t < t1; ++t) {
+        const uint8_t *row = unit_ptr(g, AVMP_POOL_KV, g.VT[0][chain[t / g.T] & 0x7FFFFFFFu]) + in_page + t % g.T * g.row_bytes;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(row + u * 16);
+            const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!T::marked(T::mark(v[i], 0))) continue;
+                const float2 y = T::unpack(v[i]);
+                uint32_t *to = o + u * 8 + i * 2;
+                if (!(fabsf(y.x) < INFINITY)) to[0] = __float_as_uint(__uint_as_float(to[0]) + y.x);
+                if (!(fabsf(y.y) < INFINITY)) to[1] = __float_as_uint(__uint_as_float(to[1]) + y.y);
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- the tiles
 struct Work {
     uint32_t k, head, split, req;
@@ -91,6 +117,7 @@ struct Work {
     uint32_t len;                 // tokens that the tile's last row sees
     uint32_t j0, j1;              // KV rounds
     uint32_t tok0, rem0;          // token and head in group of the tile's first row
+    bool end;                     // with no rows: nothing follows
 };
 
 // The i-th tile of CTA c: the list runs from long tiles to short ones, every other pass over the CTAs backwards.
@@ -116,24 +143,24 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
 }
 
 // One warp hands the CTA's tiles out, a few ahead of the others, through a ring in shared memory.  `give(work)` returns
-// false when the CTA stops.  A work item of 0 rows ends the list.
+// false when the CTA stops; `wanted(n)` tells whether the CTA's n-th tile is to be given.
 //   prefix: row blocks of the whole batch.
 //   up to 32 list entries: a lane per entry; tiles in descending order of their KV rounds over all entries, so that the
 //     long ones start first.  How many row blocks have R rounds or more has a closed form per entry, so the i-th of
 //     that order is found by bisection over R and a sum over the lanes, without a list.
 //   more: the list that prompt_plan_kernel wrote.
-template <bool PREFIX, class Give>
-__device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Give give)
+template <bool PREFIX, class Wanted, class Give>
+__device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Wanted wanted, Give give)
 {
     const uint32_t lane = threadIdx.x % 32, per = p.a.kv_heads * p.splits;
-    Work w = {};
     if (PREFIX) {
         const uint32_t r = p.a.prefix, held = held_tokens(g, r);
         for (uint32_t n = 0, i; (i = nth_tile(n)) < p.prefix_blocks * per; ++n)
-            if (!give(make_work(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
+            if (wanted(n) && !give(make_work(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
     } else if (p.tiles) {
         const uint32_t n_tiles = *(volatile uint32_t *)p.n_tiles;
         for (uint32_t n = 0, i; (i = nth_tile(n)) < n_tiles * per; ++n) {
+            if (!wanted(n)) continue;
             const Tile t = p.tiles[i / per];
             const Item it = p.items[t.k];
             if (!give(make_work(p, t.k, it.req, it.len, it.len - it.nq, it.q0, it.nq * p.group, t.b, i % per / p.splits, i % p.splits, true))) return;
@@ -160,6 +187,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
             return x - past >= nq ? blocks : min(blocks, (x - past) * p.group / kRows);
         };
         for (uint32_t n = 0, i; (i = nth_tile(n)) < all * p.a.kv_heads; ++n) {
+            if (!wanted(n)) continue;
             const uint32_t e = i / p.a.kv_heads;
             uint32_t lo = 1, hi = most + 1;              // count(lo) > e >= count(hi)
             while (lo + 1 < hi) {
@@ -181,7 +209,6 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Giv
                                 __shfl_sync(0xFFFFFFFFu, nq, owner) * p.group, block, i - e * p.a.kv_heads, 0, true))) return;
         }
     }
-    give(w);
 }
 
 template <int D>
@@ -194,7 +221,10 @@ struct Smem {
 };
 
 enum { B_FULL = 0, B_EMPTY = 10, B_Q = 20, B_S = 22, B_P = 24, B_O = 28, B_DONE = 30, B_WORK = 31, B_TAKEN = 35, B_QFREE = 39, B_COUNT = 41 };
+constexpr int kRowsBar = 1, kRowsBarThreads = 288;       // the rows' warps and the one that hands tiles out: all rows are out
 constexpr uint32_t kWorks = 4;                // ring of work items
+constexpr uint32_t kMarks = 8;                // marks of tiles, by their count (the warpgroups are less than kWorks tiles apart)
+constexpr uint32_t kRedo = 2048;              // bits for tiles to be done again (tiles that share a bit are done again together)
 
 template <class T> constexpr float kLift = T::kF16 ? 7.f : -8.f;         // weights are 2^(score - m + kLift), score - m at most 8
 
@@ -209,13 +239,14 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned long long bars_s[B_COUNT];
     __shared__ Work works[kWorks];
-    __shared__ uint32_t tmem_s, gave_up;
+    __shared__ uint32_t tmem_s, gave_up, marks[kMarks], redo[kRedo / 32], any_redo;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem), bars = smem_u32(bars_s);
     const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
     auto bar = [&](uint32_t i) { return bars + 8 * i; };
     if (threadIdx.x == 0) {
-        gave_up = 0;
+        gave_up = any_redo = 0;
+        for (uint32_t i = 0; i < kMarks; ++i) marks[i] = 0;
         for (uint32_t i = 0; i < M::kSlots; ++i) { mbar_init(bar(B_FULL + i), 1); mbar_init(bar(B_EMPTY + i), 1); }
         for (uint32_t t = 0; t < 2; ++t) {
             mbar_init(bar(B_Q + t), p.q_boxes ? 1 : 128); mbar_init(bar(B_QFREE + t), 1); mbar_init(bar(B_S + t), 1); mbar_init(bar(B_O + t), 1);
@@ -228,6 +259,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         if (p.q_boxes) tma_prefetch_map(&q_map);
     }
     if (w == 9) tmem_alloc512(smem_u32(&tmem_s));
+    if (w == 10) for (uint32_t i = lane; i < kRedo / 32; i += 32) redo[i] = 0;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -252,11 +284,15 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 if (!ok) break;
                 const Work &t = works[n % kWorks];
                 const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, head = t.head, token = t.q0 + t.tok0;
+                const bool t_end = t.end;
                 const uint32_t need = min((t.len + 15u) & ~15u, t.held);     // products run over whole steps of 16 tokens
                 const uint32_t *chain = g.r_chain + (unsigned long long)t.req * g.max_pages;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_TAKEN + n % kWorks));
-                if (rows == 0) break;
+                if (rows == 0) {
+                    if (t_end) break;
+                    continue;
+                }
                 const uint32_t part_row = (p.a.layer * 2 + v) * g.T * p.a.kv_heads + head;
                 auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
                     const uint32_t tok = j * kKv + lane * p.box_tokens;
@@ -344,9 +380,10 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     if (!ok) break;
                     const Work &t = works[n % kWorks];
                     const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, len = t.len;
+                    const bool t_end = t.end;
                     mbar_arrive(bar(B_TAKEN + n % kWorks));
-                    if (rows == 0) break;
-                    if (j0 == j1) continue;
+                    if (rows == 0 && t_end) break;
+                    if (rows == 0 || j0 == j1) continue;
                     const bool two = rows > 128;
                     // K of round j is load it + 2 (j - j0), V the one behind it
                     ok = full(it) && mbar_wait_one(bar(B_Q), tiles0++ & 1, &gave_up);
@@ -400,15 +437,24 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
             }
             __syncwarp();
         } else {
-            // ---------------- tiles
+            // ---------------- tiles, then those that are done once more
             uint32_t n = 0;
-            hand_out<PREFIX>(g, p, [&](const Work &t) {
+            auto give = [&](const Work &t) {
                 if (n >= kWorks && !mbar_wait(bar(B_TAKEN + n % kWorks), (n / kWorks - 1) & 1, &gave_up)) return false;
                 if (lane == 0) { works[n % kWorks] = t; mbar_arrive(bar(B_WORK + n % kWorks)); }
                 __syncwarp();
                 n += 1;
                 return true;
-            });
+            };
+            Work none = {};
+            hand_out<PREFIX>(g, p, [](uint32_t) { return true; }, give);
+            if (!PREFIX) {
+                give(none);
+                bar_sync(kRowsBar, kRowsBarThreads);
+                if (*(volatile uint32_t *)&any_redo) hand_out<PREFIX>(g, p, [&](uint32_t i) { return (redo[i % kRedo / 32] >> (i % 32) & 1) != 0; }, give);
+            }
+            none.end = true;
+            give(none);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -451,164 +497,208 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 t = works[n % kWorks];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_TAKEN + n % kWorks));
-                if (t.rows == 0) return false;
+                if (t.rows == 0) { n += 1; return false; }
                 if (m * 128 < t.rows) { n += 1; return true; }
                 it += 2 * (t.j1 - t.j0);
             }
         };
-        bool have = advance();
-        if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
-        while (have && ok) {
-            const uint32_t y = t.rem0 + m * 128 + tid, tok = per_group(y), token = t.tok0 + tok;
-            const bool mine = m * 128 + tid < t.rows;
-            const uint32_t qh = t.head * p.group + y - tok * p.group;
-            float top = -INFINITY, sum = 0.f;
-            // columns of a round up to this one are seen by the row
-            const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
-            for (uint32_t j = t.j0; j < t.j1; ++j, ++rounds) {
-                ok = mbar_wait(bar(B_S + m), rounds & 1, &gave_up);
+        bool again = false;
+        for (;;) {
+            bool have = advance();
+            if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
+            while (have && ok) {
+                const uint32_t y = t.rem0 + m * 128 + tid, tok = per_group(y), token = t.tok0 + tok;
+                const bool mine = m * 128 + tid < t.rows;
+                const uint32_t qh = t.head * p.group + y - tok * p.group;
+                float top = -INFINITY, sum = 0.f;
+                // columns of a round up to this one are seen by the row
+                const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
+                const uint32_t least = t.past + t.tok0 + per_group(t.rem0 + m * 128);      // what the warpgroup's first row sees
+                for (uint32_t j = t.j0; j < t.j1; ++j, ++rounds) {
+                    ok = mbar_wait(bar(B_S + m), rounds & 1, &gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t u[128];
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
+                    tmem_wait_ld();
+                    float *s = reinterpret_cast<float *>(u);
+                    if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
+                        const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
+                    }
+                    float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
+#pragma unroll
+                    for (int c = 4; c < 124; c += 8) {
+                        x0 = max3_nan(x0, s[c], s[c + 1]); x1 = max3_nan(x1, s[c + 2], s[c + 3]);
+                        x2 = max3_nan(x2, s[c + 4], s[c + 5]); x3 = max3_nan(x3, s[c + 6], s[c + 7]);
+                    }
+                    x0 = max3_nan(x0, s[124], s[125]); x1 = max3_nan(x1, s[126], s[127]);
+                    const float now = max3_nan(max3_nan(x0, x1, x2), x3, x3) * sl2;
+                    const bool grow = now > top + 8.f || (top == -INFINITY && now > -INFINITY);
+                    if (__any_sync(0xFFFFFFFFu, grow)) {
+                        const float f = grow ? exp2_approx(top - now) : 1.f;
+                        if (grow) { top = now; sum *= f; }
+                        if (j > t.j0) {
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(o, to + c);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st16(to + c, o);
+                            }
+                        }
+                    }
+                    // Tokens of this round that the products run over; of them those of the chain; of them, once more, those that every row here sees.
+                    const uint32_t rows = min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16), valid = min(t.held - j * kKv, rows);
+                    const uint32_t clear = !again ? valid : min(valid, least >= j * kKv ? least - j * kKv + 1 : 0u);
+                    if (clear < rows) {
+                        // Before this round's weights are announced: V behind the last token of the chain (leftovers of other requests) becomes
+                        // zeros, and the second time so does what is not finite in tokens that some rows do not see.
+                        const uint32_t x = it + 2 * (j - t.j0) + 1;
+                        ok = mbar_wait(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1, &gave_up);
+                        if (!ok) break;
+                        uint8_t *v = smem + M::oRing + (x % M::kSlots) * M::kTile;
+                        for (uint32_t y = tid; y < (rows - clear) * (D / 8); y += 128) {
+                            const uint32_t c = y % (D / 8), r = clear + y / (D / 8);
+                            uint4 *at = reinterpret_cast<uint4 *>(v + (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16);
+                            if (r >= valid) { *at = make_uint4(0, 0, 0, 0); continue; }
+                            const uint4 z = *at;
+                            if (!T::marked(T::mark(z.x, T::mark(z.y, T::mark(z.z, T::mark(z.w, 0)))))) continue;
+                            // The other warpgroup may see this token: it learns from the mark, set before the zero is, that there was something.
+                            *(volatile uint32_t *)&marks[n % kMarks] = n;
+                            __threadfence_block();
+                            *at = make_uint4(T::finite(z.x), T::finite(z.y), T::finite(z.z), T::finite(z.w));
+                        }
+                        fence_async_smem();
+                    }
+                    // a NaN among the scores makes the weights NaN (but for those on the multiply-add pipe) and with them the whole row
+                    const float sub = now != now ? now : top == -INFINITY ? 0.f : kLift<T> - top;
+                    const unsigned long long sub2 = pack2(sub, sub);
+                    unsigned long long sum0 = 0, sum1 = 0;
+                    // weights of 16 tokens at a time, rounded, to the first registers that are free again
+#pragma unroll
+                    for (int c = 0; c < 128; c += 16) {
+                        float2 e[8];
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            const unsigned long long v = fma2(pack2(s[c + 2 * y], s[c + 2 * y + 1]), sl22, sub2);
+                            if (kPoly >> y & 1) e[y] = exp2_poly2(v);
+                            else { const float2 z = unpack2(v); e[y] = make_float2(exp2_approx(z.x), exp2_approx(z.y)); }
+                        }
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) u[c / 2 + y] = T::pack(e[y].x, e[y].y);
+#pragma unroll
+                        for (int y = 0; y < 8; y += 4) {
+                            sum0 = add2(sum0, add2(pack2(e[y].x, e[y].y), pack2(e[y + 1].x, e[y + 1].y)));
+                            sum1 = add2(sum1, add2(pack2(e[y + 2].x, e[y + 2].y), pack2(e[y + 3].x, e[y + 3].y)));
+                        }
+                        if (c == 48) tmem_st32(ts, u);
+                        if (c == kAnnounce) {                    // the store has landed meanwhile
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(bar(B_P + 2 * m));
+                        }
+                    }
+                    tmem_st32(ts + 32, u + 32);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(B_P + 2 * m + 1));
+                    const float2 z = unpack2(add2(sum0, sum1));
+                    sum += z.x + z.y;
+                }
                 if (!ok) break;
-                tc_fence_after();
-                uint32_t u[128];
-#pragma unroll
-                for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
-                tmem_wait_ld();
-                float *s = reinterpret_cast<float *>(u);
-                if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
-                    const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
-#pragma unroll
-                    for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
+                // ---------------- rows out, while the tensor cores start on the next tile
+                const Work d = t;
+                const uint32_t count = n;
+                it += 2 * (d.j1 - d.j0);
+                have = advance();
+                if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
+                const unsigned long long at = (PREFIX || p.splits > 1)
+                    ? ((unsigned long long)d.split * (PREFIX ? p.a.n : p.a.total_q) + d.q0 + token) * p.a.q_heads + qh : 0ull;
+                if (d.j0 < d.j1) {
+                    ok = mbar_wait(bar(B_O + m), tiles & 1, &gave_up);
+                    if (!ok) break;
+                    tiles += 1;
+                    tc_fence_after();
                 }
-                float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
-#pragma unroll
-                for (int c = 4; c < 124; c += 8) {
-                    x0 = max3_nan(x0, s[c], s[c + 1]); x1 = max3_nan(x1, s[c + 2], s[c + 3]);
-                    x2 = max3_nan(x2, s[c + 4], s[c + 5]); x3 = max3_nan(x3, s[c + 6], s[c + 7]);
-                }
-                x0 = max3_nan(x0, s[124], s[125]); x1 = max3_nan(x1, s[126], s[127]);
-                const float now = max3_nan(max3_nan(x0, x1, x2), x3, x3) * sl2;
-                const bool grow = now > top + 8.f || (top == -INFINITY && now > -INFINITY);
-                if (__any_sync(0xFFFFFFFFu, grow)) {
-                    const float f = grow ? exp2_approx(top - now) : 1.f;
-                    if (grow) { top = now; sum *= f; }
-                    if (j > t.j0) {
+                if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top - kLift<T>, sum);
+                if (d.j0 < d.j1) {
+                    const float inv = 1.f / sum;
+                    uint32_t odd = 0;
+                    if (again && *(volatile uint32_t *)&marks[count % kMarks] == count) {
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
                             uint32_t o[16];
                             tmem_ld16(o, to + c);
                             tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            if (mine)                   // tokens behind the tile's first row, of this tile's rounds
+                                add_not_finite<T>(g, g.r_chain + (unsigned long long)d.req * g.max_pages, max(d.past + d.tok0 + 1, d.j0 * kKv), min(sees + 1, d.j1 * kKv),
+                                                  (unsigned long long)(p.a.layer * 2 + 1) * g.T * g.row_bytes + ((unsigned long long)d.head * D + c) * 2, o);
+                            __syncwarp();
                             tmem_st16(to + c, o);
                         }
-                    }
-                }
-                if (t.held - j * kKv < min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16)) {
-                    // V behind the last token of the chain: leftovers of other requests, and a weight of zero does not
-                    // silence a NaN.  Rows up to the next step of 16 become zeros before this round's weights are announced.
-                    const uint32_t x = it + 2 * (j - t.j0) + 1, valid = t.held - j * kKv, rows = (t.len - j * kKv + 15) / 16 * 16;
-                    ok = mbar_wait(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1, &gave_up);
-                    if (!ok) break;
-                    uint8_t *v = smem + M::oRing + (x % M::kSlots) * M::kTile;
-                    for (uint32_t y = tid; y < (rows - valid) * (D / 8); y += 128) {
-                        const uint32_t c = y % (D / 8), r = valid + y / (D / 8);
-                        *reinterpret_cast<uint4 *>(v + (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_smem();
-                }
-                // a NaN among the scores makes the weights NaN (but for those on the multiply-add pipe) and with them the whole row
-                const float sub = now != now ? now : top == -INFINITY ? 0.f : kLift<T> - top;
-                const unsigned long long sub2 = pack2(sub, sub);
-                unsigned long long sum0 = 0, sum1 = 0;
-                // weights of 16 tokens at a time, rounded, to the first registers that are free again
-#pragma unroll
-                for (int c = 0; c < 128; c += 16) {
-                    float2 e[8];
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) {
-                        const unsigned long long v = fma2(pack2(s[c + 2 * y], s[c + 2 * y + 1]), sl22, sub2);
-                        if (kPoly >> y & 1) e[y] = exp2_poly2(v);
-                        else { const float2 z = unpack2(v); e[y] = make_float2(exp2_approx(z.x), exp2_approx(z.y)); }
-                    }
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) u[c / 2 + y] = T::pack(e[y].x, e[y].y);
-#pragma unroll
-                    for (int y = 0; y < 8; y += 4) {
-                        sum0 = add2(sum0, add2(pack2(e[y].x, e[y].y), pack2(e[y + 1].x, e[y + 1].y)));
-                        sum1 = add2(sum1, add2(pack2(e[y + 2].x, e[y + 2].y), pack2(e[y + 3].x, e[y + 3].y)));
-                    }
-                    if (c == 48) tmem_st32(ts, u);
-                    if (c == kAnnounce) {                    // the store has landed meanwhile
                         tmem_wait_st();
-                        tc_fence_before();
-                        mbar_arrive(bar(B_P + 2 * m));
                     }
-                }
-                tmem_st32(ts + 32, u + 32);
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(bar(B_P + 2 * m + 1));
-                const float2 z = unpack2(add2(sum0, sum1));
-                sum += z.x + z.y;
-            }
-            if (!ok) break;
-            // ---------------- rows out, while the tensor cores start on the next tile
-            const Work d = t;
-            it += 2 * (d.j1 - d.j0);
-            have = advance();
-            if (have && t.j0 < t.j1 && !p.q_boxes) { load_q(t); q_there(); }
-            const unsigned long long at = (PREFIX || p.splits > 1)
-                ? ((unsigned long long)d.split * (PREFIX ? p.a.n : p.a.total_q) + d.q0 + token) * p.a.q_heads + qh : 0ull;
-            if (d.j0 < d.j1) {
-                ok = mbar_wait(bar(B_O + m), tiles & 1, &gave_up);
-                if (!ok) break;
-                tiles += 1;
-                tc_fence_after();
-            }
-            if ((PREFIX || p.splits > 1) && mine) p.parts.ml[at] = make_float2(top - kLift<T>, sum);
-            if (d.j0 < d.j1) {
-                const float inv = 1.f / sum;
-                // A thread holds a row, and a store of 32 rows costs a cycle each (4000 a tile).  Quads of lanes swap 16-byte units
-                // first: a store then covers 64 bytes of 8 rows.
-                const bool whole = !PREFIX && p.splits == 1;
-                const unsigned long long mine_at = !mine ? 0ull : whole
-                    ? reinterpret_cast<unsigned long long>(p.a.out + (unsigned long long)(d.q0 + token) * p.a.os + (unsigned long long)qh * D * 2)
-                    : reinterpret_cast<unsigned long long>(p.parts.o + at * D);
-                uint8_t *rows[4];                      // of the quad's four lanes, at this lane's unit; null: no such row
+                    // A thread holds a row, and a store of 32 rows costs a cycle each (4000 a tile).  Quads of lanes swap 16-byte units
+                    // first: a store then covers 64 bytes of 8 rows.
+                    const bool whole = !PREFIX && p.splits == 1;
+                    const unsigned long long mine_at = !mine ? 0ull : whole
+                        ? reinterpret_cast<unsigned long long>(p.a.out + (unsigned long long)(d.q0 + token) * p.a.os + (unsigned long long)qh * D * 2)
+                        : reinterpret_cast<unsigned long long>(p.parts.o + at * D);
+                    uint8_t *rows[4];                      // of the quad's four lanes, at this lane's unit; null: no such row
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const unsigned long long x = __shfl_sync(0xFFFFFFFFu, mine_at, (lane & ~3) + r);
-                    rows[r] = x ? reinterpret_cast<uint8_t *>(x) + (lane & 3) * 16 : nullptr;
-                }
+                    for (int r = 0; r < 4; ++r) {
+                        const unsigned long long x = __shfl_sync(0xFFFFFFFFu, mine_at, (lane & ~3) + r);
+                        rows[r] = x ? reinterpret_cast<uint8_t *>(x) + (lane & 3) * 16 : nullptr;
+                    }
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(o, to + c);
-                    tmem_wait_ld();
-                    if (whole) {
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o, to + c);
+                        tmem_wait_ld();
+                        if (whole) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) o[e / 2] = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                    }
+                            for (int e = 0; e < 32; e += 2) {
+                                o[e / 2] = T::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                                odd = T::mark(o[e / 2], odd);
+                            }
+                        } else if (!PREFIX) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (whole && h) break;
-                        uint32_t v[4][4];              // [word][row]
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) v[k][x] = o[h * 16 + x * 4 + k];
-                            quad_transpose(v[k]);
+                            for (int e = 0; e < 32; ++e) odd |= __float_as_uint(__uint_as_float(o[e]) * 0.f);
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (rows[r]) *reinterpret_cast<uint4 *>(rows[r] + (whole ? c * 2 : (c + h * 16) * 4)) = make_uint4(v[0][r], v[1][r], v[2][r], v[3][r]);
+                        for (int h = 0; h < 2; ++h) {
+                            if (whole && h) break;
+                            uint32_t v[4][4];              // [word][row]
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) v[k][x] = o[h * 16 + x * 4 + k];
+                                quad_transpose(v[k]);
+                            }
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (rows[r]) *reinterpret_cast<uint4 *>(rows[r] + (whole ? c * 2 : (c + h * 16) * 4)) = make_uint4(v[0][r], v[1][r], v[2][r], v[3][r]);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (!PREFIX && !again && mine && T::marked(odd)) {
+                        atomicOr(&redo[(count - 1) % kRedo / 32], 1u << ((count - 1) % 32));
+                        any_redo = 1;
+                    }
+                    if (!PREFIX && p.splits == 1 && mine && p.a.lse)
+                        p.a.lse[(unsigned long long)(d.q0 + token) * p.a.q_heads + qh] = (top - kLift<T>) * 0.6931471805599453f + logf(sum);
+                    tc_fence_before();     // the accumulator has been read: the next weights let products overwrite it
                 }
-                if (!PREFIX && p.splits == 1 && mine && p.a.lse)
-                    p.a.lse[(unsigned long long)(d.q0 + token) * p.a.q_heads + qh] = (top - kLift<T>) * 0.6931471805599453f + logf(sum);
-                tc_fence_before();     // the accumulator has been read: the next weights let products overwrite it
             }
+            if (PREFIX || again) break;
+            bar_sync(kRowsBar, kRowsBarThreads);
+            if (!*(volatile uint32_t *)&any_redo) break;
+            again = true;
         }
         cp_async_wait<0>();
     }

@@ -9,7 +9,8 @@ namespace avmp {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// The two 16-bit types: conversions and the warp product m16n8k16 with 32-bit sums.
+// The two 16-bit types: conversions, a mark that stays zero while both halves of every word are finite (x * 0 + mark: one
+// multiply-add for two numbers), zeros in the place of what is not, and the warp product m16n8k16 with 32-bit sums.
 struct Bf16 {
     static constexpr bool kF16 = false;
     __device__ static float2 unpack(uint32_t v) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&v)); }
@@ -17,6 +18,17 @@ struct Bf16 {
     {
         const __nv_bfloat162 r = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    __device__ static uint32_t mark(uint32_t v, uint32_t so_far)
+    {
+        uint32_t r;
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0u), "r"(so_far));
+        return r;
+    }
+    __device__ static bool marked(uint32_t mark) { return (mark & 0x7FFF7FFFu) != 0; }
+    __device__ static uint32_t finite(uint32_t v)
+    {
+        return ((v & 0x7F80u) == 0x7F80u ? 0u : v & 0xFFFFu) | ((v & 0x7F800000u) == 0x7F800000u ? 0u : v & 0xFFFF0000u);
     }
     __device__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
     {
@@ -32,6 +44,17 @@ struct F16 {
     {
         const __half2 r = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    __device__ static uint32_t mark(uint32_t v, uint32_t so_far)
+    {
+        uint32_t r;
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0u), "r"(so_far));
+        return r;
+    }
+    __device__ static bool marked(uint32_t mark) { return (mark & 0x7FFF7FFFu) != 0; }
+    __device__ static uint32_t finite(uint32_t v)
+    {
+        return ((v & 0x7C00u) == 0x7C00u ? 0u : v & 0xFFFFu) | ((v & 0x7C000000u) == 0x7C000000u ? 0u : v & 0xFFFF0000u);
     }
     __device__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
     {

@@ -44,12 +44,13 @@ SHAPES = [
     ([300, 33], [300, 33], 8, 16, 64, 32),            # more tiles than SMs
     ([260, 129], [129, 129], 2, 3, 128, 24),          # groups that do not divide a tile
     ([90] * 40, [40] * 40, 2, 8, 128, 16),            # a list with a plan of its own
+    ([400] * 20, [350] * 20, 8, 4, 128, 128),         # several tiles an SM
 ]
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("value", ["lowest"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, "lowest"])
 @pytest.mark.parametrize("case", range(len(SHAPES)))
 def test_a_value_counts_for_the_rows_that_see_it_and_no_others(case, value, dtype):
     import torch
