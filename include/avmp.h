@@ -77,7 +77,7 @@ enum {
     AVMP_DEV_BAD_REQUEST = 2,    /* gather / scatter / attn / ssm: request slot out of range or holds nothing,
                                     or a row range that does not fit what it holds */
     AVMP_DEV_OUT_OVERFLOW = 3,   /* gather_kv: rows would pass out_capacity_tokens */
-    AVMP_DEV_TIMEOUT = 4         /* a copy kernel gave up a bounded wait; the output is incomplete */
+    AVMP_DEV_TIMEOUT = 4         /* a kernel gave up a bounded wait; what its call puts out is not to be used */
 };
 
 /* Model shape: what one KV page and one SSM block hold (paper Section 3.1).
@@ -485,6 +485,10 @@ AVMP_API int avmp_session_driver_get_stats(avmp_session_driver *drv, avmp_sessio
 AVMP_API int avmp_session_driver_export(avmp_session_driver *drv, uint32_t *h_state, uint32_t *h_uid, uint32_t *h_len,
                                         uint32_t *h_remaining, uint32_t *h_turn, uint32_t *h_requeued,
                                         uint32_t *h_waiting, void *stream);
+
+/* How long a wait inside the kernels of later avmp_attn_* and avmp_ssm_prompt calls may last before they give up
+ * (AVMP_DEV_TIMEOUT): 2 000 000 000 ns unless set, which is also the most. */
+AVMP_API int avmp_set_wait_limit(avmp_ctx *ctx, uint64_t ns);
 
 /* How many kernels this context has launched so far (host counter). */
 AVMP_API uint64_t avmp_launch_count(const avmp_ctx *ctx);

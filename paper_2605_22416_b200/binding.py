@@ -145,6 +145,7 @@ def _load():
         "avmp_clear_error": (C.c_int, [vp, vp]),
         "avmp_export_tables": (C.c_int, [vp, C.POINTER(avmp_tables), vp]),
         "avmp_import_tables": (C.c_int, [vp, C.POINTER(avmp_tables), vp]),
+        "avmp_set_wait_limit": (C.c_int, [vp, C.c_uint64]),
         "avmp_launch_count": (C.c_uint64, [vp]),
         "avmp_error_string": (C.c_char_p, [C.c_int]),
     }
@@ -439,6 +440,10 @@ def avmp_clear_error(ctx, stream=None):
     _check(lib.avmp_clear_error(ctx, _stream(stream)), "avmp_clear_error")
 
 
+def avmp_set_wait_limit(ctx, ns: int):
+    _check(lib.avmp_set_wait_limit(ctx, ns), "avmp_set_wait_limit")
+
+
 def avmp_launch_count(ctx) -> int:
     return int(lib.avmp_launch_count(ctx))
 
@@ -639,6 +644,9 @@ class Context:
 
     def import_tables(self, tables: dict, stats: dict, stream=None):
         avmp_import_tables(self.handle, self.layout, self.opt, self.spec.n_ssm_layers, tables, stats, stream)
+
+    def set_wait_limit(self, ns: int):
+        avmp_set_wait_limit(self.handle, ns)
 
     def launch_count(self) -> int:
         return avmp_launch_count(self.handle)

@@ -112,6 +112,7 @@ AttnArgs attn_args(const avmp_ctx *c, const avmp_attn_desc *d, uint32_t layer, c
     const uint64_t row = (uint64_t)d->q_heads * c->spec.head_dim * 2;
     a.qs = d->q_stride_bytes ? d->q_stride_bytes : row; a.os = d->out_stride_bytes ? d->out_stride_bytes : row;
     a.ws = static_cast<uint8_t *>(ws);
+    a.wait = c->wait;
     return a;
 }
 
@@ -283,6 +284,7 @@ int avmp_create(avmp_ctx **out, const avmp_model_spec *spec, void *d_arena, uint
     avmp_ctx *c = new (std::nothrow) avmp_ctx();
     if (!c) return AVMP_EINVAL;
     c->spec = *spec; c->opt = o; c->lay = lay; c->B = migration_batch_size; c->launches = 0;
+    (void)avmp_set_wait_limit(c, kWaitLimitNs);
     c->d_workspace = d_workspace; c->workspace_bytes = workspace_bytes;
     int &dev = c->device;
     dev = 0;
@@ -619,7 +621,7 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
     if (total_tokens && !ssm_rows_ok(d_q, d_k, d_v, d_log_decay, d_out)) return AVMP_EINVAL;
     if (total_tokens >= (1u << 31) || (uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
     SsmArgs a = ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out);
-    a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
+    a.cu = d_cu; a.resume = d_resume; a.total = total_tokens; a.wait = c->wait;
     if (const size_t need = avmp_ssm_workspace_bytes(c, desc, n, total_tokens)) {
         if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
         if (workspace_bytes < need) return AVMP_ENOSPC;
@@ -716,6 +718,13 @@ int avmp_import_tables(avmp_ctx *c, const avmp_tables *t, void *stream)
     ok = ok && cudaMemcpyAsync(g.st, &d, sizeof(d), cudaMemcpyHostToDevice, s) == cudaSuccess;
     // the host arrays (and `d`) must outlive the copies
     if (!ok || cudaStreamSynchronize(s) != cudaSuccess) return AVMP_ECUDA;
+    return AVMP_OK;
+}
+
+int avmp_set_wait_limit(avmp_ctx *c, uint64_t ns)
+{
+    if (!c) return AVMP_EINVAL;
+    c->wait = WaitLimit{ns < kWaitLimitNs ? ns : kWaitLimitNs, ns < 1000000u ? 0u : 64u};
     return AVMP_OK;
 }
 

@@ -145,6 +145,8 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
     const uint32_t n = d.a.n;
     const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
     const bool lead = blockIdx.x == 0 && blockIdx.y == 0;
+    const Waits waits{&gave_up, d.a.wait};
+    uint32_t loads = 0;
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kMaxStages, ring = smem_u32(smem);
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -179,7 +181,6 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
 
     if (w == kWarps) {
         // ---- loads: the lanes look up the pages of the next 32 box rows ahead, lane 0 issues
-        uint32_t it = 0;
         const uint32_t per_step = s.shares * boxes;         // box rows per step, <= 32
         uint32_t pk = k;
         for (uint32_t st0 = first; st0 < last;) {
@@ -197,9 +198,11 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
                     tok = t % g.T;
                 }
             }
-            for (uint32_t b = 0; b < batch; ++b, ++it) {
-                const uint32_t stage = it % s.stages, round = it / s.stages;
-                if (round && !mbar_wait(empty0 + 8 * stage, (round - 1) & 1, &gave_up)) goto drain;
+            for (uint32_t b = 0; b < batch; ++b, ++loads) {
+                const uint32_t stage = loads % s.stages, round = loads / s.stages;
+                if (round && !mbar_wait(empty0 + 8 * stage, (round - 1) & 1, waits)) goto stop;
+                // (a warp that gave this stage's copy up has freed the stage too: nothing is copied on top of what is in flight)
+                if (__any_sync(0xFFFFFFFFu, waits.over())) goto stop;
                 const bool mine = lane / per_step == b && slot != kInvalid;
                 const uint32_t live = __popc(__ballot_sync(0xFFFFFFFFu, mine));
                 if (lane == 0) mbar_expect(full0 + 8 * stage, live * box_bytes * (D / 64) * 2);
@@ -218,16 +221,8 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
             st0 += batch;
             if (st0 < last) while (p.cu[pk + 1] <= st0) ++pk;
         }
-drain:
-        if (*(volatile uint32_t *)&gave_up) {      // copies in flight land before this CTA's memory is given away
-            for (uint32_t i = it > s.stages ? it - s.stages : 0; i < it; ++i) {
-                const unsigned long long t0 = global_ns();
-                while (!mbar_try(full0 + 8 * (i % s.stages), (i / s.stages) & 1) && global_ns() - t0 < kWaitLimitNs) {}
-            }
-            if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
-        }
+stop:
         if (behind) asm volatile("griddepcontrol.wait;" ::: "memory");
-        return;
     }
 
     // ---- consumers: one (head, 16 query rows, 16 tokens of a step) each
@@ -243,7 +238,8 @@ drain:
     const uint32_t kt = (lane & 7) + ((lane >> 4) << 3), vt = lane & 15;
     const uint32_t k_off = share * share_bytes + token_off(kt), v_off = share * share_bytes + token_off(vt) + s.stage_bytes / 2;
     uint32_t it = 0;
-    for (uint32_t st = first; st < last;) {
+    bool there = true;
+    for (uint32_t st = w == kWarps ? last : first; st < last;) {
         while (p.cu[k + 1] <= st) ++k;
         const uint32_t begin = p.cu[k], end = p.cu[k + 1], seg_end = min(last, end), len = p.len[k];
         // query rows as the left operand, straight from global memory
@@ -266,9 +262,9 @@ drain:
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         for (uint32_t c = st; c < seg_end; ++c, ++it) {
             const uint32_t stage = it % s.stages;
-            // A copy that never lands is reported by the loading warp and not waited for again: the warps of this CTA keep their
+            // A copy that does not land in time is reported and none is waited for again: the warps of this CTA keep their
             // barriers with each other, and the results are not to be used.
-            mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, &gave_up);
+            if (there) there = mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, waits);
             const uint32_t base = ring + stage * s.stage_bytes;
             const uint32_t t0 = (c - begin) * step_tokens + share * 16;
             if (works && t0 < len) {
@@ -424,6 +420,10 @@ drain:
         }
         d.jobs[blockIdx.x] = job;
     }
+    __syncthreads();
+    if (threadIdx.x == 0 && waits.over()) record_error(g.st, AVMP_DEV_TIMEOUT);
+    if (w == kWarps && waits.over())          // copies in flight land before this CTA's memory is given away
+        for (uint32_t i = loads > s.stages ? loads - s.stages : 0; i < loads; ++i) mbar_land(full0 + 8 * (i % s.stages), (i / s.stages) & 1);
 }
 
 // Joins parts, a warp per (request, query head): weights of 32 parts a time, one per lane, sums of 16 parts in flight.

@@ -239,10 +239,12 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned long long bars_s[B_COUNT];
     __shared__ Work works[kWorks];
-    __shared__ uint32_t tmem_s, gave_up, marks[kMarks], redo[kRedo / 32], any_redo;
+    __shared__ uint32_t tmem_s, gave_up, marks[kMarks], redo[kRedo / 32], any_redo, loads[2];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem), bars = smem_u32(bars_s);
     const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const Waits waits{&gave_up, p.a.wait};
+    uint32_t q_loads[2] = {0, 0};                            // query copies issued (by the warp that loads V)
     auto bar = [&](uint32_t i) { return bars + 8 * i; };
     if (threadIdx.x == 0) {
         gave_up = any_redo = 0;
@@ -277,10 +279,10 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         if (w == 8 || w == 10) {
             // ---------------- loads: K by one warp, V by another.  The lanes look the pages up a round ahead; one thread issues.
             const uint32_t v = w == 8 ? 0 : 1, page_rows = (uint32_t)(g.U[0] / (D * 2));
-            uint32_t it = v, q_tiles[2] = {0, 0};
+            uint32_t it = v;
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
-                ok = mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                ok = mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, waits);
                 if (!ok) break;
                 const Work &t = works[n % kWorks];
                 const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, head = t.head, token = t.q0 + t.tok0;
@@ -305,9 +307,10 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
 #pragma unroll
                     for (uint32_t m = 0; m < 2; ++m) {
                         if (m * 128 >= rows || !ok) continue;
-                        if (q_tiles[m]) ok = mbar_wait(bar(B_QFREE + m), (q_tiles[m] - 1) & 1, &gave_up);
-                        q_tiles[m] += 1;
-                        if (ok && elect_one()) {
+                        if (q_loads[m]) ok = mbar_wait(bar(B_QFREE + m), (q_loads[m] - 1) & 1, waits);
+                        if (!ok) continue;
+                        q_loads[m] += 1;
+                        if (elect_one()) {
                             mbar_expect(bar(B_Q + m), M::kQ);
 #pragma unroll
                             for (int x = 0; x < D / 64; ++x)
@@ -322,7 +325,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
                     uint32_t tok = (j * kKv) % g.T;
                     const uint32_t s = it % M::kSlots, round = it / M::kSlots, full = bar(B_FULL + s);
-                    ok = !round || mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, &gave_up);
+                    ok = !round || mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, waits);
                     if (!ok) break;
                     uint32_t dst = base + M::oRing + s * M::kTile;
                     if (elect_one()) mbar_expect(full, boxes * p.box_tokens * D * 2);
@@ -347,15 +350,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     }
                 }
             }
-            if (*(volatile uint32_t *)&gave_up) {      // copies in flight land before this CTA's memory is given away
-                for (uint32_t x = it > M::kSlots ? (it - M::kSlots + 1) & ~1u | v : v; x < it; x += 2) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1) && global_ns() - t0 < kWaitLimitNs) {}
-                }
-                const unsigned long long t0 = global_ns();      // and so do query rows
-                while (global_ns() - t0 < 1000000ull) {}
-                if (lane == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
-            }
+            if (lane == 0) loads[v] = it;
         } else if (w == 9) {
             // ---------------- products, all by one thread and for the two warpgroups in turn: that keeps them apart, so that one
             // exponentiates while the tensor cores work for the other.  (With a thread for each they fall into step and
@@ -374,9 +369,9 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     }
                     tc_commit(bar(B_S + m));
                 };
-                auto full = [&](uint32_t n) { return mbar_wait_one(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, &gave_up); };
+                auto full = [&](uint32_t n) { return mbar_wait_one(bar(B_FULL + n % M::kSlots), (n / M::kSlots) & 1, waits); };
                 for (uint32_t n = 0; ok; ++n) {
-                    ok = mbar_wait_one(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                    ok = mbar_wait_one(bar(B_WORK + n % kWorks), n / kWorks & 1, waits);
                     if (!ok) break;
                     const Work &t = works[n % kWorks];
                     const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, len = t.len;
@@ -386,13 +381,13 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     if (rows == 0 || j0 == j1) continue;
                     const bool two = rows > 128;
                     // K of round j is load it + 2 (j - j0), V the one behind it
-                    ok = full(it) && mbar_wait_one(bar(B_Q), tiles0++ & 1, &gave_up);
+                    ok = full(it) && mbar_wait_one(bar(B_Q), tiles0++ & 1, waits);
                     if (!ok) break;
                     tc_fence_after();
                     issue_s(0, it % M::kSlots);
                     if (j0 + 1 == j1) tc_commit(bar(B_QFREE));
                     if (two) {
-                        ok = mbar_wait_one(bar(B_Q + 1), tiles1++ & 1, &gave_up);
+                        ok = mbar_wait_one(bar(B_Q + 1), tiles1++ & 1, waits);
                         if (!ok) break;
                         tc_fence_after();
                         issue_s(1, it % M::kSlots);
@@ -409,7 +404,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                             // first the half of the tokens whose weights are written first
 #pragma unroll
                             for (uint32_t h = 0; h < 2; ++h) {
-                                if (!mbar_wait_one(bar(B_P + 2 * m + h), r & 1, &gave_up)) return false;
+                                if (!mbar_wait_one(bar(B_P + 2 * m + h), r & 1, waits)) return false;
                                 tc_fence_after();
 #pragma unroll
                                 for (uint32_t x = h * 4; x < h * 4 + 4; ++x)
@@ -432,15 +427,14 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 }
                 // every product is complete before tensor memory is given back
                 tc_commit(bar(B_DONE));
-                const unsigned long long t0 = global_ns();
-                while (!mbar_try(bar(B_DONE), 0) && global_ns() - t0 < kWaitLimitNs) {}
+                mbar_land(bar(B_DONE), 0);
             }
             __syncwarp();
         } else {
             // ---------------- tiles, then those that are done once more
             uint32_t n = 0;
             auto give = [&](const Work &t) {
-                if (n >= kWorks && !mbar_wait(bar(B_TAKEN + n % kWorks), (n / kWorks - 1) & 1, &gave_up)) return false;
+                if (n >= kWorks && !mbar_wait(bar(B_TAKEN + n % kWorks), (n / kWorks - 1) & 1, waits)) return false;
                 if (lane == 0) { works[n % kWorks] = t; mbar_arrive(bar(B_WORK + n % kWorks)); }
                 __syncwarp();
                 n += 1;
@@ -492,7 +486,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
         // the next tile that has rows for this warpgroup (a short one has none for the second)
         auto advance = [&] {
             for (;; ++n) {
-                ok = ok && mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, &gave_up);
+                ok = ok && mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, waits);
                 if (!ok) return false;
                 t = works[n % kWorks];
                 __syncwarp();
@@ -515,7 +509,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
                 const uint32_t least = t.past + t.tok0 + per_group(t.rem0 + m * 128);      // what the warpgroup's first row sees
                 for (uint32_t j = t.j0; j < t.j1; ++j, ++rounds) {
-                    ok = mbar_wait(bar(B_S + m), rounds & 1, &gave_up);
+                    ok = mbar_wait(bar(B_S + m), rounds & 1, waits);
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t u[128];
@@ -559,7 +553,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         // Before this round's weights are announced: V behind the last token of the chain (leftovers of other requests) becomes
                         // zeros, and the second time so does what is not finite in tokens that some rows do not see.
                         const uint32_t x = it + 2 * (j - t.j0) + 1;
-                        ok = mbar_wait(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1, &gave_up);
+                        ok = mbar_wait(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1, waits);
                         if (!ok) break;
                         uint8_t *v = smem + M::oRing + (x % M::kSlots) * M::kTile;
                         for (uint32_t y = tid; y < (rows - clear) * (D / 8); y += 128) {
@@ -620,7 +614,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 const unsigned long long at = (PREFIX || p.splits > 1)
                     ? ((unsigned long long)d.split * (PREFIX ? p.a.n : p.a.total_q) + d.q0 + token) * p.a.q_heads + qh : 0ull;
                 if (d.j0 < d.j1) {
-                    ok = mbar_wait(bar(B_O + m), tiles & 1, &gave_up);
+                    ok = mbar_wait(bar(B_O + m), tiles & 1, waits);
                     if (!ok) break;
                     tiles += 1;
                     tc_fence_after();
@@ -706,6 +700,16 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
     __syncthreads();
     tc_fence_after();
     if (w == 9) tmem_free512(tmem);
+    if (threadIdx.x == 0 && waits.over()) record_error(g.st, AVMP_DEV_TIMEOUT);
+    if ((w == 8 || w == 10) && waits.over()) {
+        // Copies in flight land before this CTA's memory is given away.  K and V have even and odd numbers; a slot that has been filled
+        // again had got its earlier copy.
+        const uint32_t v = w == 8 ? 0 : 1;
+        for (uint32_t x = loads[v] > 2 * M::kSlots + v ? loads[v] - 2 * M::kSlots : v; x < loads[v]; x += 2)
+            if (x + M::kSlots >= loads[(x + M::kSlots) & 1]) mbar_land(bar(B_FULL + x % M::kSlots), (x / M::kSlots) & 1);
+        for (uint32_t m = 0; m < 2; ++m)
+            if (q_loads[m]) mbar_land(bar(B_Q + m), (q_loads[m] - 1) & 1);
+    }
 }
 
 // Rows of a prompt call whose tokens were split: one warp per (row, query head).

@@ -190,6 +190,14 @@ inline uint32_t kv_pieces_per_page(const avmp_layout &lay, uint32_t page_tokens)
     return 2u * (uint32_t)((part + kStage - 1) / kStage);
 }
 
+// How long a bounded wait of the attention and recurrence kernels may last, and how often it looks, staying a while each time, before it
+// looks at the clock.
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+struct WaitLimit {
+    unsigned long long ns;
+    uint32_t tries;
+};
+
 // Host-side launch wrappers (defined next to their kernels).
 struct Launch {
     cudaStream_t stream;
@@ -224,6 +232,7 @@ struct SsmArgs {
     uint8_t *out;
     unsigned long long qs, ks, vs, gs, os;     // row strides in bytes
     float *ws;                                 // prompts: states and decays of shares of a long prompt
+    WaitLimit wait;
 };
 uint32_t ssm_shares(uint32_t n, uint32_t heads, uint32_t dv, uint32_t total, int n_sms);
 cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l);
@@ -240,6 +249,7 @@ struct AttnArgs {
     float *lse;                                // may be null
     unsigned long long qs, os;                 // row strides in bytes
     uint8_t *ws;
+    WaitLimit wait;
 };
 size_t attn_ws_bytes(const Geom &g, uint32_t n_reqs, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms);
 cudaError_t launch_attn_decode(const Geom &g, const AttnArgs &a, const Launch &l, uint32_t *n_launched);
@@ -261,6 +271,7 @@ struct avmp_ctx {
     int device;
     int sm_khz;          // nominal SM clock, to turn the step kernel's cycle counts into time
     uint64_t launches;
+    avmp::WaitLimit wait;
     // staging for avmp_step_host, inside the workspace
     avmp_op *d_stage_ops;
     uint32_t *d_stage_status;

@@ -299,6 +299,8 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
     const uint32_t grp = head / (a.heads / a.groups);
     const int team = threadIdx.x / 128, tid = threadIdx.x % 128, w = tid / 32, lane = tid % 32;
     const int lr = lane >> 2, lc = (lane & 3) * 2;
+    const Waits waits{&gave_up, a.wait};
+    uint32_t loads = 0;                                    // pieces of this team whose rows have been asked for (first thread)
     uint8_t *stage0 = smem + L::oStage + team * L::kBufs * L::kStage;
     float *F = reinterpret_cast<float *>(smem + L::oF);
     float *decays = reinterpret_cast<float *>(smem + L::oW + team * 2 * L::kW);
@@ -322,7 +324,8 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
     auto load = [&](uint32_t p, int buf) {
         if (p < pieces) {
             const uint32_t base = smem_u32(stage0 + buf * L::kStage), left = len - p * kC, row = row0 + p * kC;
-            if (tid == 0) {
+            if (tid == 0 && !waits.over()) {               // (nothing is copied on top of what may still be in flight)
+                loads += 1;
                 mbar_expect(bars + 8 * buf, kC * (DVT + 2 * DK) * 2);
                 tma_load_tile(base + L::kStageV, &v_map, bars + 8 * buf, head * a.dv + tile * DVT, row);
 #pragma unroll
@@ -463,12 +466,13 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
     constexpr int kTeamBar = 1 + NT;
     int buf = 0;
     uint32_t round = 0;
+    bool there = true;
     for (uint32_t p = team; p < pieces; p += NT, ++round) {
         if (L::kBufs > 1) load(p + (L::kBufs - 1) * NT, (buf + L::kBufs - 1) % L::kBufs);
         uint8_t *st = stage0 + buf * L::kStage;
         const uint32_t sq = smem_u32(st + L::kStageQ), sk = smem_u32(st + L::kStageK), sv = smem_u32(st + L::kStageV);
-        // a copy that never lands is reported and not waited for again; the barriers between the teams are still kept
-        if (!mbar_wait(bars + 8 * buf, round / L::kBufs & 1, &gave_up) && tid == 0) record_error(g.st, AVMP_DEV_TIMEOUT);
+        // a copy that does not land in time is reported and none is waited for again; the barriers between the teams are still kept
+        if (there) there = mbar_wait(bars + 8 * buf, round / L::kBufs & 1, waits);
         if (len - p * kC < kC) {
             // behind the request's last row: zeros, as a weight of zero does not silence a NaN
             constexpr int C = (L::kRowV + 2 * DK * 2) / 16;
@@ -732,11 +736,10 @@ ssm_prompt_kernel(const Geom g, const SsmArgs a, uint32_t tiles, uint32_t shares
         if (L::kBufs == 1) load(p + NT, 0);
     }
     cp_async_wait<0>();
-    if (*(volatile uint32_t *)&gave_up) {
-        // copies in flight land, or have their time, before this CTA's memory is given away
-        const unsigned long long t0 = global_ns();
-        while (global_ns() - t0 < 1000000ull) {}
-    }
+    __syncthreads();
+    if (threadIdx.x == 0 && waits.over()) record_error(g.st, AVMP_DEV_TIMEOUT);
+    if (tid == 0 && waits.over())          // copies in flight land before this CTA's memory is given away
+        for (uint32_t i = loads > (uint32_t)L::kBufs ? loads - L::kBufs : 0; i < loads; ++i) mbar_land(bars + 8 * (i % L::kBufs), i / L::kBufs & 1);
 }
 
 template <class T, int DK>

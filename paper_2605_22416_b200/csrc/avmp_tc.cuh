@@ -9,7 +9,14 @@
 
 namespace avmp {
 
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // after this a wait gives up
+// Bounded waits of a CTA.  A wait that runs out makes all its later waits fail at once, so that every role stops issuing.  Once all
+// roles have stopped, behind a barrier of the whole CTA, the kernel looks at over(): it counts one AVMP_DEV_TIMEOUT, and whoever has
+// copies in flight lets them land (mbar_land) before the CTA's memory is given away.
+struct Waits {
+    volatile uint32_t *gave_up;   // in shared memory
+    WaitLimit limit;
+    __device__ bool over() const { return *gave_up != 0; }
+};
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
 {
@@ -33,34 +40,47 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits until the phase with this parity is complete.  False after kWaitLimitNs, or once `gave_up` is set (which a
-// failed wait does, so that every role of the CTA stops): the caller then issues nothing more and leaves.  Whole warps.
-__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)      // the same without staying
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits until the phase with this parity is complete.  False once the limit has passed, for this wait or an earlier one of the CTA:
+// the caller then issues nothing more.
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, Waits w)
 {
     const unsigned long long t0 = global_ns();
-    while (!mbar_try(bar, parity)) {
-        if (*gave_up) return false;
-        if (global_ns() - t0 > kWaitLimitNs) { *gave_up = 1; return false; }
+    while (!mbar_test(bar, parity)) {
+        if (w.over()) return false;
+        if (global_ns() - t0 >= w.limit.ns) {
+            *w.gave_up = 1;
+            return false;
+        }
     }
     return true;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+// For one thread on its own.
+__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, const Waits &w)
 {
-    bool ok = false;
+    bool ok = mbar_test(bar, parity);
 #pragma unroll 1
-    for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try(bar, parity);
-    if (!ok) ok = mbar_wait_slow(bar, parity, gave_up);
-    __syncwarp();
-    return ok;
+    for (uint32_t i = 0; i < w.limit.tries && !ok; ++i) ok = mbar_try(bar, parity);
+    return ok || mbar_wait_slow(bar, parity, w);
 }
-
-// The same for one thread on its own.
-__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+// For a whole warp; the same answer for all its lanes.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits &w)
 {
-    bool ok = false;
-#pragma unroll 1
-    for (int i = 0; i < 64 && !ok; ++i) ok = mbar_try(bar, parity);
-    return ok || mbar_wait_slow(bar, parity, gave_up);
+    return __all_sync(0xFFFFFFFFu, mbar_wait_one(bar, parity, w));
+}
+// A copy or product in flight is given two seconds to complete, whatever the limit is.
+__device__ __forceinline__ void mbar_land(uint32_t bar, uint32_t parity)
+{
+    const unsigned long long t0 = global_ns();
+    while (!mbar_test(bar, parity) && global_ns() - t0 < kWaitLimitNs) {}
 }
 // One thread of a converged warp (the form the compiler knows as a single issuing thread).
 __device__ __forceinline__ bool elect_one()
