@@ -382,8 +382,9 @@ typedef struct {
     uint64_t q_stride_bytes, k_stride_bytes, v_stride_bytes, decay_stride_bytes, out_stride_bytes;
 } avmp_ssm_desc;
 
-/* Scratch bytes avmp_ssm_prompt needs for these sizes: 0 (its workspace may then be NULL) unless few heads and long
- * prompts would leave SMs idle. */
+/* Scratch bytes that any avmp_ssm_prompt call of up to n_reqs list entries and total_tokens rows needs (under 5 MB; 0 on
+ * invalid arguments).  Only calls whose few heads and long prompts would leave SMs idle use scratch: where this is 0, and for a
+ * call of many requests or heads, the workspace may be NULL. */
 AVMP_API size_t avmp_ssm_workspace_bytes(const avmp_ctx *ctx, const avmp_ssm_desc *desc, uint32_t n_reqs, uint32_t total_tokens);
 
 /* Whole prompts: rows d_cu[k] .. d_cu[k+1] are consecutive tokens of request d_reqs[k]; the state after the last

@@ -149,6 +149,13 @@ bool ssm_rows_ok(const void *q, const void *k, const void *v, const float *decay
     return q && k && v && decay && out && !(((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) && !((uintptr_t)decay & 3);
 }
 
+// Scratch of one call of the recurrence over prompts: a state and a decay for each run of each (request, head, columns).
+size_t ssm_ws_bytes(const avmp_ctx *c, const avmp_ssm_desc *d, uint32_t n, uint32_t total)
+{
+    const uint32_t shares = ssm_shares(n, d->heads, d->dv, total, c->n_sms);
+    return shares < 2 ? 0 : (size_t)n * shares * ((size_t)d->heads * d->dv * d->dk + (size_t)d->heads * (d->dv / 32)) * 4;
+}
+
 // A snapshot is accepted only if the kernels could have produced it: they index the tables
 // without bounds checks, so a table that does not hang together must never reach the device.
 bool tables_consistent(const avmp_ctx *c, const avmp_tables *t)
@@ -606,9 +613,14 @@ int avmp_attn_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, co
 
 size_t avmp_ssm_workspace_bytes(const avmp_ctx *c, const avmp_ssm_desc *desc, uint32_t n, uint32_t total_tokens)
 {
-    if (!c || !ssm_desc_ok(c, desc) || n == 0) return 0;
-    const uint32_t shares = ssm_shares(n, desc->heads, desc->dv, total_tokens, c->n_sms);
-    return shares < 2 ? 0 : (size_t)n * shares * ((size_t)desc->heads * desc->dv * desc->dk + (size_t)desc->heads * (desc->dv / 32)) * 4;
+    if (!c || !ssm_desc_ok(c, desc)) return 0;
+    // Fewer requests are cut into more runs; from n_sms / (3 heads) requests up none is (see ssm_shares).
+    size_t most = 0;
+    for (uint32_t k = 1; k <= n && k <= (uint32_t)c->n_sms; ++k) {
+        const size_t b = ssm_ws_bytes(c, desc, k, total_tokens);
+        if (b > most) most = b;
+    }
+    return most;
 }
 
 int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs, uint32_t n,
@@ -622,9 +634,9 @@ int avmp_ssm_prompt(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, cons
     if (total_tokens >= (1u << 31) || (uint64_t)n * desc->heads * (desc->dv / 32) >= (1ull << 31)) return AVMP_EINVAL;
     SsmArgs a = ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out);
     a.cu = d_cu; a.resume = d_resume; a.total = total_tokens; a.wait = c->wait;
-    if (const size_t need = avmp_ssm_workspace_bytes(c, desc, n, total_tokens)) {
+    if (ssm_ws_bytes(c, desc, n, total_tokens)) {
         if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
-        if (workspace_bytes < need) return AVMP_ENOSPC;
+        if (workspace_bytes < avmp_ssm_workspace_bytes(c, desc, n, total_tokens)) return AVMP_ENOSPC;
         a.ws = static_cast<float *>(d_workspace);
     }
     uint32_t launched = 0;

@@ -161,3 +161,34 @@ def test_states_carried_over_the_runs_of_a_cut_prompt(dtype, heads, dk, dv, lens
         _near(out[a:b], o, mass, f"request {r}")
         _near_state(st[r].view(heads, dv, dk), S, -(-lens[r] // 64), f"state {r}")
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,dk,dv", [(32, 16, 64), (1, 128, 32), (8, 64, 96)])
+def test_a_workspace_for_the_largest_batch_serves_smaller_ones(heads, dk, dv):
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    m, slots = _model(heads, dk, dv, layers=1), 34
+    ctx = _ctx(m, slots, list(range(slots)))
+    desc = B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=torch.bfloat16)
+    most, total = slots, 4000
+    sizes = [[ctx.ssm_workspace_bytes(desc, n, t) for t in (0, 1, 500, 2000, 3999, total)] for n in range(1, most + 1)]
+    assert all(a <= b for row in sizes for a, b in zip(row, row[1:])) and all(a <= b for x, y in zip(sizes, sizes[1:]) for a, b in zip(x, y))
+    size = sizes[-1][-1]
+    assert 0 < size < 5 << 20
+    ws = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(heads)
+    q, k = ((torch.randn(total, 1, dk, device="cuda", generator=gen) * 0.2).to(torch.bfloat16) for _ in range(2))
+    v = torch.randn(total, heads, dv, device="cuda", generator=gen).to(torch.bfloat16)
+    g = -torch.rand(total, heads, device="cuda", generator=gen) * 1e-2
+    for n, tot in ((1, 2500), (2, 4000), (most, total)):
+        cu = np.linspace(0, tot, n + 1).astype(int)
+        out = torch.zeros_like(v)
+        ctx.ssm_prompt(0, desc, _i32(range(n)), n, _i32(cu), tot, None, q, k, v, g, out, ws, size)
+        r = n - 1
+        _, o, mass = _recurrence(torch.zeros(heads, dv, dk, dtype=torch.float64, device="cuda"), *(x[cu[r]:cu[r + 1]] for x in (q, k, v, g)), heads)
+        _near(out[cu[r]:cu[r + 1]], o, mass, f"{n} requests")
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(0, desc, _i32(range(most)), most, _i32(np.linspace(0, total, most + 1).astype(int)), total, None, q, k, v, g, out)      # not cut: no workspace
+    assert (ws[size:] == 0xFF).all() and ctx.stats()["error_count"] == 0
+    ctx.close()
