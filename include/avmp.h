@@ -374,7 +374,7 @@ AVMP_API int avmp_attn_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_att
  * heads * dv * dk):   S <- exp(g) S + v k^T,   out = S q.
  * Rows: q and k [groups][dk], v and out [heads][dv], g (log decay, fp32, at most 0) [heads]; head h
  * reads group h / (heads / groups).  g of -inf clears the state.  Supported: dk 16, 32, 64 or 128, dv a
- * multiple of 32, heads a multiple of groups; else AVMP_EINVAL.  The convolution window of the block is
+ * multiple of 32, heads a multiple of groups, at most 2^31 state elements; else AVMP_EINVAL.  The convolution window of the block is
  * not touched. */
 typedef struct {
     uint32_t type, heads, groups, dk, dv;

@@ -122,6 +122,7 @@ inline bool ssm_desc_ok(const avmp_ctx *c, const avmp_ssm_desc *d)
     if (d->dk != 16 && d->dk != 32 && d->dk != 64 && d->dk != 128) return false;
     if (d->dv == 0 || d->dv % 32 || d->heads == 0 || d->groups == 0 || d->heads % d->groups) return false;
     if ((unsigned __int128)d->heads * d->dv * d->dk != c->spec.ssm_state_elems) return false;
+    if (c->spec.ssm_state_elems > 1u << 31) return false;      // the kernels count a block's elements, and a round beyond the last, in 32 bits
     const uint64_t qk = (uint64_t)d->groups * d->dk * 2, v = (uint64_t)d->heads * d->dv * 2;
     auto stride_ok = [](uint64_t s, uint64_t row, uint64_t unit) { return s == 0 || (s >= row && s % unit == 0 && s < (1ull << 40)); };
     return stride_ok(d->q_stride_bytes, qk, 16) && stride_ok(d->k_stride_bytes, qk, 16) && stride_ok(d->v_stride_bytes, v, 16) &&

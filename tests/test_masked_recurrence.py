@@ -192,3 +192,20 @@ def test_a_workspace_for_the_largest_batch_serves_smaller_ones(heads, dk, dv):
     ctx.ssm_prompt(0, desc, _i32(range(most)), most, _i32(np.linspace(0, total, most + 1).astype(int)), total, None, q, k, v, g, out)      # not cut: no workspace
     assert (ws[size:] == 0xFF).all() and ctx.stats()["error_count"] == 0
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(1 << 22) + 1, (1 << 23) - 1])
+def test_blocks_too_large_to_count_are_refused(heads):
+    """More than 2^31 state elements (no such block fits this pool; the call is refused before it looks)."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    ctx = B.Context(_model(heads, 16, 32), 1 << 20, 0.0, 1, max_requests=2, max_pages=4)
+    desc = B.ssm_desc(heads=heads, groups=1, dk=16, dv=32, dtype=torch.bfloat16)
+    x = torch.zeros(1024, device="cuda")
+    with pytest.raises(B.AvmpError, match="invalid argument"):
+        ctx.ssm_step(0, desc, _i32([0]), 1, x, x, x, x, x)
+    with pytest.raises(B.AvmpError, match="invalid argument"):
+        ctx.ssm_prompt(0, desc, _i32([0]), 1, _i32([0, 1]), 1, None, x, x, x, x, x)
+    assert ctx.ssm_workspace_bytes(desc, 1, 1 << 20) == 0 and ctx.stats()["error_count"] == 0
+    ctx.close()
