@@ -38,7 +38,9 @@ def _near(out, want, size, what):
     import torch
     fin = torch.isfinite(want)
     assert torch.equal(torch.isfinite(out), fin), f"{what}: {int((torch.isfinite(out) != fin).sum())} entries finite or not where they should be"
-    d = ((out.double() - want).abs() - 3.25 * torch.finfo(out.dtype).eps / 2 * size)[fin]
+    # An output below the type's normal range is rounded by half the spacing there, smallest_normal * eps, and not by eps/2 of itself.
+    info = torch.finfo(out.dtype)
+    d = ((out.double() - want).abs() - 3.25 * info.eps / 2 * size - info.smallest_normal * info.eps / 2)[fin]
     assert d.numel() == 0 or float(d.max()) <= 0, f"{what}: {float(d.max()):.3g} too far off"
 
 
@@ -208,4 +210,60 @@ def test_blocks_too_large_to_count_are_refused(heads):
     with pytest.raises(B.AvmpError, match="invalid argument"):
         ctx.ssm_prompt(0, desc, _i32([0]), 1, _i32([0, 1]), 1, None, x, x, x, x, x)
     assert ctx.ssm_workspace_bytes(desc, 1, 1 << 20) == 0 and ctx.stats()["error_count"] == 0
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("heads,dk,dv", [(1, 16, 64), (2, 128, 32)])
+def test_bad_rows_in_a_cut_prompt(heads, dk, dv, value, dtype):
+    """The same over the runs of a long prompt: a bad state in the block, reset in the first run; a bad row in one run, reset in a
+    later one; a bad row that is never reset."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, m, tot = getattr(torch, dtype), _model(heads, dk, dv), 4000
+    ctx = _ctx(m, 2, [0])
+    gen = torch.Generator("cuda").manual_seed(dk)
+    first, conv = _fill_state(ctx, 0, [0], m, gen)
+    first.view(heads, dv, dk)[0, 3, 5] = value
+    ctx.scatter_ssm(0, _i32([0]), 1, first, conv)
+    q, k = ((torch.randn(tot, 1, dk, device="cuda", generator=gen) * 0.2).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) * 1e-3
+    g[[300, 2900]] = -math.inf
+    v[900, heads - 1, 7], v[3300, 0, 20] = value, value
+    desc = B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=dt)
+    size = ctx.ssm_workspace_bytes(desc, 1, tot)
+    assert size > 0
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(0, desc, _i32([0]), 1, _i32([0, tot]), tot, _i32([1]), q, k, v, g, out, torch.empty(size, dtype=torch.uint8, device="cuda"), size)
+    S, o, _ = _recurrence(first.view(heads, dv, dk).double(), q, k, v, g, heads)
+    z = lambda x: torch.nan_to_num(x, 0.0, 0.0, -math.inf if x is g else 0.0)
+    mass = _recurrence(z(first).view(heads, dv, dk).double(), z(q), z(k), z(v), z(g), heads)[2]
+    for a, b in ((0, 300), (300, 900), (900, 2900), (2900, 3300), (3300, tot)):
+        _near(out[a:b], o[a:b], mass[a:b], f"rows {a} to {b}")
+    _near_state(_states(ctx, 0, [0], m)[0].view(heads, dv, dk), S, -(-tot // 64), "state")
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("every", [2, 3, 7])
+def test_many_resets_in_a_piece(every, dtype):
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    heads, dk, dv, tot = 3, 16, 64, 200
+    dt, m = getattr(torch, dtype), _model(heads, dk, dv)
+    ctx = _ctx(m, 2, [0])
+    gen = torch.Generator("cuda").manual_seed(every)
+    q, k = ((torch.randn(tot, 1, dk, device="cuda", generator=gen) * 0.3).to(dt) for _ in range(2))
+    v = torch.randn(tot, heads, dv, device="cuda", generator=gen).to(dt)
+    g = -torch.rand(tot, heads, device="cuda", generator=gen) * 0.5
+    g[::every] = -math.inf
+    out = torch.zeros_like(v)
+    ctx.ssm_prompt(0, B.ssm_desc(heads=heads, groups=1, dk=dk, dv=dv, dtype=dt), _i32([0]), 1, _i32([0, tot]), tot, None, q, k, v, g, out)
+    S, o, mass = _recurrence(torch.zeros(heads, dv, dk, dtype=torch.float64, device="cuda"), q, k, v, g, heads)
+    _near(out, o, mass, "rows")
+    _near_state(_states(ctx, 0, [0], m)[0].view(heads, dv, dk), S, 4, "state")
     ctx.close()
