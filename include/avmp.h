@@ -334,7 +334,13 @@ AVMP_API int avmp_scatter_ssm_layers(avmp_ctx *ctx, uint32_t first_layer, uint32
  * a call needs scratch it takes a caller's buffer, whose content need not be preserved and which two calls
  * may share if they cannot overlap on the GPU.  Calls can be captured into graphs; nothing is read on the host
  * but the arguments.  An item that only the device can see to be wrong (see each call) is skipped, its output
- * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST. */
+ * rows and its state are left as they were, and it counts one AVMP_DEV_BAD_REQUEST.
+ * Numerics: sums, softmax statistics and states are held in 32 bits.  Besides the outputs, these are rounded to the rows' 16 bits:
+ * the softmax weights that multiply V (their denominator is summed before), and in avmp_ssm_prompt the decayed scores and the
+ * carried state where they enter an output (not where they enter the state that is kept).  One in eight of the exponentials of
+ * avmp_attn_prompt and of a shared prefix is a polynomial with a relative error of 2.6e-6.  What a row does not see (later tokens,
+ * tokens in front of a reset, other requests' rows and leftovers of pages) does not reach it, whatever it holds; NaN and
+ * infinities that it does see do.  A row all of whose scores are -inf is NaN, its logarithm -inf. */
 enum { AVMP_TYPE_BF16 = 0, AVMP_TYPE_F16 = 1 };   /* type of input and output rows (and of cached K and V) */
 
 /* q and out rows are [q_heads][head_dim].  Query head h reads KV head h / (q_heads / kv_heads).
@@ -373,7 +379,9 @@ AVMP_API int avmp_attn_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_att
  * elements of the SSM blocks, laid out [heads][dv][dk] in fp32 (ssm_elem_bytes 4, ssm_state_elems =
  * heads * dv * dk):   S <- exp(g) S + v k^T,   out = S q.
  * Rows: q and k [groups][dk], v and out [heads][dv], g (log decay, fp32, at most 0) [heads]; head h
- * reads group h / (heads / groups).  g of -inf clears the state.  Supported: dk 16, 32, 64 or 128, dv a
+ * reads group h / (heads / groups).  g of -inf clears the state, whatever it held; a state that is not finite is also gone once the
+ * decays since then multiply to less than 2^-126.  There is one decay for a head's whole dv x dk elements: layers with a decay of
+ * its own for every channel and state element cannot be expressed.  Supported: dk 16, 32, 64 or 128, dv a
  * multiple of 32, heads a multiple of groups, at most 2^31 state elements; else AVMP_EINVAL.  The convolution window of the block is
  * not touched. */
 typedef struct {

@@ -9,8 +9,8 @@
 // border leaves unnormalised sums, maximum and denominator in the workspace; the joining pass adds the parts in CTA
 // order, so results do not depend on timing.
 //
-// Measured (32 query heads on 8 KV heads of 128, bf16): 1024 chains of 40 to 2400 tokens 409 us (96 % of the measured copy rate),
-// 128 chains, a fifth of 16 to 64 thousand tokens, 611 us (104 %); 32 chains of 48 to 640 tokens 15.6 us, of which the
+// Measured (32 query heads on 8 KV heads of 128, bf16): 1024 chains of 40 to 2400 tokens 408 to 420 us (93 to 96 % of the measured copy
+// rate), 128 chains, a fifth of 16 to 64 thousand tokens, 608 to 624 us (101 to 104 %); 32 chains of 48 to 640 tokens 16 to 19 us, of which the
 // kernel's own beginning (list, pages: four dependent reads) and the second launch are most.
 #include "avmp_tc.cuh"
 

@@ -12,9 +12,9 @@
 // puts them where their type has room: bf16 to at most 1 (a weight of 2^8 times a value of 2^120 would pass 32 bits), fp16 to at most
 // 2^15 (its subnormal numbers begin at 2^-14; tens of thousands of weights of 2^-25 would be rounded to nothing).
 //
-// Measured (32 query heads on 8 KV heads of 128, bf16): a prompt of 32 749 tokens 7.2 ms alone (1 220 TFLOP/s), 7.8 ms in a
-// loop, where the card's power limit holds the clock at 1.57 GHz (81 to 84 % of what cuBLAS sustains there).  Long
-// tiles are bound by that; short ones (32 prompts of 32 to 512 tokens: 48 us) by the chain load, S, P, O, store.
+// Measured (32 query heads on 8 KV heads of 128, bf16): a prompt of 32 749 tokens 7.0 ms alone (1 250 TFLOP/s), 8.0 to 8.1 ms in a
+// loop, where the card's power limit holds the clock near 1.58 GHz (1 090 TFLOP/s, 81 % of what cuBLAS sustains there).  Long
+// tiles are bound by that; short ones (32 prompts of 32 to 512 tokens: 51 us) by the chain load, S, P, O, store.
 // P is rounded to the 16 bits of V (eps/2 per weight, averaged over the tokens); denominators are summed before that.
 // A weight of zero does not silence a NaN or an infinity in V, so one in a token that some rows of a tile do not see spoils those rows.
 // It shows when they are written out: such tiles are noted and done once more behind the others, with zeros in the place of what is not finite

@@ -2,10 +2,12 @@
 //     S_t = exp(g_t) S_{t-1} + v_t k_t^T,   o_t = S_t q_t        (S: [dv][dk], fp32, one per request and head)
 //
 // ssm_step_kernel     one token per request: every state element is read once and written once, bound by HBM (1 GB of state:
-//                     372 us, 91 % of the measured copy rate).
+//                     362 to 382 us, 89 to 94 % of the measured copy rate).
 // ssm_prompt_kernel   whole prompts by pieces of 64 tokens: inside a piece the recurrence is two triangular
-//                     products, between pieces only the state is carried (65 521 tokens of 128 heads, dv 64, dk 16: 875 us,
-//                     2.6 TB/s of rows and state; bound by the latency of four warps per scheduler, not by HBM).
+//                     products, between pieces only the state is carried.  65 521 tokens of 128 heads, dv 64, dk 16: 850 us, 2.7 TB/s
+//                     of rows and state; two thirds of the issue slots and shared memory's cycles are taken, and four warps per scheduler
+//                     leave the rest to latency: not bound by HBM.  65 536 tokens of 64 heads, dv 64, dk 128 (64 CTAs of two
+//                     teams, which wait for each piece's rows): 2 650 us, 15 times what its bytes take.
 #include "avmp_tc.cuh"
 
 #include <type_traits>
@@ -137,7 +139,7 @@ ssm_step_kernel(const Geom g, const SsmArgs a, uint32_t parts, uint32_t part_ele
 // A product takes in rows that count for nothing with a weight of zero, and 0 x NaN and 0 x inf are NaN; the parts of an infinite
 // e^(..) v are inf - inf.  Every row of V and K enters some warp's update, so an update that is not finite shows a piece with such a
 // row: its update and its output rows are then worked out again token by token, as the recurrence is written (walk_state, walk_rows).
-// The look at the updates costs 5 % (the prompt above: 826 us without).
+// The look at the updates costs 3 to 8 % (the two prompts above: 826 and 2 520 us without).
 constexpr int kC = 64;                            // tokens per piece
 
 template <int DK, int DVT, int NT>
@@ -780,9 +782,11 @@ cudaError_t prompt_launch(const Geom &g, const SsmArgs &a, const Launch &l, uint
 template <class T, int DVT>
 cudaError_t prompt_dv(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *launched)
 {
-    // Short keys: two CTAs of two teams on an SM overlap their beginnings and ends (32 prompts of 272 tokens: 36 against 45 us;
-    // 16 of 2048: 394 against 423), one of four teams walks a long prompt faster (65 521 tokens: 823 against 1697).  Only
-    // the mean length is known here.
+    // Short keys: two CTAs of two teams on an SM overlap their beginnings and ends, one of four teams walks a long prompt faster.
+    // us with two and with four, 32 heads: 32 prompts of 272 tokens 45 and 64, of 512 62 and 84, 16 of 1 024 62 and 74, of 2 048 116
+    // and 128, of 8 192 433 and 440, 12 of 8 192 348 and 331; 63 of 100 beside one of 50 000 851 and 666.  Only the mean length is known
+    // here, and a long prompt may hide behind a short mean: from 1 024 on four teams, which gives away up to a sixth where all
+    // are alike; below two, which gives away a fifth where one is long.
     const bool small = a.total / a.n < 1024u && (unsigned long long)a.n * a.heads * (a.dv / DVT) >= 2ull * l.n_sms;
     switch (a.dk) {
     case 16: return small ? prompt_launch<T, 16, DVT, 2>(g, a, l, launched) : prompt_launch<T, 16, DVT, 4>(g, a, l, launched);
@@ -814,8 +818,8 @@ cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l, 
     return a.f16 ? prompt_dv<F16, 32>(g, a, l, launched) : prompt_dv<Bf16, 32>(g, a, l, launched);
 }
 // Runs that each prompt is cut into: as many as leave no SM without one, of 8 pieces or more on the mean; 1 where the first pass
-// would cost more than it gives (it reads keys and values once more).  65 536 tokens of 1 head 58 us against 789 in one run,
-// of 8 heads 93 against 797, of 48 468 against 805; 16 384 tokens of 32 heads of 64 keys 174 against 389.
+// would cost more than it gives (it reads keys and values once more).  65 536 tokens of 1 head 61 us, of 8 heads 97, of 48 495, each
+// about 800 in one run; 16 384 tokens of 32 heads of 64 keys 183 against 390.
 uint32_t ssm_shares(uint32_t n, uint32_t heads, uint32_t dv, uint32_t total, int n_sms)
 {
     const unsigned long long items = (unsigned long long)n * heads * (dv % 64 ? dv / 32 : dv / 64);
