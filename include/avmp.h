@@ -15,8 +15,10 @@
  *   avmp_gather_kv   paged gather of one attention layer into ragged batch buffers;
  *   avmp_gather_ssm  gather of one SSM layer's state blocks into batch buffers;
  *   avmp_scatter_*   the matching write side;
- *   avmp_attn_*      attention over the KV chains where they lie (whole prompts, single tokens);
- *   avmp_ssm_*       the linear recurrence on the SSM blocks where they lie (prompts, single tokens).
+ *   avmp_attn_*      attention over the KV chains where they lie (whole prompts, single tokens, with and without a window);
+ *                    norms, rotation and cache writes of new rows;
+ *   avmp_ssm_*       the linear recurrence on the SSM blocks where they lie (prompts, single tokens);
+ *   avmp_conv_*, avmp_scan_*   short convolution and selective scan on the SSM blocks where they lie.
  *
  * Conventions
  *   - "d_" arguments are DEVICE pointers, "h_" arguments are HOST pointers.
@@ -375,13 +377,52 @@ AVMP_API int avmp_attn_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_att
                               uint32_t n_reqs, uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse,
                               void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* The same two calls through a window: the row at position p sees the tokens j <= p with j > p - window or j < sinks (its own token, the
+ * window - 1 in front of it, and the first `sinks` tokens of the chain).  window >= 1; a window as long as the chain shows all of it.  The
+ * work is that of the tokens that are seen; pages that no row sees are not read, but stay in the chain.  What the calls take, skip and need
+ * as scratch is otherwise as above (there is no shared prefix). */
+AVMP_API int avmp_attn_window_prompt(avmp_ctx *ctx, uint32_t attn_layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks,
+                                     const uint32_t *d_reqs, uint32_t n_reqs, const uint32_t *d_cu_q, uint32_t total_q, const void *d_q,
+                                     void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream);
+AVMP_API int avmp_attn_window_decode(avmp_ctx *ctx, uint32_t attn_layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks,
+                                     const uint32_t *d_reqs, uint32_t n_reqs, const void *d_q, void *d_out, float *d_lse,
+                                     void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* What stands between a projection and attention, in one pass: query and key heads are normalised and rotated, keys and values go to
+ * their pages, queries to d_out.  A head x of head_dim columns becomes
+ *     y = x / sqrt(mean(x^2) + eps) * weight        (weight: fp32 [head_dim], one for queries and one for keys; NULL: y = x),
+ * and its first rotary_dim columns are rotated in pairs (a, b) <- (a cos t - b sin t, b cos t + a sin t) with t = position * freq[i] for
+ * pair i: columns i and i + rotary_dim / 2 (AVMP_ROTATE_HALVES) or 2 i and 2 i + 1 (AVMP_ROTATE_NEIGHBOURS).  Values are copied.
+ * All of it is computed in 32 bits (angles in 64) and rounded once.  d_freq: fp32 [rotary_dim / 2], NULL if that is 0.  Positions are the
+ * tokens' places in their chains, or d_pos (one per row) where that is not NULL, e.g. behind a shared prefix.
+ * Supported: kv_elem_bytes 2, head_dim 64 or 128, rotary_dim a multiple of 8 up to head_dim; else AVMP_EINVAL. */
+enum { AVMP_ROTATE_HALVES = 0, AVMP_ROTATE_NEIGHBOURS = 1 };
+typedef struct {
+    uint32_t type, q_heads, rotary_dim, pairing;
+    float eps;                 /* >= 0 */
+    uint32_t rsvd;             /* 0 */
+    uint64_t q_stride_bytes, k_stride_bytes, v_stride_bytes, out_stride_bytes;
+} avmp_rows_desc;
+
+/* Rows d_cu[k] .. d_cu[k+1] are the LAST tokens of request d_reqs[k]'s chain, which already counts them (avmp_step); their K and V are
+ * written to attention layer attn_layer of its pages.  Skipped items: a slot that holds nothing, a slot that an earlier entry of the
+ * list names, more rows than held tokens, offsets that decrease or pass total_tokens.  n_reqs <= max_requests; total_tokens < 2^31. */
+AVMP_API int avmp_attn_rows_prompt(avmp_ctx *ctx, uint32_t attn_layer, const avmp_rows_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                                   const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_pos, const void *d_q, const void *d_k,
+                                   const void *d_v, const float *d_q_weight, const float *d_k_weight, const float *d_freq, void *d_out,
+                                   void *stream);
+/* One token per request: row k is the last token of d_reqs[k]'s chain.  Skipped items as above. */
+AVMP_API int avmp_attn_rows_step(avmp_ctx *ctx, uint32_t attn_layer, const avmp_rows_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                                 const uint32_t *d_pos, const void *d_q, const void *d_k, const void *d_v, const float *d_q_weight,
+                                 const float *d_k_weight, const float *d_freq, void *d_out, void *stream);
+
 /* Linear attention with a decay for each head (the recurrence of a state-space layer), on the state
  * elements of the SSM blocks, laid out [heads][dv][dk] in fp32 (ssm_elem_bytes 4, ssm_state_elems =
  * heads * dv * dk):   S <- exp(g) S + v k^T,   out = S q.
  * Rows: q and k [groups][dk], v and out [heads][dv], g (log decay, fp32, at most 0) [heads]; head h
  * reads group h / (heads / groups).  g of -inf clears the state, whatever it held; a state that is not finite is also gone once the
- * decays since then multiply to less than 2^-126.  There is one decay for a head's whole dv x dk elements: layers with a decay of
- * its own for every channel and state element cannot be expressed.  Supported: dk 16, 32, 64 or 128, dv a
+ * decays since then multiply to less than 2^-126.  There is one decay for a head's whole dv x dk elements (layers with a decay
+ * of its own for every channel and state element: avmp_scan_prompt and avmp_scan_step).  Supported: dk 16, 32, 64 or 128, dv a
  * multiple of 32, heads a multiple of groups, at most 2^31 state elements; else AVMP_EINVAL.  The convolution window of the block is
  * not touched. */
 typedef struct {
@@ -410,6 +451,54 @@ AVMP_API int avmp_ssm_prompt(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_d
 AVMP_API int avmp_ssm_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_desc *desc, const uint32_t *d_reqs,
                            uint32_t n_reqs, const void *d_q, const void *d_k, const void *d_v, const float *d_log_decay,
                            void *d_out, void *stream);
+
+/* Short causal convolution over a state layer's rows, each channel for itself:
+ *     y_t = bias + sum_j weight[j] x_(t - width + 1 + j),   out_t = y_t, or y_t / (1 + exp(-y_t)) with silu 1.
+ * Rows of x and out: [channels].  weight: fp32 [channels][width], 16-byte aligned; bias: fp32 [channels], 16-byte aligned, or NULL.  The
+ * window elements of the SSM blocks are the last width - 1 rows of a request, oldest first, [width - 1][channels] in fp32.
+ * Supported: ssm_elem_bytes 4, width 2, 3 or 4, channels a multiple of 8, ssm_conv_elems = channels * (width - 1), ssm_state_elems a
+ * multiple of 4; else AVMP_EINVAL.  The state elements of the block are not touched. */
+typedef struct {
+    uint32_t type, channels, width, silu;
+    uint64_t x_stride_bytes, out_stride_bytes;
+} avmp_conv_desc;
+
+/* Whole prompts and single tokens; rows, requests, d_resume (here: whether the window is continued or counts as zeros) and skipped items
+ * as for avmp_ssm_prompt and avmp_ssm_step.  The window after the last row is left in the block. */
+AVMP_API int avmp_conv_prompt(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                              const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume, const void *d_x,
+                              const float *d_weight, const float *d_bias, void *d_out, void *stream);
+AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                            const void *d_x, const float *d_weight, const float *d_bias, void *d_out, void *stream);
+
+/* Selective scan: the recurrence of a state layer whose channels and state elements have a decay each, on the state elements of the SSM
+ * blocks, laid out [channels][states] in fp32:
+ *     step = delta_t + delta_bias, with softplus 1: log(1 + exp(that));
+ *     h <- exp(step * A) h + step * u_t * B_t,   y = <C_t, h> + D * u_t,   out_t = y * z_t / (1 + exp(-z_t)).
+ * Rows: u, delta, z and out [channels], b and c [groups][states]; channel i reads group i / (channels / groups).
+ * A: fp32 [channels][states], 16-byte aligned, finite (at most 0 where steps are positive, or states grow without bound); D and delta_bias: fp32
+ * [channels] or NULL (0); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state.
+ * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups, ssm_state_elems = channels * states; else
+ * AVMP_EINVAL.  The convolution window of the block is not touched. */
+typedef struct {
+    uint32_t type, channels, groups, states, softplus;
+    uint32_t rsvd;             /* 0 */
+    uint64_t u_stride_bytes, delta_stride_bytes, z_stride_bytes, b_stride_bytes, c_stride_bytes, out_stride_bytes;
+} avmp_scan_desc;
+
+/* Scratch bytes that any avmp_scan_prompt call of up to n_reqs list entries and total_tokens rows needs (0 on invalid arguments).  Only calls
+ * whose few channels and long prompts would leave SMs idle use scratch: where this is 0, and for a call of many requests or channels, the
+ * workspace may be NULL. */
+AVMP_API size_t avmp_scan_workspace_bytes(const avmp_ctx *ctx, const avmp_scan_desc *desc, uint32_t n_reqs, uint32_t total_tokens);
+
+/* Whole prompts and single tokens; rows, requests, d_resume and skipped items as for avmp_ssm_prompt and avmp_ssm_step. */
+AVMP_API int avmp_scan_prompt(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_scan_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                              const uint32_t *d_cu, uint32_t total_tokens, const uint32_t *d_resume, const void *d_u, const void *d_delta,
+                              const void *d_b, const void *d_c, const void *d_z, const float *d_a, const float *d_d,
+                              const float *d_delta_bias, void *d_out, void *d_workspace, size_t workspace_bytes, void *stream);
+AVMP_API int avmp_scan_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_scan_desc *desc, const uint32_t *d_reqs, uint32_t n_reqs,
+                            const void *d_u, const void *d_delta, const void *d_b, const void *d_c, const void *d_z, const float *d_a,
+                            const float *d_d, const float *d_delta_bias, void *d_out, void *stream);
 
 /* Counters -> host.  Synchronises the stream. */
 AVMP_API int avmp_get_stats(avmp_ctx *ctx, avmp_stats *h_out, void *stream);

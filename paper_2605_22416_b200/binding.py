@@ -82,6 +82,22 @@ class avmp_ssm_desc(C.Structure):
                                           "out_stride_bytes")]
 
 
+class avmp_rows_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "q_heads", "rotary_dim", "pairing")] + [("eps", C.c_float), ("rsvd", C.c_uint32)] + \
+               [(n, C.c_uint64) for n in ("q_stride_bytes", "k_stride_bytes", "v_stride_bytes", "out_stride_bytes")]
+
+
+class avmp_conv_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "channels", "width", "silu")] + \
+               [(n, C.c_uint64) for n in ("x_stride_bytes", "out_stride_bytes")]
+
+
+class avmp_scan_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("type", "channels", "groups", "states", "softplus", "rsvd")] + \
+               [(n, C.c_uint64) for n in ("u_stride_bytes", "delta_stride_bytes", "z_stride_bytes", "b_stride_bytes", "c_stride_bytes",
+                                          "out_stride_bytes")]
+
+
 _u32p = C.POINTER(C.c_uint32)
 
 
@@ -137,6 +153,17 @@ def _load():
                                        vp, C.c_size_t, vp]),
         "avmp_attn_decode": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_attn_desc), vp, C.c_uint32, C.c_uint32, vp, vp, vp,
                                        vp, C.c_size_t, vp]),
+        "avmp_attn_window_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_attn_desc), C.c_uint32, C.c_uint32, vp, C.c_uint32, vp,
+                                              C.c_uint32, vp, vp, vp, vp, C.c_size_t, vp]),
+        "avmp_attn_window_decode": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_attn_desc), C.c_uint32, C.c_uint32, vp, C.c_uint32, vp, vp,
+                                              vp, vp, C.c_size_t, vp]),
+        "avmp_attn_rows_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_rows_desc), vp, C.c_uint32, vp, C.c_uint32] + [vp] * 9),
+        "avmp_attn_rows_step": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_rows_desc), vp, C.c_uint32] + [vp] * 9),
+        "avmp_conv_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_conv_desc), vp, C.c_uint32, vp, C.c_uint32] + [vp] * 6),
+        "avmp_conv_step": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_conv_desc), vp, C.c_uint32] + [vp] * 5),
+        "avmp_scan_workspace_bytes": (C.c_size_t, [vp, C.POINTER(avmp_scan_desc), C.c_uint32, C.c_uint32]),
+        "avmp_scan_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_scan_desc), vp, C.c_uint32, vp, C.c_uint32] + [vp] * 11 + [C.c_size_t, vp]),
+        "avmp_scan_step": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_scan_desc), vp, C.c_uint32] + [vp] * 10),
         "avmp_ssm_workspace_bytes": (C.c_size_t, [vp, C.POINTER(avmp_ssm_desc), C.c_uint32, C.c_uint32]),
         "avmp_ssm_prompt": (C.c_int, [vp, C.c_uint32, C.POINTER(avmp_ssm_desc), vp, C.c_uint32, vp, C.c_uint32, vp, vp, vp, vp,
                                       vp, vp, vp, C.c_size_t, vp]),
@@ -430,6 +457,80 @@ def avmp_ssm_step(ctx, ssm_layer, desc, d_reqs, n_reqs, d_q, d_k, d_v, d_log_dec
                              _ptr(d_log_decay), _ptr(d_out), _stream(stream)), "avmp_ssm_step")
 
 
+def rows_desc(*, q_heads: int, rotary_dim: int, neighbours: bool, eps: float, dtype: torch.dtype, q_stride_bytes: int = 0,
+              k_stride_bytes: int = 0, v_stride_bytes: int = 0, out_stride_bytes: int = 0) -> avmp_rows_desc:
+    if dtype not in _TYPES:
+        raise AvmpError(f"rows_desc: {dtype} is not bfloat16 or float16")
+    return avmp_rows_desc(_TYPES[dtype], q_heads, rotary_dim, int(neighbours), eps, 0, q_stride_bytes, k_stride_bytes, v_stride_bytes,
+                          out_stride_bytes)
+
+
+def conv_desc(*, channels: int, width: int, silu: bool, dtype: torch.dtype, x_stride_bytes: int = 0, out_stride_bytes: int = 0) -> avmp_conv_desc:
+    if dtype not in _TYPES:
+        raise AvmpError(f"conv_desc: {dtype} is not bfloat16 or float16")
+    return avmp_conv_desc(_TYPES[dtype], channels, width, int(silu), x_stride_bytes, out_stride_bytes)
+
+
+def scan_desc(*, channels: int, groups: int, states: int, softplus: bool, dtype: torch.dtype, u_stride_bytes: int = 0,
+              delta_stride_bytes: int = 0, z_stride_bytes: int = 0, b_stride_bytes: int = 0, c_stride_bytes: int = 0,
+              out_stride_bytes: int = 0) -> avmp_scan_desc:
+    if dtype not in _TYPES:
+        raise AvmpError(f"scan_desc: {dtype} is not bfloat16 or float16")
+    return avmp_scan_desc(_TYPES[dtype], channels, groups, states, int(softplus), 0, u_stride_bytes, delta_stride_bytes, z_stride_bytes,
+                          b_stride_bytes, c_stride_bytes, out_stride_bytes)
+
+
+def avmp_attn_window_prompt(ctx, attn_layer, desc, window, sinks, d_reqs, n_reqs, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace,
+                            workspace_bytes, stream=None):
+    _check(lib.avmp_attn_window_prompt(ctx, attn_layer, C.byref(desc), window, sinks, _ptr(d_reqs), n_reqs, _ptr(d_cu_q), total_q, _ptr(d_q),
+                                       _ptr(d_out), _ptr(d_lse), _ptr(d_workspace), workspace_bytes, _stream(stream)),
+           "avmp_attn_window_prompt")
+
+
+def avmp_attn_window_decode(ctx, attn_layer, desc, window, sinks, d_reqs, n_reqs, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                            stream=None):
+    _check(lib.avmp_attn_window_decode(ctx, attn_layer, C.byref(desc), window, sinks, _ptr(d_reqs), n_reqs, _ptr(d_q), _ptr(d_out),
+                                       _ptr(d_lse), _ptr(d_workspace), workspace_bytes, _stream(stream)), "avmp_attn_window_decode")
+
+
+def avmp_attn_rows_prompt(ctx, attn_layer, desc, d_reqs, n_reqs, d_cu, total_tokens, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq,
+                          d_out, stream=None):
+    _check(lib.avmp_attn_rows_prompt(ctx, attn_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_cu), total_tokens, _ptr(d_pos), _ptr(d_q),
+                                     _ptr(d_k), _ptr(d_v), _ptr(d_q_weight), _ptr(d_k_weight), _ptr(d_freq), _ptr(d_out), _stream(stream)),
+           "avmp_attn_rows_prompt")
+
+
+def avmp_attn_rows_step(ctx, attn_layer, desc, d_reqs, n_reqs, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out, stream=None):
+    _check(lib.avmp_attn_rows_step(ctx, attn_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_pos), _ptr(d_q), _ptr(d_k), _ptr(d_v),
+                                   _ptr(d_q_weight), _ptr(d_k_weight), _ptr(d_freq), _ptr(d_out), _stream(stream)), "avmp_attn_rows_step")
+
+
+def avmp_conv_prompt(ctx, ssm_layer, desc, d_reqs, n_reqs, d_cu, total_tokens, d_resume, d_x, d_weight, d_bias, d_out, stream=None):
+    _check(lib.avmp_conv_prompt(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_cu), total_tokens, _ptr(d_resume), _ptr(d_x),
+                                _ptr(d_weight), _ptr(d_bias), _ptr(d_out), _stream(stream)), "avmp_conv_prompt")
+
+
+def avmp_conv_step(ctx, ssm_layer, desc, d_reqs, n_reqs, d_x, d_weight, d_bias, d_out, stream=None):
+    _check(lib.avmp_conv_step(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_x), _ptr(d_weight), _ptr(d_bias), _ptr(d_out),
+                              _stream(stream)), "avmp_conv_step")
+
+
+def avmp_scan_workspace_bytes(ctx, desc: avmp_scan_desc, n_reqs: int, total_tokens: int) -> int:
+    return lib.avmp_scan_workspace_bytes(ctx, C.byref(desc), n_reqs, total_tokens)
+
+
+def avmp_scan_prompt(ctx, ssm_layer, desc, d_reqs, n_reqs, d_cu, total_tokens, d_resume, d_u, d_delta, d_b, d_c, d_z, d_a, d_d,
+                     d_delta_bias, d_out, d_workspace, workspace_bytes, stream=None):
+    _check(lib.avmp_scan_prompt(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_cu), total_tokens, _ptr(d_resume), _ptr(d_u),
+                                _ptr(d_delta), _ptr(d_b), _ptr(d_c), _ptr(d_z), _ptr(d_a), _ptr(d_d), _ptr(d_delta_bias), _ptr(d_out),
+                                _ptr(d_workspace), workspace_bytes, _stream(stream)), "avmp_scan_prompt")
+
+
+def avmp_scan_step(ctx, ssm_layer, desc, d_reqs, n_reqs, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out, stream=None):
+    _check(lib.avmp_scan_step(ctx, ssm_layer, C.byref(desc), _ptr(d_reqs), n_reqs, _ptr(d_u), _ptr(d_delta), _ptr(d_b), _ptr(d_c), _ptr(d_z),
+                              _ptr(d_a), _ptr(d_d), _ptr(d_delta_bias), _ptr(d_out), _stream(stream)), "avmp_scan_step")
+
+
 def avmp_get_stats(ctx, stream=None) -> dict:
     s = avmp_stats()
     _check(lib.avmp_get_stats(ctx, C.byref(s), _stream(stream)), "avmp_get_stats")
@@ -632,6 +733,40 @@ class Context:
 
     def ssm_step(self, layer, desc, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out, stream=None):
         avmp_ssm_step(self.handle, layer, desc, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out, stream)
+
+    def attn_window_prompt(self, layer, desc, window, sinks, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                           stream=None):
+        avmp_attn_window_prompt(self.handle, layer, desc, window, sinks, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace,
+                                workspace_bytes, stream)
+
+    def attn_window_decode(self, layer, desc, window, sinks, d_reqs, n, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream=None):
+        avmp_attn_window_decode(self.handle, layer, desc, window, sinks, d_reqs, n, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                                stream)
+
+    def attn_rows_prompt(self, layer, desc, d_reqs, n, d_cu, total_tokens, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out,
+                         stream=None):
+        avmp_attn_rows_prompt(self.handle, layer, desc, d_reqs, n, d_cu, total_tokens, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight,
+                              d_freq, d_out, stream)
+
+    def attn_rows_step(self, layer, desc, d_reqs, n, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out, stream=None):
+        avmp_attn_rows_step(self.handle, layer, desc, d_reqs, n, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out, stream)
+
+    def conv_prompt(self, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_x, d_weight, d_bias, d_out, stream=None):
+        avmp_conv_prompt(self.handle, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_x, d_weight, d_bias, d_out, stream)
+
+    def conv_step(self, layer, desc, d_reqs, n, d_x, d_weight, d_bias, d_out, stream=None):
+        avmp_conv_step(self.handle, layer, desc, d_reqs, n, d_x, d_weight, d_bias, d_out, stream)
+
+    def scan_workspace_bytes(self, desc, n, total_tokens) -> int:
+        return avmp_scan_workspace_bytes(self.handle, desc, n, total_tokens)
+
+    def scan_prompt(self, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out,
+                    d_workspace=None, workspace_bytes=0, stream=None):
+        avmp_scan_prompt(self.handle, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_u, d_delta, d_b, d_c, d_z, d_a, d_d,
+                         d_delta_bias, d_out, d_workspace, workspace_bytes, stream)
+
+    def scan_step(self, layer, desc, d_reqs, n, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out, stream=None):
+        avmp_scan_step(self.handle, layer, desc, d_reqs, n, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out, stream)
 
     def stats(self, stream=None) -> dict:
         return avmp_get_stats(self.handle, stream)

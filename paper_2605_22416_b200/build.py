@@ -13,8 +13,9 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libavmp.so"
 SOURCES = ["avmp_api.cu", "avmp_step.cu", "avmp_copy.cu", "avmp_noalloc.cu", "avmp_driver.cu",
            "avmp_sessions.cu", "avmp_ssm.cu", "avmp_attn.cu",
-           "avmp_attn_prompt.cu"]
-HEADERS = [CSRC / "avmp_dev.cuh", CSRC / "avmp_step_body.cuh", CSRC / "avmp_mma.cuh", CSRC / "avmp_tc.cuh", ROOT / "include" / "avmp.h"]
+           "avmp_attn_prompt.cu", "avmp_conv.cu", "avmp_scan.cu", "avmp_rows.cu"]
+HEADERS = [CSRC / "avmp_dev.cuh", CSRC / "avmp_step_body.cuh", CSRC / "avmp_mma.cuh", CSRC / "avmp_tc.cuh", CSRC / "avmp_lists.cuh",
+           ROOT / "include" / "avmp.h"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
               "-cudart", "static", f"-I{ROOT / 'include'}", f"-I{CSRC}"]

@@ -150,11 +150,153 @@ bool ssm_rows_ok(const void *q, const void *k, const void *v, const float *decay
     return q && k && v && decay && out && !(((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) && !((uintptr_t)decay & 3);
 }
 
+inline bool stride_ok(uint64_t s, uint64_t row) { return s == 0 || (s >= row && s % 16 == 0 && s < (1ull << 40)); }
+inline bool off16(const void *p) { return ((uintptr_t)p & 15) != 0; }
+inline bool off4(const void *p) { return ((uintptr_t)p & 3) != 0; }
+
+bool conv_desc_ok(const avmp_ctx *c, const avmp_conv_desc *d)
+{
+    const avmp_model_spec &m = c->spec;
+    if (!d || d->type > AVMP_TYPE_F16 || d->silu > 1 || m.ssm_elem_bytes != 4 || m.n_ssm_layers == 0 || m.ssm_state_elems % 4) return false;
+    if (d->width < 2 || d->width > 4 || d->channels == 0 || d->channels % 8) return false;
+    if ((uint64_t)d->channels * (d->width - 1) != m.ssm_conv_elems) return false;
+    return stride_ok(d->x_stride_bytes, (uint64_t)d->channels * 2) && stride_ok(d->out_stride_bytes, (uint64_t)d->channels * 2);
+}
+
+int conv_call(avmp_ctx *c, uint32_t layer, const avmp_conv_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_cu,
+              uint32_t total, const uint32_t *d_resume, const void *d_x, const float *d_weight, const float *d_bias, void *d_out, void *stream)
+{
+    if (!d_weight || off16(d_weight) || off16(d_bias)) return AVMP_EINVAL;
+    if (total && (!d_x || !d_out || off16(d_x) || off16(d_out))) return AVMP_EINVAL;
+    ConvArgs a = {};
+    a.layer = layer; a.n = n; a.channels = desc->channels; a.width = desc->width; a.total = total; a.state_elems = c->spec.ssm_state_elems;
+    a.f16 = desc->type == AVMP_TYPE_F16; a.act = desc->silu != 0;
+    a.reqs = d_reqs; a.cu = d_cu; a.resume = d_resume;
+    a.x = static_cast<const uint8_t *>(d_x); a.weight = d_weight; a.bias = d_bias; a.out = static_cast<uint8_t *>(d_out);
+    const uint64_t row = (uint64_t)desc->channels * 2;
+    a.xs = desc->x_stride_bytes ? desc->x_stride_bytes : row; a.os = desc->out_stride_bytes ? desc->out_stride_bytes : row;
+    c->launches += 1;
+    return cu(launch_conv(c->g, a, L(c, stream)));
+}
+
+bool scan_desc_ok(const avmp_ctx *c, const avmp_scan_desc *d)
+{
+    const avmp_model_spec &m = c->spec;
+    if (!d || d->type > AVMP_TYPE_F16 || d->softplus > 1 || d->rsvd || m.ssm_elem_bytes != 4 || m.n_ssm_layers == 0) return false;
+    if (d->states != 8 && d->states != 16 && d->states != 32 && d->states != 64) return false;
+    if (d->channels == 0 || d->groups == 0 || d->channels % d->groups || d->channels / d->groups % 8) return false;
+    if ((uint64_t)d->channels * d->states != m.ssm_state_elems) return false;
+    const uint64_t row = (uint64_t)d->channels * 2, bc = (uint64_t)d->groups * d->states * 2;
+    return stride_ok(d->u_stride_bytes, row) && stride_ok(d->delta_stride_bytes, row) && stride_ok(d->z_stride_bytes, row) &&
+           stride_ok(d->out_stride_bytes, row) && stride_ok(d->b_stride_bytes, bc) && stride_ok(d->c_stride_bytes, bc);
+}
+
+// (rows: whether the call has any)
+bool scan_rows_ok(bool rows, const void *u, const void *delta, const void *b, const void *c, const void *z, const float *a, const float *d,
+                  const float *bias, const void *out)
+{
+    if (!a || off16(a) || off4(d) || off4(bias) || off16(z)) return false;
+    return !rows || (u && delta && b && c && out && !(off16(u) || off16(delta) || off16(b) || off16(c) || off16(out)));
+}
+
+ScanArgs scan_args(const avmp_scan_desc *d, uint32_t layer, const uint32_t *reqs, uint32_t n, const void *u, const void *delta, const void *b,
+                   const void *c, const void *z, const float *da, const float *dd, const float *bias, void *out)
+{
+    ScanArgs a = {};
+    a.layer = layer; a.n = n; a.channels = d->channels; a.groups = d->groups; a.states = d->states; a.shares = 1;
+    a.f16 = d->type == AVMP_TYPE_F16; a.softplus = d->softplus != 0;
+    a.reqs = reqs;
+    a.u = static_cast<const uint8_t *>(u); a.d = static_cast<const uint8_t *>(delta); a.b = static_cast<const uint8_t *>(b);
+    a.c = static_cast<const uint8_t *>(c); a.z = static_cast<const uint8_t *>(z);
+    a.a = da; a.skip = dd; a.bias = bias; a.out = static_cast<uint8_t *>(out);
+    const uint64_t row = (uint64_t)d->channels * 2, bc = (uint64_t)d->groups * d->states * 2;
+    a.us = d->u_stride_bytes ? d->u_stride_bytes : row; a.ds = d->delta_stride_bytes ? d->delta_stride_bytes : row;
+    a.zs = d->z_stride_bytes ? d->z_stride_bytes : row; a.os = d->out_stride_bytes ? d->out_stride_bytes : row;
+    a.bs = d->b_stride_bytes ? d->b_stride_bytes : bc; a.cs = d->c_stride_bytes ? d->c_stride_bytes : bc;
+    return a;
+}
+
+// Scratch of one scan over prompts: a state and a sum of steps for each run of each (request, channel).
+size_t scan_ws_bytes(const avmp_ctx *c, const avmp_scan_desc *d, uint32_t n, uint32_t total)
+{
+    const uint32_t shares = scan_shares(n, d->channels, d->groups, total, c->n_sms);
+    return shares < 2 ? 0 : (size_t)n * shares * d->channels * (d->states + 1) * 4;
+}
+
+bool rows_desc_ok(const avmp_ctx *c, const avmp_rows_desc *d)
+{
+    const avmp_model_spec &m = c->spec;
+    if (!d || d->type > AVMP_TYPE_F16 || d->pairing > AVMP_ROTATE_NEIGHBOURS || d->rsvd || !(d->eps >= 0.f) || !std::isfinite(d->eps)) return false;
+    if (m.n_attn_layers == 0 || m.kv_elem_bytes != 2 || (m.head_dim != 64 && m.head_dim != 128) || m.kv_heads == 0 || m.kv_heads > 65535u) return false;
+    if (d->q_heads == 0 || d->q_heads > 65535u || d->rotary_dim > m.head_dim || d->rotary_dim % 8) return false;
+    const uint64_t q = (uint64_t)d->q_heads * m.head_dim * 2, kv = (uint64_t)m.kv_heads * m.head_dim * 2;
+    return stride_ok(d->q_stride_bytes, q) && stride_ok(d->out_stride_bytes, q) && stride_ok(d->k_stride_bytes, kv) && stride_ok(d->v_stride_bytes, kv);
+}
+
+int rows_call(avmp_ctx *c, uint32_t layer, const avmp_rows_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_cu,
+              uint32_t total, const uint32_t *d_pos, const void *d_q, const void *d_k, const void *d_v, const float *d_q_weight,
+              const float *d_k_weight, const float *d_freq, void *d_out, void *stream)
+{
+    if (off4(d_pos) || off4(d_q_weight) || off4(d_k_weight) || off4(d_freq) || (desc->rotary_dim && !d_freq)) return AVMP_EINVAL;
+    if (total && (!d_q || !d_k || !d_v || !d_out || off16(d_q) || off16(d_k) || off16(d_v) || off16(d_out))) return AVMP_EINVAL;
+    const avmp_model_spec &m = c->spec;
+    RowsArgs a = {};
+    a.layer = layer; a.n = n; a.q_heads = desc->q_heads; a.kv_heads = m.kv_heads; a.head_dim = m.head_dim; a.rotary = desc->rotary_dim; a.total = total;
+    a.f16 = desc->type == AVMP_TYPE_F16; a.neighbours = desc->pairing == AVMP_ROTATE_NEIGHBOURS; a.eps = desc->eps;
+    a.reqs = d_reqs; a.cu = d_cu; a.pos = d_pos;
+    a.q = static_cast<const uint8_t *>(d_q); a.k = static_cast<const uint8_t *>(d_k); a.v = static_cast<const uint8_t *>(d_v);
+    a.wq = d_q_weight; a.wk = d_k_weight; a.freq = d_freq; a.out = static_cast<uint8_t *>(d_out);
+    const uint64_t q = (uint64_t)desc->q_heads * m.head_dim * 2, kv = (uint64_t)m.kv_heads * m.head_dim * 2;
+    a.qs = desc->q_stride_bytes ? desc->q_stride_bytes : q; a.os = desc->out_stride_bytes ? desc->out_stride_bytes : q;
+    a.ks = desc->k_stride_bytes ? desc->k_stride_bytes : kv; a.vs = desc->v_stride_bytes ? desc->v_stride_bytes : kv;
+    c->launches += 1;
+    return cu(launch_attn_rows(c->g, a, L(c, stream)));
+}
+
 // Scratch of one call of the recurrence over prompts: a state and a decay for each run of each (request, head, columns).
 size_t ssm_ws_bytes(const avmp_ctx *c, const avmp_ssm_desc *d, uint32_t n, uint32_t total)
 {
     const uint32_t shares = ssm_shares(n, d->heads, d->dv, total, c->n_sms);
     return shares < 2 ? 0 : (size_t)n * shares * ((size_t)d->heads * d->dv * d->dk + (size_t)d->heads * (d->dv / 32)) * 4;
+}
+
+// Attention calls with and without (window 0) a window.
+int attn_prompt_call(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks, const uint32_t *d_reqs, uint32_t n,
+                     const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out, float *d_lse, void *d_workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu_q || (((uintptr_t)d_reqs | (uintptr_t)d_cu_q | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
+    if (total_q && (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15))) return AVMP_EINVAL;
+    if ((uint64_t)total_q * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
+    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
+    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
+    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
+    a.window = window; a.sinks = sinks; a.cu = d_cu_q; a.total_q = total_q;
+    uint32_t launched = 0;
+    const cudaError_t e = launch_attn_prompt(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
+}
+
+int attn_decode_call(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks, const uint32_t *d_reqs, uint32_t n,
+                     uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes,
+                     void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || (((uintptr_t)d_reqs | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
+    if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return AVMP_EINVAL;
+    if ((uint64_t)n * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
+    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
+    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
+    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
+    a.window = window; a.sinks = sinks; a.prefix = prefix_req;
+    uint32_t launched = 0;
+    const cudaError_t e = launch_attn_decode(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
 }
 
 // A snapshot is accepted only if the kernels could have produced it: they index the tables
@@ -578,38 +720,29 @@ int avmp_attn_prompt(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, co
                      const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out, float *d_lse, void *d_workspace,
                      size_t workspace_bytes, void *stream)
 {
-    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
-    if (n == 0) return AVMP_OK;
-    if (!d_reqs || !d_cu_q || (((uintptr_t)d_reqs | (uintptr_t)d_cu_q | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
-    if (total_q && (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15))) return AVMP_EINVAL;
-    if ((uint64_t)total_q * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
-    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
-    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
-    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
-    a.cu = d_cu_q; a.total_q = total_q;
-    uint32_t launched = 0;
-    const cudaError_t e = launch_attn_prompt(c->g, a, L(c, stream), &launched);
-    c->launches += launched;
-    return cu(e);
+    return attn_prompt_call(c, layer, desc, 0, 0, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream);
+}
+
+int avmp_attn_window_prompt(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks, const uint32_t *d_reqs,
+                            uint32_t n, const uint32_t *d_cu_q, uint32_t total_q, const void *d_q, void *d_out, float *d_lse,
+                            void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (window == 0) return AVMP_EINVAL;
+    return attn_prompt_call(c, layer, desc, window, sinks, d_reqs, n, d_cu_q, total_q, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream);
 }
 
 int avmp_attn_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, const uint32_t *d_reqs, uint32_t n,
                      uint32_t prefix_req, const void *d_q, void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes,
                      void *stream)
 {
-    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !attn_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
-    if (n == 0) return AVMP_OK;
-    if (!d_reqs || (((uintptr_t)d_reqs | (uintptr_t)d_lse) & 3)) return AVMP_EINVAL;
-    if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return AVMP_EINVAL;
-    if ((uint64_t)n * desc->q_heads >= (1ull << 31)) return AVMP_EINVAL;
-    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return AVMP_EINVAL;
-    if (workspace_bytes < avmp_attn_workspace_bytes(c, desc, n)) return AVMP_ENOSPC;
-    AttnArgs a = attn_args(c, desc, layer, d_reqs, n, d_q, d_out, d_lse, d_workspace);
-    a.prefix = prefix_req;
-    uint32_t launched = 0;
-    const cudaError_t e = launch_attn_decode(c->g, a, L(c, stream), &launched);
-    c->launches += launched;
-    return cu(e);
+    return attn_decode_call(c, layer, desc, 0, 0, d_reqs, n, prefix_req, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream);
+}
+
+int avmp_attn_window_decode(avmp_ctx *c, uint32_t layer, const avmp_attn_desc *desc, uint32_t window, uint32_t sinks, const uint32_t *d_reqs,
+                            uint32_t n, const void *d_q, void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (window == 0) return AVMP_EINVAL;
+    return attn_decode_call(c, layer, desc, window, sinks, d_reqs, n, AVMP_INVALID, d_q, d_out, d_lse, d_workspace, workspace_bytes, stream);
 }
 
 size_t avmp_ssm_workspace_bytes(const avmp_ctx *c, const avmp_ssm_desc *desc, uint32_t n, uint32_t total_tokens)
@@ -655,6 +788,92 @@ int avmp_ssm_step(avmp_ctx *c, uint32_t layer, const avmp_ssm_desc *desc, const 
     if ((uint64_t)n * ((c->spec.ssm_state_elems + 1023u) / 1024u) >= (1ull << 31)) return AVMP_EINVAL;
     c->launches += 1;
     return cu(launch_ssm_step(c->g, ssm_args(desc, layer, d_reqs, n, d_q, d_k, d_v, d_log_decay, d_out), L(c, stream)));
+}
+
+int avmp_conv_prompt(avmp_ctx *c, uint32_t layer, const avmp_conv_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_cu,
+                     uint32_t total_tokens, const uint32_t *d_resume, const void *d_x, const float *d_weight, const float *d_bias,
+                     void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !conv_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu || off4(d_reqs) || off4(d_cu) || off4(d_resume) || total_tokens >= (1u << 31)) return AVMP_EINVAL;
+    return conv_call(c, layer, desc, d_reqs, n, d_cu, total_tokens, d_resume, d_x, d_weight, d_bias, d_out, stream);
+}
+
+int avmp_conv_step(avmp_ctx *c, uint32_t layer, const avmp_conv_desc *desc, const uint32_t *d_reqs, uint32_t n, const void *d_x,
+                   const float *d_weight, const float *d_bias, void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !conv_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || off4(d_reqs)) return AVMP_EINVAL;
+    return conv_call(c, layer, desc, d_reqs, n, nullptr, n, nullptr, d_x, d_weight, d_bias, d_out, stream);
+}
+
+size_t avmp_scan_workspace_bytes(const avmp_ctx *c, const avmp_scan_desc *desc, uint32_t n, uint32_t total_tokens)
+{
+    if (!c || !scan_desc_ok(c, desc)) return 0;
+    // Fewer requests are cut into more runs; from 2 n_sms requests up none is (see scan_shares).
+    size_t most = 0;
+    for (uint32_t k = 1; k <= n && k <= 2u * (uint32_t)c->n_sms; ++k) {
+        const size_t b = scan_ws_bytes(c, desc, k, total_tokens);
+        if (b > most) most = b;
+    }
+    return most;
+}
+
+int avmp_scan_prompt(avmp_ctx *c, uint32_t layer, const avmp_scan_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_cu,
+                     uint32_t total_tokens, const uint32_t *d_resume, const void *d_u, const void *d_delta, const void *d_b, const void *d_c,
+                     const void *d_z, const float *d_a, const float *d_d, const float *d_delta_bias, void *d_out, void *d_workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !scan_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu || off4(d_reqs) || off4(d_cu) || off4(d_resume) || total_tokens >= (1u << 31)) return AVMP_EINVAL;
+    if (!scan_rows_ok(total_tokens != 0, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out)) return AVMP_EINVAL;
+    if ((uint64_t)n * desc->groups * ((desc->channels / desc->groups + 31) / 32) >= (1ull << 31)) return AVMP_EINVAL;
+    ScanArgs a = scan_args(desc, layer, d_reqs, n, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out);
+    a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
+    if (scan_ws_bytes(c, desc, n, total_tokens)) {
+        if (!d_workspace || off16(d_workspace)) return AVMP_EINVAL;
+        if (workspace_bytes < avmp_scan_workspace_bytes(c, desc, n, total_tokens)) return AVMP_ENOSPC;
+        a.ws = static_cast<float *>(d_workspace);
+        a.shares = scan_shares(n, desc->channels, desc->groups, total_tokens, c->n_sms);
+    }
+    uint32_t launched = 0;
+    const cudaError_t e = launch_scan_prompt(c->g, a, L(c, stream), &launched);
+    c->launches += launched;
+    return cu(e);
+}
+
+int avmp_scan_step(avmp_ctx *c, uint32_t layer, const avmp_scan_desc *desc, const uint32_t *d_reqs, uint32_t n, const void *d_u,
+                   const void *d_delta, const void *d_b, const void *d_c, const void *d_z, const float *d_a, const float *d_d,
+                   const float *d_delta_bias, void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_ssm_layers || n > c->opt.max_requests || !scan_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || off4(d_reqs) || !scan_rows_ok(true, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out)) return AVMP_EINVAL;
+    c->launches += 1;
+    return cu(launch_scan_step(c->g, scan_args(desc, layer, d_reqs, n, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out), L(c, stream)));
+}
+
+int avmp_attn_rows_prompt(avmp_ctx *c, uint32_t layer, const avmp_rows_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_cu,
+                          uint32_t total_tokens, const uint32_t *d_pos, const void *d_q, const void *d_k, const void *d_v,
+                          const float *d_q_weight, const float *d_k_weight, const float *d_freq, void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !rows_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || !d_cu || off4(d_reqs) || off4(d_cu) || total_tokens >= (1u << 31)) return AVMP_EINVAL;
+    return rows_call(c, layer, desc, d_reqs, n, d_cu, total_tokens, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out, stream);
+}
+
+int avmp_attn_rows_step(avmp_ctx *c, uint32_t layer, const avmp_rows_desc *desc, const uint32_t *d_reqs, uint32_t n, const uint32_t *d_pos,
+                        const void *d_q, const void *d_k, const void *d_v, const float *d_q_weight, const float *d_k_weight,
+                        const float *d_freq, void *d_out, void *stream)
+{
+    if (!c || layer >= c->spec.n_attn_layers || n > c->opt.max_requests || !rows_desc_ok(c, desc) || !device_ok(c)) return AVMP_EINVAL;
+    if (n == 0) return AVMP_OK;
+    if (!d_reqs || off4(d_reqs)) return AVMP_EINVAL;
+    return rows_call(c, layer, desc, d_reqs, n, nullptr, n, d_pos, d_q, d_k, d_v, d_q_weight, d_k_weight, d_freq, d_out, stream);
 }
 
 int avmp_get_stats(avmp_ctx *c, avmp_stats *h_out, void *stream)

@@ -94,6 +94,25 @@ struct DecodeArgs {
     uint32_t pre_parts;
 };
 
+// What the one row of a chain of `len` tokens sees through a window, in steps: `lead` steps with sinks, then, `skip` steps further on,
+// those from the window's first token.  Every one of them has a token that is seen.
+struct Sight {
+    uint32_t low, lead, skip;      // low: the window's first token
+    __device__ Sight(const AttnArgs &a, uint32_t len, uint32_t step)
+    {
+        low = len > a.window ? len - a.window : 0u;
+        lead = (min(a.sinks, low) + step - 1) / step;
+        skip = low / step > lead ? low / step - lead : 0u;
+    }
+    __device__ uint32_t at(uint32_t i) const { return i < lead ? i : i + skip; }
+};
+template <bool WINDOW>
+__device__ __forceinline__ uint32_t steps_of(const AttnArgs &a, uint32_t len, uint32_t step)
+{
+    const uint32_t all = (len + step - 1) / step;
+    return WINDOW ? all - Sight(a, len, step).skip : all;
+}
+
 // CTAs that have work: at least one step each, so that every part that is read has been written.
 __device__ __forceinline__ uint32_t busy_ctas(const Split &s, unsigned long long total)
 {
@@ -101,6 +120,7 @@ __device__ __forceinline__ uint32_t busy_ctas(const Split &s, unsigned long long
 }
 
 // The step list, by the whole CTA.  Bad entries own no step.
+template <bool WINDOW>
 __device__ __forceinline__ void make_plan(const Geom &g, const DecodeArgs &d, const Plan &to, unsigned long long *tmp, bool lead)
 {
     const uint32_t n = d.a.n, step = 16 * d.s.shares;
@@ -111,24 +131,25 @@ __device__ __forceinline__ void make_plan(const Geom &g, const DecodeArgs &d, co
         const uint32_t r = __ldcg(d.a.reqs + k), own = held_tokens(g, r), len = dead ? 0u : own;
         if (lead && len == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
         to.req[k] = r; to.len[k] = len;
-        mine += (len + step - 1) / step;
+        mine += steps_of<WINDOW>(d.a, len, step);
     }
     unsigned long long run = block_incl_scan(mine, tmp, &tot) - mine;
     for (uint32_t k = k0; k < k1; ++k) {
         to.cu[k] = (uint32_t)run;
-        run += (to.len[k] + step - 1) / step;
+        run += steps_of<WINDOW>(d.a, to.len[k], step);
     }
     if (threadIdx.x == 0) to.cu[n] = (uint32_t)tot;
 }
 
+template <bool WINDOW>
 __global__ void __launch_bounds__(kStepThreads) attn_plan_kernel(const Geom g, const DecodeArgs d)
 {
     __shared__ unsigned long long tmp[32];
     pdl_prologue();
-    make_plan(g, d, d.ws, tmp, true);
+    make_plan<WINDOW>(g, d, d.ws, tmp, true);
 }
 
-template <class T, int D>
+template <class T, int D, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUtensorMap map)
 {
@@ -162,7 +183,7 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
     if (n <= kLocalPlanMax) {
         p.cu = reinterpret_cast<uint32_t *>(smem + s.stages * s.stage_bytes);
         p.req = p.cu + n + 1; p.len = p.req + n;
-        make_plan(g, d, p, tmp, lead);
+        make_plan<WINDOW>(g, d, p, tmp, lead);
     }
     __syncthreads();
     if (n <= kLocalPlanMax && lead) {       // the joining pass reads it
@@ -191,7 +212,9 @@ attn_decode_kernel(const Geom g, const DecodeArgs d, const __grid_constant__ CUt
                 const uint32_t st = st0 + lane / per_step;
                 uint32_t kk = pk;
                 while (p.cu[kk + 1] <= st) ++kk;
-                const uint32_t t = (st - p.cu[kk]) * step_tokens + (lane % per_step) * s.box_tokens;
+                uint32_t i = st - p.cu[kk];
+                if (WINDOW) i = Sight(d.a, p.len[kk], step_tokens).at(i);
+                const uint32_t t = i * step_tokens + (lane % per_step) * s.box_tokens;
                 if (t < p.len[kk]) {
                     const uint32_t h = __ldcg(g.r_chain + ((unsigned long long)p.req[kk] * g.max_pages + t / g.T));
                     slot = __ldcg(g.VT[0] + (h & 0x7FFFFFFFu));
@@ -260,15 +283,19 @@ stop:
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[x][i] = 0.f;
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        const Sight sight(d.a, WINDOW ? len : 0u, step_tokens);
         for (uint32_t c = st; c < seg_end; ++c, ++it) {
             const uint32_t stage = it % s.stages;
             // A copy that does not land in time is reported and none is waited for again: the warps of this CTA keep their
             // barriers with each other, and the results are not to be used.
             if (there) there = mbar_wait(full0 + 8 * stage, (it / s.stages) & 1, waits);
             const uint32_t base = ring + stage * s.stage_bytes;
-            const uint32_t t0 = (c - begin) * step_tokens + share * 16;
+            const uint32_t t0 = (WINDOW ? sight.at(c - begin) : c - begin) * step_tokens + share * 16;
             if (works && t0 < len) {
                 const uint32_t valid = len - t0;
+                // of these 16 tokens: the first that the window shows, and how many are sinks
+                const uint32_t low = sight.low > t0 ? sight.low - t0 : 0u, sinks = d.a.sinks > t0 ? d.a.sinks - t0 : 0u;
+                auto seen = [&](uint32_t t) { return t < valid && (!WINDOW || t >= low || t < sinks); };
                 float x[2][4] = {};
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
@@ -282,7 +309,7 @@ stop:
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[h][i] = (uint32_t)(h * 8 + lc + (i & 1)) < valid ? x[h][i] * sl2 : -INFINITY;
+                    for (int i = 0; i < 4; ++i) x[h][i] = seen(h * 8 + lc + (i & 1)) ? x[h][i] * sl2 : -INFINITY;
                 float n0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
                 float n1 = fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3]));
 #pragma unroll
@@ -308,8 +335,8 @@ stop:
                 }
                 const uint32_t pa[4] = {T::pack(x[0][0], x[0][1]), T::pack(x[0][2], x[0][3]), T::pack(x[1][0], x[1][1]), T::pack(x[1][2], x[1][3])};
                 // a weight of zero does not silence a NaN: leftover rows of V count as zeros
-                const uint32_t keep0 = (lc < valid ? 0xFFFFu : 0u) | (lc + 1 < valid ? 0xFFFF0000u : 0u);
-                const uint32_t keep1 = (lc + 8 < valid ? 0xFFFFu : 0u) | (lc + 9 < valid ? 0xFFFF0000u : 0u);
+                const uint32_t keep0 = (seen(lc) ? 0xFFFFu : 0u) | (seen(lc + 1) ? 0xFFFF0000u : 0u);
+                const uint32_t keep1 = (seen(lc + 8) ? 0xFFFFu : 0u) | (seen(lc + 9) ? 0xFFFF0000u : 0u);
 #pragma unroll
                 for (int i = 0; i < ND / 2; ++i) {
                     const uint32_t ch = i * 2 + (lane >> 4);
@@ -511,25 +538,32 @@ Split make_split(const Geom &g, const AttnArgs &a, int n_sms)
     return s;
 }
 
-template <class T, int D>
+template <class T, int D, bool WINDOW>
 cudaError_t decode_launch(const Geom &g, const DecodeArgs &d, const CUtensorMap &map, const Launch &l, uint32_t *launched)
 {
     cudaError_t e;
     if (d.a.n > kLocalPlanMax) {
-        e = launch_pdl(attn_plan_kernel, dim3(1), dim3(kStepThreads), 0, l.stream, g, d);
+        e = launch_pdl(attn_plan_kernel<WINDOW>, dim3(1), dim3(kStepThreads), 0, l.stream, g, d);
         if (e != cudaSuccess) return e;
         *launched += 1;
     }
     const size_t smem = 1024 + d.s.stages * d.s.stage_bytes + (d.a.n <= kLocalPlanMax ? 3 * ((size_t)d.a.n + 1) * 4 : 0);
-    e = allow_smem<attn_decode_kernel<T, D>>(l.device, 1024 + kRingBytes + 3 * (kLocalPlanMax + 1) * 4);
+    e = allow_smem<attn_decode_kernel<T, D, WINDOW>>(l.device, 1024 + kRingBytes + 3 * (kLocalPlanMax + 1) * 4);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(attn_decode_kernel<T, D>, dim3(d.s.ctas, d.s.head_groups), dim3(kThreads), smem, l.stream, g, d, map);
+    e = launch_pdl(attn_decode_kernel<T, D, WINDOW>, dim3(d.s.ctas, d.s.head_groups), dim3(kThreads), smem, l.stream, g, d, map);
     if (e != cudaSuccess) return e;
     *launched += 1;
     const uint32_t jobs = d.a.prefix == kInvalid ? d.s.ctas - 1 : d.a.n;
     if (jobs == 0) return cudaSuccess;
     *launched += 1;
     return launch_pdl(attn_join_kernel<T, D>, dim3(jobs, (d.a.q_heads + 3) / 4), dim3(128), 0, l.stream, d);
+}
+
+template <bool WINDOW>
+cudaError_t decode_type(const Geom &g, const DecodeArgs &d, const CUtensorMap &map, const Launch &l, uint32_t *launched)
+{
+    if (d.a.head_dim == 128) return d.a.f16 ? decode_launch<F16, 128, WINDOW>(g, d, map, l, launched) : decode_launch<Bf16, 128, WINDOW>(g, d, map, l, launched);
+    return d.a.f16 ? decode_launch<F16, 64, WINDOW>(g, d, map, l, launched) : decode_launch<Bf16, 64, WINDOW>(g, d, map, l, launched);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -559,8 +593,7 @@ cudaError_t launch_attn_decode(const Geom &g, const AttnArgs &a, const Launch &l
         if (e != cudaSuccess) return e;
         *launched += 1;
     }
-    if (a.head_dim == 128) return a.f16 ? decode_launch<F16, 128>(g, d, map, l, launched) : decode_launch<Bf16, 128>(g, d, map, l, launched);
-    return a.f16 ? decode_launch<F16, 64>(g, d, map, l, launched) : decode_launch<Bf16, 64>(g, d, map, l, launched);
+    return a.window ? decode_type<true>(g, d, map, l, launched) : decode_type<false>(g, d, map, l, launched);
 }
 
 size_t attn_ws_bytes(const Geom &g, uint32_t n, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, int n_sms)

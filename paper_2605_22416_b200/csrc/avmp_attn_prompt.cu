@@ -116,6 +116,7 @@ struct Work {
     uint32_t held;                // tokens of the chain
     uint32_t len;                 // tokens that the tile's last row sees
     uint32_t j0, j1;              // KV rounds
+    uint32_t lead, skip;          // with a window: rounds from `lead` on stand for those `skip` further on (in front of it are the sinks)
     uint32_t tok0, rem0;          // token and head in group of the tile's first row
     bool end;                     // with no rows: nothing follows
 };
@@ -123,6 +124,11 @@ struct Work {
 // The i-th tile of CTA c: the list runs from long tiles to short ones, every other pass over the CTAs backwards.
 __device__ __forceinline__ uint32_t nth_tile(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
 
+// The round of the chain that round j of a tile is.
+template <bool WINDOW>
+__device__ __forceinline__ uint32_t chain_round(const Work &w, uint32_t j) { return WINDOW && j >= w.lead ? j + w.skip : j; }
+
+template <bool WINDOW>
 __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint32_t req, uint32_t held, uint32_t past, uint32_t q0,
                                           uint32_t all_rows, uint32_t block, uint32_t head, uint32_t split, bool causal)
 {
@@ -132,7 +138,14 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
     w.rows = min((uint32_t)kRows, all_rows - w.row0);
     w.tok0 = w.row0 / p.group; w.rem0 = w.row0 - w.tok0 * p.group;
     w.len = causal ? past + (w.row0 + w.rows - 1) / p.group + 1 : held;
-    const uint32_t rounds = (w.len + kKv - 1) / kKv;
+    uint32_t rounds = (w.len + kKv - 1) / kKv;
+    w.lead = w.skip = 0;
+    if (WINDOW) {      // from the first token in the window of the tile's first row; all rounds that have sinks in front of it
+        const uint32_t low = past + w.tok0 >= p.a.window ? past + w.tok0 - p.a.window + 1 : 0u;
+        w.lead = (min(p.a.sinks, low) + kKv - 1) / kKv;
+        w.skip = low / kKv > w.lead ? low / kKv - w.lead : 0u;
+        rounds -= w.skip;
+    }
     w.j0 = 0; w.j1 = rounds;
     if (p.splits > 1) {      // shares of whole rounds: the first `rest` get one more
         const uint32_t each = rounds / p.splits, rest = rounds - each * p.splits;
@@ -149,21 +162,21 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
 //     long ones start first.  How many row blocks have R rounds or more has a closed form per entry, so the i-th of
 //     that order is found by bisection over R and a sum over the lanes, without a list.
 //   more: the list that prompt_plan_kernel wrote.
-template <bool PREFIX, class Wanted, class Give>
+template <bool PREFIX, bool WINDOW, class Wanted, class Give>
 __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Wanted wanted, Give give)
 {
     const uint32_t lane = threadIdx.x % 32, per = p.a.kv_heads * p.splits;
     if (PREFIX) {
         const uint32_t r = p.a.prefix, held = held_tokens(g, r);
         for (uint32_t n = 0, i; (i = nth_tile(n)) < p.prefix_blocks * per; ++n)
-            if (wanted(n) && !give(make_work(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
+            if (wanted(n) && !give(make_work<WINDOW>(p, 0, r, held, 0, 0, p.a.n * p.group, i / per, i % per / p.splits, i % p.splits, false))) return;
     } else if (p.tiles) {
         const uint32_t n_tiles = *(volatile uint32_t *)p.n_tiles;
         for (uint32_t n = 0, i; (i = nth_tile(n)) < n_tiles * per; ++n) {
             if (!wanted(n)) continue;
             const Tile t = p.tiles[i / per];
             const Item it = p.items[t.k];
-            if (!give(make_work(p, t.k, it.req, it.len, it.len - it.nq, it.q0, it.nq * p.group, t.b, i % per / p.splits, i % p.splits, true))) return;
+            if (!give(make_work<WINDOW>(p, t.k, it.req, it.len, it.len - it.nq, it.q0, it.nq * p.group, t.b, i % per / p.splits, i % p.splits, true))) return;
         }
     } else {
         uint32_t req = 0, held = 0, q0 = 0, nq = 0, blocks = 0, top = 0;
@@ -204,7 +217,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Wan
             const uint32_t at = e - __reduce_add_sync(0xFFFFFFFFu, blocks - f1);
             const uint32_t owner = __ffs(__ballot_sync(0xFFFFFFFFu, incl > at)) - 1;
             const uint32_t block = __shfl_sync(0xFFFFFFFFu, f0 + at - (incl - mine), owner);
-            if (!give(make_work(p, owner, __shfl_sync(0xFFFFFFFFu, req, owner), __shfl_sync(0xFFFFFFFFu, held, owner),
+            if (!give(make_work<WINDOW>(p, owner, __shfl_sync(0xFFFFFFFFu, req, owner), __shfl_sync(0xFFFFFFFFu, held, owner),
                                 __shfl_sync(0xFFFFFFFFu, past, owner), __shfl_sync(0xFFFFFFFFu, q0, owner),
                                 __shfl_sync(0xFFFFFFFFu, nq, owner) * p.group, block, i - e * p.a.kv_heads, 0, true))) return;
         }
@@ -228,7 +241,7 @@ constexpr uint32_t kRedo = 2048;              // bits for tiles to be done again
 
 template <class T> constexpr float kLift = T::kF16 ? 7.f : -8.f;         // weights are 2^(score - m + kLift), score - m at most 8
 
-template <class T, int D, bool PREFIX>
+template <class T, int D, bool PREFIX, bool WINDOW>
 __global__ void __launch_bounds__(kCta, 1)
 attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map)
 {
@@ -284,7 +297,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
             for (uint32_t n = 0; ok; ++n) {
                 ok = mbar_wait(bar(B_WORK + n % kWorks), n / kWorks & 1, waits);
                 if (!ok) break;
-                const Work &t = works[n % kWorks];
+                const Work t = works[n % kWorks];
                 const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, head = t.head, token = t.q0 + t.tok0;
                 const bool t_end = t.end;
                 const uint32_t need = min((t.len + 15u) & ~15u, t.held);     // products run over whole steps of 16 tokens
@@ -297,7 +310,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 }
                 const uint32_t part_row = (p.a.layer * 2 + v) * g.T * p.a.kv_heads + head;
                 auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
-                    const uint32_t tok = j * kKv + lane * p.box_tokens;
+                    const uint32_t tok = chain_round<WINDOW>(t, j) * kKv + lane * p.box_tokens;
                     if (j >= j1 || lane * p.box_tokens >= kKv || tok >= need) return kInvalid;
                     return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
                 };
@@ -323,7 +336,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 for (uint32_t j = j0; j < j1; ++j, it += 2) {
                     const uint32_t slot = next;
                     const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
-                    uint32_t tok = (j * kKv) % g.T;
+                    uint32_t tok = (chain_round<WINDOW>(t, j) * kKv) % g.T;
                     const uint32_t s = it % M::kSlots, round = it / M::kSlots, full = bar(B_FULL + s);
                     ok = !round || mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, waits);
                     if (!ok) break;
@@ -373,7 +386,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 for (uint32_t n = 0; ok; ++n) {
                     ok = mbar_wait_one(bar(B_WORK + n % kWorks), n / kWorks & 1, waits);
                     if (!ok) break;
-                    const Work &t = works[n % kWorks];
+                    const Work t = works[n % kWorks];
                     const uint32_t rows = t.rows, j0 = t.j0, j1 = t.j1, len = t.len;
                     const bool t_end = t.end;
                     mbar_arrive(bar(B_TAKEN + n % kWorks));
@@ -398,7 +411,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     for (uint32_t j = j0; j < j1 && ok; ++j, it += 2) {
                         const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
                         const bool more = j + 1 < j1;
-                        const uint32_t steps = min((uint32_t)kKv / 16, (len - j * kKv + 15) / 16);
+                        const uint32_t steps = min((uint32_t)kKv / 16, (len - chain_round<WINDOW>(t, j) * kKv + 15) / 16);
                         const unsigned long long b = v_desc + ((sv * M::kTile) >> 4);
                         auto weigh = [&](uint32_t m, uint32_t r) {
                             // first the half of the tokens whose weights are written first
@@ -441,11 +454,11 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 return true;
             };
             Work none = {};
-            hand_out<PREFIX>(g, p, [](uint32_t) { return true; }, give);
+            hand_out<PREFIX, WINDOW>(g, p, [](uint32_t) { return true; }, give);
             if (!PREFIX) {
                 give(none);
                 bar_sync(kRowsBar, kRowsBarThreads);
-                if (*(volatile uint32_t *)&any_redo) hand_out<PREFIX>(g, p, [&](uint32_t i) { return (redo[i % kRedo / 32] >> (i % 32) & 1) != 0; }, give);
+                if (*(volatile uint32_t *)&any_redo) hand_out<PREFIX, WINDOW>(g, p, [&](uint32_t i) { return (redo[i % kRedo / 32] >> (i % 32) & 1) != 0; }, give);
             }
             none.end = true;
             give(none);
@@ -508,6 +521,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 // columns of a round up to this one are seen by the row
                 const uint32_t sees = PREFIX ? t.len - 1 : t.past + token;
                 const uint32_t least = t.past + t.tok0 + per_group(t.rem0 + m * 128);      // what the warpgroup's first row sees
+                const uint32_t low = WINDOW && sees >= p.a.window ? sees - p.a.window + 1 : 0u;     // the first token in the row's window
                 for (uint32_t j = t.j0; j < t.j1; ++j, ++rounds) {
                     ok = mbar_wait(bar(B_S + m), rounds & 1, waits);
                     if (!ok) break;
@@ -517,10 +531,16 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
                     tmem_wait_ld();
                     float *s = reinterpret_cast<float *>(u);
-                    if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
-                        const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
+                    const uint32_t j_tok = chain_round<WINDOW>(t, j) * kKv;      // the round's first token
+                    if (__any_sync(0xFFFFFFFFu, sees < j_tok + kKv - 1)) {
+                        const int lim = sees >= j_tok ? (int)min(sees - j_tok, 127u) : -1;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
+                    }
+                    if (WINDOW && __any_sync(0xFFFFFFFFu, low > j_tok && low > p.a.sinks)) {
+                        const int from = low > j_tok ? (int)min(low - j_tok, 128u) : 0, sinks = p.a.sinks > j_tok ? (int)min(p.a.sinks - j_tok, 128u) : 0;
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s[c] = c >= from || c < sinks ? s[c] : -INFINITY;
                     }
                     float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
 #pragma unroll
@@ -547,8 +567,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         }
                     }
                     // Tokens of this round that the products run over; of them those of the chain; of them, once more, those that every row here sees.
-                    const uint32_t rows = min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16), valid = min(t.held - j * kKv, rows);
-                    const uint32_t clear = !again ? valid : min(valid, least >= j * kKv ? least - j * kKv + 1 : 0u);
+                    const uint32_t rows = min((uint32_t)kKv, (t.len - j_tok + 15) / 16 * 16), valid = min(t.held - j_tok, rows);
+                    const uint32_t clear = !again ? valid : WINDOW ? 0u : min(valid, least >= j_tok ? least - j_tok + 1 : 0u);
                     if (clear < rows) {
                         // Before this round's weights are announced: V behind the last token of the chain (leftovers of other requests) becomes
                         // zeros, and the second time so does what is not finite in tokens that some rows do not see.
@@ -629,9 +649,16 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                             uint32_t o[16];
                             tmem_ld16(o, to + c);
                             tmem_wait_ld();
-                            if (mine)                   // tokens behind the tile's first row, of this tile's rounds
-                                add_not_finite<T>(g, g.r_chain + (unsigned long long)d.req * g.max_pages, max(d.past + d.tok0 + 1, d.j0 * kKv), min(sees + 1, d.j1 * kKv),
-                                                  (unsigned long long)(p.a.layer * 2 + 1) * g.T * g.row_bytes + ((unsigned long long)d.head * D + c) * 2, o);
+                            const uint32_t *chain = g.r_chain + (unsigned long long)d.req * g.max_pages;
+                            const unsigned long long in_page = (unsigned long long)(p.a.layer * 2 + 1) * g.T * g.row_bytes + ((unsigned long long)d.head * D + c) * 2;
+                            if (mine && !WINDOW)        // tokens behind the tile's first row, of this tile's rounds
+                                add_not_finite<T>(g, chain, max(d.past + d.tok0 + 1, d.j0 * kKv), min(sees + 1, d.j1 * kKv), in_page, o);
+                            if (mine && WINDOW)         // all that the row sees: sinks, and what is in its window
+                                for (uint32_t j = d.j0; j < d.j1; ++j) {
+                                    const uint32_t from = chain_round<true>(d, j) * kKv, to_tok = min(from + kKv, sees + 1);
+                                    add_not_finite<T>(g, chain, from, min(to_tok, p.a.sinks), in_page, o);
+                                    add_not_finite<T>(g, chain, max(from, max(low, p.a.sinks)), to_tok, in_page, o);
+                                }
                             __syncwarp();
                             tmem_st16(to + c, o);
                         }
@@ -762,25 +789,25 @@ uint32_t box_of(uint32_t T)
 // Rows of partial sums that a call may leave.  Splits x row blocks x KV heads never pass the SMs, and a row block has 256 rows.
 size_t part_rows(size_t rows, int n_sms) { const size_t full = (size_t)n_sms * kRows; return rows > full ? rows : full; }
 
-template <class T, int D, bool PREFIX>
+template <class T, int D, bool PREFIX, bool WINDOW>
 cudaError_t tile_launch(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
 {
     CUtensorMap map;
     if (!row_map(&map, g, p.a.head_dim, p.box_tokens)) return cudaErrorNotSupported;
-    const cudaError_t e = allow_smem<attn_tile_kernel<T, D, PREFIX>>(l.device, Smem<D>::kTotal);
+    const cudaError_t e = allow_smem<attn_tile_kernel<T, D, PREFIX, WINDOW>>(l.device, Smem<D>::kTotal);
     if (e != cudaSuccess) return e;
     CUtensorMap q_map = {};
     PromptArgs a = p;
     const uint32_t rows = PREFIX ? p.a.n : p.a.total_q;
     a.q_boxes = (p.group & (p.group - 1)) == 0 && rows &&
                 query_map(&q_map, p.a.q, p.a.head_dim, p.a.q_heads, rows, p.a.qs, 128 / p.group, p.group);
-    return launch_pdl(attn_tile_kernel<T, D, PREFIX>, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, a, map, q_map);
+    return launch_pdl(attn_tile_kernel<T, D, PREFIX, WINDOW>, dim3(grid), dim3(kCta), Smem<D>::kTotal, l.stream, g, a, map, q_map);
 }
-template <bool PREFIX>
+template <bool PREFIX, bool WINDOW = false>
 cudaError_t tile_type(const Geom &g, const PromptArgs &p, uint32_t grid, const Launch &l)
 {
-    if (p.a.head_dim == 128) return p.a.f16 ? tile_launch<F16, 128, PREFIX>(g, p, grid, l) : tile_launch<Bf16, 128, PREFIX>(g, p, grid, l);
-    return p.a.f16 ? tile_launch<F16, 64, PREFIX>(g, p, grid, l) : tile_launch<Bf16, 64, PREFIX>(g, p, grid, l);
+    if (p.a.head_dim == 128) return p.a.f16 ? tile_launch<F16, 128, PREFIX, WINDOW>(g, p, grid, l) : tile_launch<Bf16, 128, PREFIX, WINDOW>(g, p, grid, l);
+    return p.a.f16 ? tile_launch<F16, 64, PREFIX, WINDOW>(g, p, grid, l) : tile_launch<Bf16, 64, PREFIX, WINDOW>(g, p, grid, l);
 }
 template <class T>
 cudaError_t join_type(const PromptArgs &p, uint32_t grid, const Launch &l)
@@ -831,6 +858,10 @@ cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l
     const unsigned long long most = (unsigned long long)a.total_q * p.group / kRows + a.n;      // row blocks of the buffers' rows
     p.cap = (uint32_t)min(full, most);
     p.splits = split_of(most * a.kv_heads, l.n_sms);           // (parts lie by row of the buffers: see part_rows)
+    if (a.window) {      // no more than a tile has rounds: those of its rows' windows and of the sinks, each with two ends that need not be at a round's
+        const unsigned long long rounds = ((unsigned long long)a.window + kRows) / kKv + a.sinks / kKv + 4;
+        if (p.splits > rounds) p.splits = (uint32_t)rounds;
+    }
     uint8_t *w = a.ws;
     p.n_tiles = reinterpret_cast<uint32_t *>(w); w += 256;
     p.tiles = reinterpret_cast<Tile *>(w); w += up256((size_t)full * sizeof(Tile));
@@ -847,12 +878,13 @@ cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l
         *launched += 1;
     }
     const unsigned long long tiles = (unsigned long long)p.cap * a.kv_heads * p.splits;
-    e = tile_type<false>(g, p, (uint32_t)min(tiles, (unsigned long long)l.n_sms), l);
+    const uint32_t grid = (uint32_t)min(tiles, (unsigned long long)l.n_sms);
+    e = a.window ? tile_type<false, true>(g, p, grid, l) : tile_type<false>(g, p, grid, l);
     if (e != cudaSuccess) return e;
     *launched += 1;
     if (p.splits > 1) {
-        const uint32_t grid = (uint32_t)min((unsigned long long)p.cap * a.kv_heads, 4ull * l.n_sms);
-        e = a.f16 ? join_type<F16>(p, grid, l) : join_type<Bf16>(p, grid, l);
+        const uint32_t joins = (uint32_t)min((unsigned long long)p.cap * a.kv_heads, 4ull * l.n_sms);
+        e = a.f16 ? join_type<F16>(p, joins, l) : join_type<Bf16>(p, joins, l);
         *launched += 1;
     }
     return e;

@@ -237,10 +237,48 @@ struct SsmArgs {
 uint32_t ssm_shares(uint32_t n, uint32_t heads, uint32_t dv, uint32_t total, int n_sms);
 cudaError_t launch_ssm_step(const Geom &g, const SsmArgs &a, const Launch &l);
 cudaError_t launch_ssm_prompt(const Geom &g, const SsmArgs &a, const Launch &l, uint32_t *n_launched);
+// Short convolution on the windows of SSM blocks (avmp_conv.cu).
+struct ConvArgs {
+    uint32_t layer, n, channels, width, total, state_elems;
+    bool f16, act;
+    const uint32_t *reqs, *cu, *resume;        // cu null: one row per entry
+    const uint8_t *x;
+    const float *weight, *bias;                // bias may be null
+    uint8_t *out;
+    unsigned long long xs, os;                 // row strides in bytes
+};
+cudaError_t launch_conv(const Geom &g, const ConvArgs &a, const Launch &l);
+// Selective scan on the states of SSM blocks (avmp_scan.cu).
+struct ScanArgs {
+    uint32_t layer, n, channels, groups, states, total, shares;
+    bool f16, softplus;
+    const uint32_t *reqs, *cu, *resume;
+    const uint8_t *u, *d, *b, *c, *z;          // z may be null
+    const float *a, *skip, *bias;              // skip and bias may be null
+    uint8_t *out;
+    unsigned long long us, ds, bs, cs, zs, os; // row strides in bytes
+    float *ws;
+};
+uint32_t scan_shares(uint32_t n, uint32_t channels, uint32_t groups, uint32_t total, int n_sms);
+cudaError_t launch_scan_prompt(const Geom &g, const ScanArgs &a, const Launch &l, uint32_t *n_launched);
+cudaError_t launch_scan_step(const Geom &g, const ScanArgs &a, const Launch &l);
+// Norms, rotation and page writes of new rows (avmp_rows.cu).
+struct RowsArgs {
+    uint32_t layer, n, q_heads, kv_heads, head_dim, rotary, total;
+    bool f16, neighbours;
+    float eps;
+    const uint32_t *reqs, *cu, *pos;           // cu null: one row per entry; pos may be null
+    const uint8_t *q, *k, *v;
+    const float *wq, *wk, *freq;               // weights may be null
+    uint8_t *out;
+    unsigned long long qs, ks, vs, os;         // row strides in bytes
+};
+cudaError_t launch_attn_rows(const Geom &g, const RowsArgs &a, const Launch &l);
 // Attention over KV chains (avmp_attn.cu, avmp_attn_prompt.cu).
 struct AttnArgs {
     uint32_t layer, n, q_heads, kv_heads, head_dim, total_q;
     uint32_t prefix;                           // slot, or kInvalid
+    uint32_t window, sinks;                    // window 0: all tokens
     bool f16;
     float scale;
     const uint32_t *reqs, *cu;

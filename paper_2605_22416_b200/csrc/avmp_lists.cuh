@@ -1,0 +1,76 @@
+// What the calls over request lists share: the state block behind a list entry, repeated slots, runs of rows of packed buffers.
+#pragma once
+
+#include "avmp_dev.cuh"
+#include "avmp_mma.cuh"
+
+namespace avmp {
+
+// The block of a request's state layer, or null where the slot is out of range or not LIVE.
+__device__ __forceinline__ float *state_block(const Geom &g, uint32_t layer, uint32_t r)
+{
+    uint32_t slot = kInvalid;
+    if (r < g.R) {
+        const uint32_t state = g.r_state[r], h = g.r_ssm[(unsigned long long)r * g.ns + layer];
+        if (state == AVMP_REQ_LIVE && h != kInvalid) slot = g.VT[1][h & 0x7FFFFFFFu];
+    }
+    return slot == kInvalid ? nullptr : reinterpret_cast<float *>(unit_ptr(g, AVMP_POOL_SSM, slot));
+}
+// Whether an earlier entry of the list names the same slot (two entries would write one block at the same time).  Whole CTA.
+__device__ __forceinline__ bool named_before(const uint32_t *reqs, uint32_t k, uint32_t r)
+{
+    bool dup = false;
+    for (uint32_t j = threadIdx.x; j < k; j += blockDim.x) dup |= reqs[j] == r;
+    return __syncthreads_or(dup);
+}
+
+// The rows of all list entries, in runs of `rows` at most: an entry without rows, or with offsets that do not fit the buffers, has
+// one too, so that somebody looks after it.  A CTA walks them in ascending order; the entries' offsets pass through shared memory as
+// many at a time as the CTA has threads.
+struct Runs {
+    const uint32_t *cu;          // null: one row each
+    uint32_t n, total, rows;
+    uint32_t *pre;               // shared, blockDim.x + 1
+    unsigned long long *tmp;     // shared, 32
+    uint32_t k0, cnt;
+    unsigned long long begin, end;
+
+    __device__ Runs(const uint32_t *cu_, uint32_t n_, uint32_t total_, uint32_t rows_, uint32_t *pre_, unsigned long long *tmp_)
+        : cu(cu_), n(n_), total(total_), rows(rows_), pre(pre_), tmp(tmp_), k0(0), cnt(0), begin(0), end(0) {}
+    // Run i: its entry and its number there.  False behind the last one.  Whole CTA; i ascends from call to call.
+    __device__ bool seek(unsigned long long i, uint32_t *k, uint32_t *run)
+    {
+        if (!cu) {
+            *k = (uint32_t)i; *run = 0;
+            return i < n;
+        }
+        while (i >= end) {
+            if (k0 + cnt >= n) return false;
+            k0 += cnt;
+            cnt = min(blockDim.x, n - k0);
+            __syncthreads();                       // the offsets before have been read
+            unsigned long long mine = 0, all;
+            if (threadIdx.x < cnt) {
+                const uint32_t c0 = cu[k0 + threadIdx.x], c1 = cu[k0 + threadIdx.x + 1];
+                mine = c1 > c0 && c1 <= total ? (c1 - c0 + rows - 1) / rows : 1u;
+            }
+            const unsigned long long incl = block_incl_scan(mine, tmp, &all);
+            pre[threadIdx.x] = (uint32_t)(incl - mine);
+            begin = end; end += all;
+            __syncthreads();
+        }
+        const uint32_t at = find_owner(pre, 0, cnt, 0, (uint32_t)(i - begin));
+        *k = k0 + at; *run = (uint32_t)(i - begin) - pre[at];
+        return true;
+    }
+};
+
+// x / (1 + e^-x)
+__device__ __forceinline__ float silu(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_approx(x * -1.4426950408889634f)));
+    return x * r;
+}
+
+}  // namespace avmp
