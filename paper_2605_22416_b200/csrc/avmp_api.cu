@@ -219,7 +219,7 @@ ScanArgs scan_args(const avmp_scan_desc *d, uint32_t layer, const uint32_t *reqs
 // Scratch of one scan over prompts: a state and a sum of steps for each run of each (request, channel).
 size_t scan_ws_bytes(const avmp_ctx *c, const avmp_scan_desc *d, uint32_t n, uint32_t total)
 {
-    const uint32_t shares = scan_shares(n, d->channels, d->groups, total, c->n_sms);
+    const uint32_t shares = scan_shares(n, d->channels, d->groups, d->states, total, c->n_sms);
     return shares < 2 ? 0 : (size_t)n * shares * d->channels * (d->states + 1) * 4;
 }
 
@@ -812,9 +812,9 @@ int avmp_conv_step(avmp_ctx *c, uint32_t layer, const avmp_conv_desc *desc, cons
 size_t avmp_scan_workspace_bytes(const avmp_ctx *c, const avmp_scan_desc *desc, uint32_t n, uint32_t total_tokens)
 {
     if (!c || !scan_desc_ok(c, desc)) return 0;
-    // Fewer requests are cut into more runs; from 2 n_sms requests up none is (see scan_shares).
+    // Fewer requests are cut into more runs; from n_sms requests up none is (see scan_plan).
     size_t most = 0;
-    for (uint32_t k = 1; k <= n && k <= 2u * (uint32_t)c->n_sms; ++k) {
+    for (uint32_t k = 1; k <= n && k <= (uint32_t)c->n_sms; ++k) {
         const size_t b = scan_ws_bytes(c, desc, k, total_tokens);
         if (b > most) most = b;
     }
@@ -830,14 +830,14 @@ int avmp_scan_prompt(avmp_ctx *c, uint32_t layer, const avmp_scan_desc *desc, co
     if (n == 0) return AVMP_OK;
     if (!d_reqs || !d_cu || off4(d_reqs) || off4(d_cu) || off4(d_resume) || total_tokens >= (1u << 31)) return AVMP_EINVAL;
     if (!scan_rows_ok(total_tokens != 0, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out)) return AVMP_EINVAL;
-    if ((uint64_t)n * desc->groups * ((desc->channels / desc->groups + 31) / 32) >= (1ull << 31)) return AVMP_EINVAL;
+    if ((uint64_t)n * (desc->channels / 8) >= (1ull << 31)) return AVMP_EINVAL;
     ScanArgs a = scan_args(desc, layer, d_reqs, n, d_u, d_delta, d_b, d_c, d_z, d_a, d_d, d_delta_bias, d_out);
     a.cu = d_cu; a.resume = d_resume; a.total = total_tokens;
     if (scan_ws_bytes(c, desc, n, total_tokens)) {
         if (!d_workspace || off16(d_workspace)) return AVMP_EINVAL;
         if (workspace_bytes < avmp_scan_workspace_bytes(c, desc, n, total_tokens)) return AVMP_ENOSPC;
         a.ws = static_cast<float *>(d_workspace);
-        a.shares = scan_shares(n, desc->channels, desc->groups, total_tokens, c->n_sms);
+        a.shares = scan_shares(n, desc->channels, desc->groups, desc->states, total_tokens, c->n_sms);
     }
     uint32_t launched = 0;
     const cudaError_t e = launch_scan_prompt(c->g, a, L(c, stream), &launched);

@@ -259,7 +259,7 @@ struct ScanArgs {
     unsigned long long us, ds, bs, cs, zs, os; // row strides in bytes
     float *ws;
 };
-uint32_t scan_shares(uint32_t n, uint32_t channels, uint32_t groups, uint32_t total, int n_sms);
+uint32_t scan_shares(uint32_t n, uint32_t channels, uint32_t groups, uint32_t states, uint32_t total, int n_sms);
 cudaError_t launch_scan_prompt(const Geom &g, const ScanArgs &a, const Launch &l, uint32_t *n_launched);
 cudaError_t launch_scan_step(const Geom &g, const ScanArgs &a, const Launch &l);
 // Norms, rotation and page writes of new rows (avmp_rows.cu).
