@@ -13,8 +13,8 @@ namespace avmp {
 
 namespace {
 
-constexpr int kCta = 256;
-constexpr int kMostRows = 8;          // tokens of a run
+constexpr int kCta = 128;
+constexpr int kMostRows = 4;          // tokens of a run
 constexpr int kFly = 4;               // heads of a lane whose loads are in flight together
 
 // NEIGHBOURS: pairs are columns (2 i, 2 i + 1), else (i, i + rotary / 2).
@@ -45,24 +45,11 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
             continue;
         }
         const uint32_t first = c0 + run * rows, count = min(rows, c1 - first), place = held - (c1 - first);      // place of the run's first token in the chain
-        if (threadIdx.x < count) {
-            const uint32_t p = place + threadIdx.x, h = __ldcg(g.r_chain + ((unsigned long long)r * g.max_pages + p / g.T));
-            page[threadIdx.x] = unit_ptr(g, AVMP_POOL_KV, __ldcg(g.VT[0] + (h & 0x7FFFFFFFu))) + a.layer * g.kv_layer_bytes + p % g.T * g.row_bytes;
-        }
-        for (uint32_t x = threadIdx.x; x < count * half; x += kCta) {
-            const uint32_t t = x / half, j = x % half;
-            const double turn = (double)(a.pos ? a.pos[first + t] : place + t) * (double)a.freq[j] * 0.15915494309189533577;
-            float sn, cs;
-            sincospif((float)(2.0 * (turn - rint(turn))), &sn, &cs);
-            cosine[t][j] = cs; sine[t][j] = sn;
-        }
-        __syncthreads();
         uint32_t t = 0, chunk = w;
         auto settle = [&] { while (chunk >= chunks) { chunk -= chunks; ++t; } };
-        settle();
-        while (t < count) {
-            uint4 x[kFly];
-            uint32_t head[kFly], tok[kFly];
+        uint4 x[kFly];
+        uint32_t head[kFly], tok[kFly];
+        auto fetch = [&] {
 #pragma unroll
             for (int e = 0; e < kFly; ++e) {
                 head[e] = t < count ? chunk * HEADS + lane / LANES : heads;
@@ -81,6 +68,22 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
                     x[e] = make_uint4(lo.x, lo.y, hi.x, hi.y);
                 }
             }
+        };
+        settle();
+        fetch();                      // while the pages are looked up
+        if (threadIdx.x < count) {
+            const uint32_t p = place + threadIdx.x, h = __ldcg(g.r_chain + ((unsigned long long)r * g.max_pages + p / g.T));
+            page[threadIdx.x] = unit_ptr(g, AVMP_POOL_KV, __ldcg(g.VT[0] + (h & 0x7FFFFFFFu))) + a.layer * g.kv_layer_bytes + p % g.T * g.row_bytes;
+        }
+        for (uint32_t x = threadIdx.x; x < count * half; x += kCta) {
+            const uint32_t t = x / half, j = x % half;
+            const double turn = (double)(a.pos ? a.pos[first + t] : place + t) * (double)a.freq[j] * 0.15915494309189533577;
+            float sn, cs;
+            sincospif((float)(2.0 * (turn - rint(turn))), &sn, &cs);
+            cosine[t][j] = cs; sine[t][j] = sn;
+        }
+        __syncthreads();
+        for (;;) {
 #pragma unroll
             for (int e = 0; e < kFly; ++e) {
                 const bool there = head[e] < heads, is_q = head[e] < a.q_heads, is_v = head[e] >= a.q_heads + a.kv_heads;
@@ -124,6 +127,8 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
                     *reinterpret_cast<uint2 *>(dst + s * 2) = make_uint2(to.z, to.w);
                 }
             }
+            if (t >= count) break;
+            fetch();
         }
         __syncthreads();
     }
@@ -133,7 +138,7 @@ template <class T, int D>
 cudaError_t launch(const Geom &g, const RowsArgs &a, const Launch &l)
 {
     uint32_t rows = a.cu ? kMostRows : 1;
-    while (rows > 1 && a.total / rows < 4u * l.n_sms) rows >>= 1;
+    while (rows > 1 && a.total / rows < 16u * l.n_sms) rows >>= 1;
     const unsigned long long runs = a.cu ? (unsigned long long)a.total / rows + a.n : a.n;
     const dim3 grid((uint32_t)min(runs, 1ull << 20));
     return a.neighbours ? launch_pdl(rows_kernel<T, D, true>, grid, dim3(kCta), 0, l.stream, g, a, rows)

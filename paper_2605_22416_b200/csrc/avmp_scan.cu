@@ -373,68 +373,103 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
 }
 
 // ---------------------------------------------------------------- one token
-// CTA (i, j): kEntries entries, every gridDim.y-th run of kCta * 4 / N channels.  A thread has four states of a channel, for all entries of the CTA:
-// their decays stay in registers.
+// CTA (i, j): kEntries entries, the j-th run of `rounds` times kCta * 8 / N channels.  A thread has eight states of a channel, for all entries of
+// the CTA, so that decays and B and C are read once for several states; the next round's loads are on their way while one is worked on.
 constexpr int kEntries = 2;
 
 template <class T, int N>
-__global__ void __launch_bounds__(kCta) scan_step_kernel(const Geom g, const ScanArgs a)
+__global__ void __launch_bounds__(kCta) scan_step_kernel(const Geom g, const ScanArgs a, uint32_t rounds)
 {
-    constexpr int LANES = N / 4;
+    constexpr int LANES = N / 8;
     constexpr uint32_t CB = kCta / LANES;
     pdl_prologue();
-    const uint32_t k0 = blockIdx.x * kEntries, s = threadIdx.x % LANES * 4;
+    const uint32_t k0 = blockIdx.x * kEntries, s = threadIdx.x % LANES * 8, end = min(a.channels, (blockIdx.y + 1) * rounds * CB);
     float *block[kEntries];
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) block[e] = k0 + e < a.n ? state_block(g, a.layer, a.reqs[k0 + e]) : nullptr;
-    bool checked = false;
     const uint32_t per_group = a.channels / a.groups;
-    for (uint32_t ch = blockIdx.y * CB + threadIdx.x / LANES; ch - threadIdx.x / LANES < a.channels; ch += gridDim.y * CB) {
-        const bool mine = ch < a.channels;
+    struct Round {
+        float4 h[kEntries][2], A[2];
+        uint16_t u[kEntries], d[kEntries], z[kEntries];
+        float bias, skip;
+    };
+    auto fetch = [&](Round &r, uint32_t ch) {
+        if (ch >= end) return;
         const unsigned long long at = (unsigned long long)ch * N + s;
-        float4 h[kEntries], A = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int e = 0; e < kEntries; ++e)
-            if (mine && block[e]) h[e] = *reinterpret_cast<const float4 *>(block[e] + at);
-        if (mine) A = *reinterpret_cast<const float4 *>(a.a + at);
-        if (!checked) {          // while the first loads are on their way
-#pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                if (k0 + e >= a.n) continue;
-                if (named_before(a.reqs, k0 + e, a.reqs[k0 + e])) block[e] = nullptr;
-                if (!block[e] && blockIdx.y == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
-            }
-            checked = true;
-        }
-        const uint32_t grp = mine ? ch / per_group : 0u;
-        const float bias = mine && a.bias ? a.bias[ch] : 0.f, skip = mine && a.skip ? a.skip[ch] : 0.f;
 #pragma unroll
         for (int e = 0; e < kEntries; ++e) {
+            if (!block[e]) continue;
             const uint32_t k = k0 + e;
+            r.h[e][0] = *reinterpret_cast<const float4 *>(block[e] + at);
+            r.h[e][1] = *reinterpret_cast<const float4 *>(block[e] + at + 4);
+            r.u[e] = *reinterpret_cast<const uint16_t *>(a.u + k * a.us + ch * 2);
+            r.d[e] = *reinterpret_cast<const uint16_t *>(a.d + k * a.ds + ch * 2);
+            if (a.z) r.z[e] = *reinterpret_cast<const uint16_t *>(a.z + k * a.zs + ch * 2);
+        }
+        r.A[0] = *reinterpret_cast<const float4 *>(a.a + at);
+        r.A[1] = *reinterpret_cast<const float4 *>(a.a + at + 4);
+        r.bias = a.bias ? a.bias[ch] : 0.f;
+        r.skip = a.skip ? a.skip[ch] : 0.f;
+    };
+    uint4 b[kEntries], c[kEntries];
+    uint32_t grp = kInvalid;
+    auto work = [&](Round &r, uint32_t ch) {
+        const bool mine = ch < end;
+        if (mine && ch / per_group != grp) {
+            grp = ch / per_group;
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e) {
+                if (!block[e]) continue;
+                b[e] = *reinterpret_cast<const uint4 *>(a.b + (k0 + e) * a.bs + (grp * N + s) * 2);
+                c[e] = *reinterpret_cast<const uint4 *>(a.c + (k0 + e) * a.cs + (grp * N + s) * 2);
+            }
+        }
+        const float A[8] = {r.A[0].x, r.A[0].y, r.A[0].z, r.A[0].w, r.A[1].x, r.A[1].y, r.A[1].z, r.A[1].w};
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            const bool there = mine && block[e];
             float y = 0.f, u = 0.f;
-            if (mine && block[e]) {
-                u = T::unpack(*reinterpret_cast<const uint16_t *>(a.u + k * a.us + ch * 2)).x;
-                float d = T::unpack(*reinterpret_cast<const uint16_t *>(a.d + k * a.ds + ch * 2)).x + bias;
+            if (there) {
+                u = T::unpack(r.u[e]).x;
+                float d = T::unpack(r.d[e]).x + r.bias;
                 if (a.softplus) d = softplus(d);
-                const uint2 bb = *reinterpret_cast<const uint2 *>(a.b + k * a.bs + (grp * N + s) * 2);
-                const uint2 cc = *reinterpret_cast<const uint2 *>(a.c + k * a.cs + (grp * N + s) * 2);
-                const float2 b0 = T::unpack(bb.x), b1 = T::unpack(bb.y), c0 = T::unpack(cc.x), c1 = T::unpack(cc.y);
                 const float du = d * u, x = d * kLog2e;
-                h[e].x = fmaf(exp2_approx(x * A.x), h[e].x, du * b0.x);
-                h[e].y = fmaf(exp2_approx(x * A.y), h[e].y, du * b0.y);
-                h[e].z = fmaf(exp2_approx(x * A.z), h[e].z, du * b1.x);
-                h[e].w = fmaf(exp2_approx(x * A.w), h[e].w, du * b1.y);
-                *reinterpret_cast<float4 *>(block[e] + at) = h[e];
-                y = h[e].x * c0.x + h[e].y * c0.y + h[e].z * c1.x + h[e].w * c1.y;
+                const uint32_t bb[4] = {b[e].x, b[e].y, b[e].z, b[e].w}, cc[4] = {c[e].x, c[e].y, c[e].z, c[e].w};
+                float h[8] = {r.h[e][0].x, r.h[e][0].y, r.h[e][0].z, r.h[e][0].w, r.h[e][1].x, r.h[e][1].y, r.h[e][1].z, r.h[e][1].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 B = T::unpack(bb[i]), C = T::unpack(cc[i]);
+                    h[2 * i] = fmaf(exp2_approx(x * A[2 * i]), h[2 * i], du * B.x);
+                    h[2 * i + 1] = fmaf(exp2_approx(x * A[2 * i + 1]), h[2 * i + 1], du * B.y);
+                    y = fmaf(h[2 * i], C.x, fmaf(h[2 * i + 1], C.y, y));
+                }
+                float *to = block[e] + (unsigned long long)ch * N + s;
+                *reinterpret_cast<float4 *>(to) = make_float4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<float4 *>(to + 4) = make_float4(h[4], h[5], h[6], h[7]);
             }
 #pragma unroll
             for (int o = LANES / 2; o; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
-            if (mine && block[e] && s == 0) {
-                y = fmaf(skip, u, y);
-                if (a.z) y *= silu(T::unpack(*reinterpret_cast<const uint16_t *>(a.z + k * a.zs + ch * 2)).x);
-                *reinterpret_cast<uint16_t *>(a.out + k * a.os + ch * 2) = (uint16_t)T::pack(y, 0.f);
+            if (there && s == 0) {
+                y = fmaf(r.skip, u, y);
+                if (a.z) y *= silu(T::unpack(r.z[e]).x);
+                *reinterpret_cast<uint16_t *>(a.out + (k0 + e) * a.os + ch * 2) = (uint16_t)T::pack(y, 0.f);
             }
         }
+    };
+    const uint32_t ch0 = blockIdx.y * rounds * CB + threadIdx.x / LANES;
+    Round r[2];
+    fetch(r[0], ch0);
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {      // while the first loads are on their way
+        if (k0 + e >= a.n) continue;
+        if (named_before(a.reqs, k0 + e, a.reqs[k0 + e])) block[e] = nullptr;
+        if (!block[e] && blockIdx.y == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+    }
+    for (uint32_t i = 0; i < rounds; i += 2) {
+        fetch(r[1], ch0 + (i + 1) * CB);
+        work(r[0], ch0 + i * CB);
+        fetch(r[0], ch0 + (i + 2) * CB);
+        work(r[1], ch0 + (i + 1) * CB);
     }
 }
 
@@ -473,11 +508,11 @@ cudaError_t prompt_type(const Geom &g, const ScanArgs &a, const Launch &l, uint3
 template <class T, int N>
 cudaError_t step_launch(const Geom &g, const ScanArgs &a, const Launch &l)
 {
-    const uint32_t cb = kCta / (N / 4), parts = (a.channels + cb - 1) / cb, groups = (a.n + kEntries - 1) / kEntries;
+    const uint32_t cb = kCta / (N / 8), parts = (a.channels + cb - 1) / cb, groups = (a.n + kEntries - 1) / kEntries;
     // 8 rounds amortise a CTA's look-ups; fewer where that leaves SMs idle
     uint32_t rounds = 8;
-    while (rounds > 1 && (unsigned long long)groups * ((parts + rounds - 1) / rounds) < 16ull * l.n_sms) rounds >>= 1;
-    return launch_pdl(scan_step_kernel<T, N>, dim3(groups, (parts + rounds - 1) / rounds), dim3(kCta), 0, l.stream, g, a);
+    while (rounds > 2 && (unsigned long long)groups * ((parts + rounds - 1) / rounds) < 8ull * l.n_sms) rounds >>= 1;
+    return launch_pdl(scan_step_kernel<T, N>, dim3(groups, (parts + rounds - 1) / rounds), dim3(kCta), 0, l.stream, g, a, rounds);
 }
 template <class T>
 cudaError_t step_type(const Geom &g, const ScanArgs &a, const Launch &l)
