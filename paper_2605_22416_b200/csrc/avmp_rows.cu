@@ -3,9 +3,11 @@
 // its leading columns are rotated by the token's position (pairs of columns as complex numbers, times e^(i position freq)), keys and
 // values are written to their pages and queries to a buffer; all in one pass.
 //
-// Bound by HBM: every element is read once and written once, 2 bytes each way.  A lane has 8 columns of a head such that both columns of
-// every pair are its own; sines and cosines are worked out once for all heads of a token.  Angles are taken in 64 bits: 2^-24 of a far
-// position's angle would be thousandths of a turn.
+// Bound by HBM: every element is read once and written once, 2 bytes each way.  A warp has one token, and of it two heads of 128 columns or four of 64 at a time;
+// a lane has 8 columns of a head such that both columns of every pair are its own, so that a rotation needs no exchange, and
+// weights, sines and cosines, multiplied once, serve all heads of the token from registers.  Angles are taken in 64 bits: 2^-24 of a far
+// position's angle would be thousandths of a turn.  Heads come through a ring in shared memory by asynchronous copies, a lane's own columns for
+// itself: with loads into registers too little is on its way (12 turns of 256 to 2048 tokens, 64 query heads: 112 us).
 #include "avmp_lists.cuh"
 #include "avmp_tc.cuh"
 
@@ -14,8 +16,9 @@ namespace avmp {
 namespace {
 
 constexpr int kCta = 128;
-constexpr int kMostRows = 4;          // tokens of a run
-constexpr int kFly = 4;               // heads of a lane whose loads are in flight together
+constexpr uint32_t kWarps = kCta / 32;
+constexpr int kSteps = 2;             // a stage: so many heads (or pairs, or fours) of a warp
+constexpr int kStages = 8;            // stages of the ring: one is worked on, the others are on their way
 
 // NEIGHBOURS: pairs are columns (2 i, 2 i + 1), else (i, i + rotary / 2).
 template <class T, int D, bool NEIGHBOURS>
@@ -24,121 +27,154 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
     constexpr uint32_t LANES = D / 8, HEADS = 32 / LANES;      // lanes of a head; heads a warp has at a time
     __shared__ uint32_t pre[kCta + 1];
     __shared__ unsigned long long tmp[32];
-    __shared__ __align__(16) float cosine[kMostRows][D / 2], sine[kMostRows][D / 2], weight[2][D];
-    __shared__ uint8_t *page[kMostRows];
+    __shared__ uint4 ring[kStages * kSteps][kCta];
     pdl_prologue();
     const uint32_t half = a.rotary / 2, w = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % LANES;
-    for (uint32_t i = threadIdx.x; i < 2 * D; i += kCta) {
-        const float *from = i < D ? a.wq : a.wk;
-        weight[i / D][i % D] = from ? from[i % D] : 1.f;
-    }
-    // this lane's columns: f .. f + 3 and s .. s + 3
+    // this lane's columns: f .. f + 3 and s .. s + 3; its pairs are 4 l .. 4 l + 3
     const bool turns = 8 * l < a.rotary;
     const uint32_t f = NEIGHBOURS || !turns ? 8 * l : 4 * l, s = NEIGHBOURS || !turns ? 8 * l + 4 : half + 4 * l;
-    const uint32_t heads = a.q_heads + 2 * a.kv_heads, chunks = (heads + HEADS - 1) / HEADS;
+    const uint32_t h0 = w / rows * HEADS + lane / LANES, h_step = kWarps / rows * HEADS;
+    auto write = [&](uint8_t *p, const uint4 &v) {
+        if (NEIGHBOURS) {
+            *reinterpret_cast<uint4 *>(p + f * 2) = v;
+        } else {
+            *reinterpret_cast<uint2 *>(p + f * 2) = make_uint2(v.x, v.y);
+            *reinterpret_cast<uint2 *>(p + s * 2) = make_uint2(v.z, v.w);
+        }
+    };
     Runs runs(a.cu, a.n, a.total, rows, pre, tmp);
     uint32_t k, run;
     for (unsigned long long i = blockIdx.x; runs.seek(i, &k, &run); i += gridDim.x) {
-        const uint32_t r = a.reqs[k], c0 = a.cu ? a.cu[k] : k, c1 = a.cu ? a.cu[k + 1] : k + 1, held = held_tokens(g, r);
-        if (named_before(a.reqs, k, r) || held == 0 || c1 < c0 || c1 > a.total || c1 - c0 > held) {
+        const uint32_t r = a.reqs[k], c0 = a.cu ? a.cu[k] : k, c1 = a.cu ? a.cu[k + 1] : k + 1;
+        const bool rows_ok = c1 >= c0 && c1 <= a.total;
+        const uint32_t row = c0 + run * rows + w % rows;            // this warp's token
+        const bool mine = rows_ok && row < c1;
+        const uint8_t *q = a.q + (unsigned long long)row * a.qs, *kk = a.k + (unsigned long long)row * a.ks, *v = a.v + (unsigned long long)row * a.vs;
+        // the warp's stages: those of the query heads, then of the keys, then of the values
+        const uint32_t q_stages = (a.q_heads + kSteps * h_step - 1) / (kSteps * h_step), kv_stages = (a.kv_heads + kSteps * h_step - 1) / (kSteps * h_step);
+        uint32_t next = 0, place_in = 0;
+        auto load = [&] {
+            const bool is_q = next < q_stages, is_k = next < q_stages + kv_stages;
+            const uint8_t *from = is_q ? q : is_k ? kk : v;
+            const uint32_t heads = is_q ? a.q_heads : next < q_stages + 2 * kv_stages ? a.kv_heads : 0u;
+            const uint32_t h = h0 + (next - (is_q ? 0u : is_k ? q_stages : q_stages + kv_stages)) * (kSteps * h_step);
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e) {
+                if (!mine || h + e * h_step >= heads) continue;
+                const uint8_t *p = from + (h + e * h_step) * (D * 2);
+                const uint32_t to = smem_u32(&ring[place_in * kSteps + e][threadIdx.x]);
+                if (NEIGHBOURS) {
+                    cp_async16(to, p + f * 2, true);
+                } else {
+                    cp_async8(to, p + f * 2);
+                    cp_async8(to + 8, p + s * 2);
+                }
+            }
+            cp_async_commit();
+            next += 1;
+            place_in = place_in + 1 == kStages ? 0 : place_in + 1;
+        };
+#pragma unroll
+        for (int e = 0; e < kStages - 1; ++e) load();               // while the slot and the page are looked up
+        const uint32_t held = held_tokens(g, r);
+        if (named_before(a.reqs, k, r) || held == 0 || !rows_ok || c1 - c0 > held) {
             if (run == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+            cp_async_wait<0>();
             continue;
         }
-        const uint32_t first = c0 + run * rows, count = min(rows, c1 - first), place = held - (c1 - first);      // place of the run's first token in the chain
-        uint32_t t = 0, chunk = w;
-        auto settle = [&] { while (chunk >= chunks) { chunk -= chunks; ++t; } };
-        uint4 x[kFly];
-        uint32_t head[kFly], tok[kFly];
-        auto fetch = [&] {
+        if (!mine) continue;
+        const uint32_t place = held - (c1 - row), page = __ldcg(g.r_chain + ((unsigned long long)r * g.max_pages + place / g.T));
+        uint8_t *to_k = unit_ptr(g, AVMP_POOL_KV, __ldcg(g.VT[0] + (page & 0x7FFFFFFFu))) + a.layer * g.kv_layer_bytes + place % g.T * g.row_bytes;
+        uint8_t *to_v = to_k + g.T * g.row_bytes, *to_q = a.out + (unsigned long long)row * a.os;
+        // sines and cosines: the lanes that have the same columns of different heads work out a share of them each
+        float cs[4], sn[4];
+        {
+            constexpr uint32_t EACH = 4 / HEADS;
+            float c[EACH], d[EACH];
 #pragma unroll
-            for (int e = 0; e < kFly; ++e) {
-                head[e] = t < count ? chunk * HEADS + lane / LANES : heads;
-                tok[e] = t;
-                chunk += kCta / 32;
-                settle();
-                if (head[e] >= heads) continue;
-                const unsigned long long row = first + tok[e];
-                const uint8_t *from = head[e] < a.q_heads ? a.q + row * a.qs + head[e] * D * 2
-                    : head[e] < a.q_heads + a.kv_heads ? a.k + row * a.ks + (head[e] - a.q_heads) * D * 2
-                                                       : a.v + row * a.vs + (head[e] - a.q_heads - a.kv_heads) * D * 2;
-                if (NEIGHBOURS) {
-                    x[e] = *reinterpret_cast<const uint4 *>(from + f * 2);
-                } else {
-                    const uint2 lo = *reinterpret_cast<const uint2 *>(from + f * 2), hi = *reinterpret_cast<const uint2 *>(from + s * 2);
-                    x[e] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            for (uint32_t j = 0; j < EACH; ++j) {
+                c[j] = 1.f; d[j] = 0.f;
+                if (turns) {
+                    const double turn = (double)(a.pos ? a.pos[row] : place) * (double)a.freq[4 * l + lane / LANES * EACH + j] * 0.15915494309189533577;
+                    sincospif((float)(2.0 * (turn - rint(turn))), &d[j], &c[j]);
                 }
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                cs[j] = __shfl_sync(0xFFFFFFFFu, c[j % EACH], l + j / EACH * LANES);
+                sn[j] = __shfl_sync(0xFFFFFFFFu, d[j % EACH], l + j / EACH * LANES);
+            }
+        }
+        uint32_t place_out = 0;
+        auto heads_of = [&](uint8_t *to, uint32_t heads, uint32_t stages, const float *weight) {
+            // a pair (p, o) becomes by * (p pc - o os, o oc + p ps)
+            float pc[4], os[4], oc[4], ps[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float wp = weight ? weight[NEIGHBOURS ? f + 2 * j : f + j] : 1.f, wo = weight ? weight[NEIGHBOURS ? f + 2 * j + 1 : s + j] : 1.f;
+                pc[j] = wp * cs[j]; os[j] = wo * sn[j]; oc[j] = wo * cs[j]; ps[j] = wp * sn[j];
+            }
+            uint32_t h = h0;
+            for (uint32_t x = 0; x < stages; ++x) {
+                load();
+                cp_async_wait<kStages - 1>();
+#pragma unroll
+                for (int e = 0; e < kSteps; ++e, h += h_step) {
+                    const uint4 in4 = ring[place_out * kSteps + e][threadIdx.x];
+                    const uint32_t in[4] = {in4.x, in4.y, in4.z, in4.w};
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 z = T::unpack(in[j]);
+                        y[2 * j] = z.x; y[2 * j + 1] = z.y;
+                    }
+                    float by = 1.f;
+                    if (weight) {
+                        float sq = y[0] * y[0];
+#pragma unroll
+                        for (int j = 1; j < 8; ++j) sq = fmaf(y[j], y[j], sq);
+#pragma unroll
+                        for (uint32_t o = LANES / 2; o; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
+                        by = rsqrtf(sq * (1.f / D) + a.eps);
+                    }
+                    uint32_t out[4];
+                    float re[4], im[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = y[NEIGHBOURS ? 2 * j : j], o = y[NEIGHBOURS ? 2 * j + 1 : j + 4];
+                        re[j] = by * (p * pc[j] - o * os[j]); im[j] = by * (o * oc[j] + p * ps[j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (NEIGHBOURS) { out[2 * j] = T::pack(re[2 * j], im[2 * j]); out[2 * j + 1] = T::pack(re[2 * j + 1], im[2 * j + 1]); }
+                        else { out[j] = T::pack(re[2 * j], re[2 * j + 1]); out[2 + j] = T::pack(im[2 * j], im[2 * j + 1]); }
+                    }
+                    if (h < heads) write(to + h * (D * 2), make_uint4(out[0], out[1], out[2], out[3]));
+                }
+                place_out = place_out + 1 == kStages ? 0 : place_out + 1;
             }
         };
-        settle();
-        fetch();                      // while the pages are looked up
-        if (threadIdx.x < count) {
-            const uint32_t p = place + threadIdx.x, h = __ldcg(g.r_chain + ((unsigned long long)r * g.max_pages + p / g.T));
-            page[threadIdx.x] = unit_ptr(g, AVMP_POOL_KV, __ldcg(g.VT[0] + (h & 0x7FFFFFFFu))) + a.layer * g.kv_layer_bytes + p % g.T * g.row_bytes;
+        heads_of(to_q, a.q_heads, q_stages, a.wq);
+        heads_of(to_k, a.kv_heads, kv_stages, a.wk);
+        uint32_t h = h0;
+        for (uint32_t x = 0; x < kv_stages; ++x) {
+            load();
+            cp_async_wait<kStages - 1>();
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e, h += h_step)
+                if (h < a.kv_heads) write(to_v + h * (D * 2), ring[place_out * kSteps + e][threadIdx.x]);
+            place_out = place_out + 1 == kStages ? 0 : place_out + 1;
         }
-        for (uint32_t x = threadIdx.x; x < count * half; x += kCta) {
-            const uint32_t t = x / half, j = x % half;
-            const double turn = (double)(a.pos ? a.pos[first + t] : place + t) * (double)a.freq[j] * 0.15915494309189533577;
-            float sn, cs;
-            sincospif((float)(2.0 * (turn - rint(turn))), &sn, &cs);
-            cosine[t][j] = cs; sine[t][j] = sn;
-        }
-        __syncthreads();
-        for (;;) {
-#pragma unroll
-            for (int e = 0; e < kFly; ++e) {
-                const bool there = head[e] < heads, is_q = head[e] < a.q_heads, is_v = head[e] >= a.q_heads + a.kv_heads;
-                const uint32_t in[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
-                float y[8], sq = 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 v = there ? T::unpack(in[j]) : make_float2(0.f, 0.f);
-                    y[2 * j] = v.x; y[2 * j + 1] = v.y;
-                    sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
-                }
-#pragma unroll
-                for (uint32_t o = LANES / 2; o; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
-                if (!there) continue;
-                uint4 to = x[e];
-                if (!is_v) {
-                    if (is_q ? a.wq != nullptr : a.wk != nullptr) {
-                        const float by = rsqrtf(sq * (1.f / D) + a.eps);
-                        const float4 w0 = *reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][f]), w1 = *reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][s]);
-                        y[0] *= by * w0.x; y[1] *= by * w0.y; y[2] *= by * w0.z; y[3] *= by * w0.w;
-                        y[4] *= by * w1.x; y[5] *= by * w1.y; y[6] *= by * w1.z; y[7] *= by * w1.w;
-                    }
-                    if (turns) {
-                        const float4 c4 = *reinterpret_cast<const float4 *>(&cosine[tok[e]][4 * l]), s4 = *reinterpret_cast<const float4 *>(&sine[tok[e]][4 * l]);
-                        const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float &p = y[NEIGHBOURS ? 2 * j : j], &o = y[NEIGHBOURS ? 2 * j + 1 : j + 4];
-                            const float re = p * cs[j] - o * sn[j], im = o * cs[j] + p * sn[j];
-                            p = re; o = im;
-                        }
-                    }
-                    to = make_uint4(T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7]));
-                }
-                uint8_t *dst = is_q ? a.out + (unsigned long long)(first + tok[e]) * a.os + head[e] * D * 2
-                             : page[tok[e]] + (is_v ? g.T * g.row_bytes + (head[e] - a.q_heads - a.kv_heads) * D * 2 : (unsigned long long)(head[e] - a.q_heads) * D * 2);
-                if (NEIGHBOURS) {
-                    *reinterpret_cast<uint4 *>(dst + f * 2) = to;
-                } else {
-                    *reinterpret_cast<uint2 *>(dst + f * 2) = make_uint2(to.x, to.y);
-                    *reinterpret_cast<uint2 *>(dst + s * 2) = make_uint2(to.z, to.w);
-                }
-            }
-            if (t >= count) break;
-            fetch();
-        }
-        __syncthreads();
+        cp_async_wait<0>();
     }
 }
 
 template <class T, int D>
 cudaError_t launch(const Geom &g, const RowsArgs &a, const Launch &l)
 {
-    uint32_t rows = a.cu ? kMostRows : 1;
-    while (rows > 1 && a.total / rows < 16u * l.n_sms) rows >>= 1;
+    // A token for each warp; where that leaves SMs idle, one or two for all four.
+    uint32_t rows = a.cu ? kWarps : 1;
+    while (rows > 1 && a.total / rows < 4u * l.n_sms) rows >>= 1;
     const unsigned long long runs = a.cu ? (unsigned long long)a.total / rows + a.n : a.n;
     const dim3 grid((uint32_t)min(runs, 1ull << 20));
     return a.neighbours ? launch_pdl(rows_kernel<T, D, true>, grid, dim3(kCta), 0, l.stream, g, a, rows)
