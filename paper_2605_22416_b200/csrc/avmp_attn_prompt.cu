@@ -116,17 +116,13 @@ struct Work {
     uint32_t held;                // tokens of the chain
     uint32_t len;                 // tokens that the tile's last row sees
     uint32_t j0, j1;              // KV rounds
-    uint32_t lead, skip;          // with a window: rounds from `lead` on stand for those `skip` further on (in front of it are the sinks)
+    uint32_t lead, shift;         // with a window, `past`, `held` and `len` leave the `shift` tokens out that no row sees: they lie behind the first `lead`
     uint32_t tok0, rem0;          // token and head in group of the tile's first row
     bool end;                     // with no rows: nothing follows
 };
 
 // The i-th tile of CTA c: the list runs from long tiles to short ones, every other pass over the CTAs backwards.
 __device__ __forceinline__ uint32_t nth_tile(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
-
-// The round of the chain that round j of a tile is.
-template <bool WINDOW>
-__device__ __forceinline__ uint32_t chain_round(const Work &w, uint32_t j) { return WINDOW && j >= w.lead ? j + w.skip : j; }
 
 template <bool WINDOW>
 __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint32_t req, uint32_t held, uint32_t past, uint32_t q0,
@@ -138,14 +134,16 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
     w.rows = min((uint32_t)kRows, all_rows - w.row0);
     w.tok0 = w.row0 / p.group; w.rem0 = w.row0 - w.tok0 * p.group;
     w.len = causal ? past + (w.row0 + w.rows - 1) / p.group + 1 : held;
-    uint32_t rounds = (w.len + kKv - 1) / kKv;
-    w.lead = w.skip = 0;
-    if (WINDOW) {      // from the first token in the window of the tile's first row; all rounds that have sinks in front of it
-        const uint32_t low = past + w.tok0 >= p.a.window ? past + w.tok0 - p.a.window + 1 : 0u;
-        w.lead = (min(p.a.sinks, low) + kKv - 1) / kKv;
-        w.skip = low / kKv > w.lead ? low / kKv - w.lead : 0u;
-        rounds -= w.skip;
+    w.lead = w.shift = 0;
+    if (WINDOW) {
+        // What the tile's rows see: the sinks, then everything from the first token in the first row's window, in whole boxes.  Rounds
+        // run over these tokens without the gap between.
+        const uint32_t at = past + w.tok0, low = at >= p.a.window ? (at - p.a.window + 1) / p.box_tokens * p.box_tokens : 0u;
+        w.lead = p.a.sinks < low ? (p.a.sinks + p.box_tokens - 1) / p.box_tokens * p.box_tokens : low;
+        w.shift = low - w.lead;
+        w.past -= w.shift; w.held -= w.shift; w.len -= w.shift;
     }
+    const uint32_t rounds = (w.len + kKv - 1) / kKv;
     w.j0 = 0; w.j1 = rounds;
     if (p.splits > 1) {      // shares of whole rounds: the first `rest` get one more
         const uint32_t each = rounds / p.splits, rest = rounds - each * p.splits;
@@ -309,10 +307,11 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     continue;
                 }
                 const uint32_t part_row = (p.a.layer * 2 + v) * g.T * p.a.kv_heads + head;
+                auto in_chain = [&](uint32_t tok) { return WINDOW && tok >= t.lead ? tok + t.shift : tok; };
                 auto look = [&](uint32_t j) -> uint32_t {      // lane b: slot of the page that holds box b of round j
-                    const uint32_t tok = chain_round<WINDOW>(t, j) * kKv + lane * p.box_tokens;
+                    const uint32_t tok = j * kKv + lane * p.box_tokens;
                     if (j >= j1 || lane * p.box_tokens >= kKv || tok >= need) return kInvalid;
-                    return g.VT[0][chain[tok / g.T] & 0x7FFFFFFFu];
+                    return g.VT[0][chain[in_chain(tok) / g.T] & 0x7FFFFFFFu];
                 };
                 uint32_t next = look(j0);
                 if (v == 1 && p.q_boxes && j0 < j1) {
@@ -336,7 +335,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 for (uint32_t j = j0; j < j1; ++j, it += 2) {
                     const uint32_t slot = next;
                     const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, slot != kInvalid));
-                    uint32_t tok = (chain_round<WINDOW>(t, j) * kKv) % g.T;
+                    uint32_t tok = (j * kKv) % g.T;
+                    const uint32_t off = WINDOW ? in_chain(j * kKv + lane * p.box_tokens) % g.T : 0u;      // lane b: of box b in its page
                     const uint32_t s = it % M::kSlots, round = it / M::kSlots, full = bar(B_FULL + s);
                     ok = !round || mbar_wait(bar(B_EMPTY + s), (round - 1) & 1, waits);
                     if (!ok) break;
@@ -344,6 +344,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     if (elect_one()) mbar_expect(full, boxes * p.box_tokens * D * 2);
                     for (uint32_t b = 0; b < boxes; ++b) {
                         const uint32_t page = __shfl_sync(0xFFFFFFFFu, slot, b);
+                        if (WINDOW) tok = __shfl_sync(0xFFFFFFFFu, off, b);
                         if (elect_one()) tma_load_rows(dst, &map, full, tok / 8, page * page_rows + part_row);
                         dst += p.box_tokens * D * 2;
                         tok += p.box_tokens;
@@ -411,7 +412,7 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     for (uint32_t j = j0; j < j1 && ok; ++j, it += 2) {
                         const uint32_t sv = (it + 1) % M::kSlots, sk = (it + 2) % M::kSlots;
                         const bool more = j + 1 < j1;
-                        const uint32_t steps = min((uint32_t)kKv / 16, (len - chain_round<WINDOW>(t, j) * kKv + 15) / 16);
+                        const uint32_t steps = min((uint32_t)kKv / 16, (len - j * kKv + 15) / 16);
                         const unsigned long long b = v_desc + ((sv * M::kTile) >> 4);
                         auto weigh = [&](uint32_t m, uint32_t r) {
                             // first the half of the tokens whose weights are written first
@@ -531,14 +532,13 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
                     tmem_wait_ld();
                     float *s = reinterpret_cast<float *>(u);
-                    const uint32_t j_tok = chain_round<WINDOW>(t, j) * kKv;      // the round's first token
-                    if (__any_sync(0xFFFFFFFFu, sees < j_tok + kKv - 1)) {
-                        const int lim = sees >= j_tok ? (int)min(sees - j_tok, 127u) : -1;
+                    if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
+                        const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
                     }
-                    if (WINDOW && __any_sync(0xFFFFFFFFu, low > j_tok && low > p.a.sinks)) {
-                        const int from = low > j_tok ? (int)min(low - j_tok, 128u) : 0, sinks = p.a.sinks > j_tok ? (int)min(p.a.sinks - j_tok, 128u) : 0;
+                    if (WINDOW && __any_sync(0xFFFFFFFFu, low > j * kKv && low > p.a.sinks)) {
+                        const int from = low > j * kKv ? (int)min(low - j * kKv, 128u) : 0, sinks = p.a.sinks > j * kKv ? (int)min(p.a.sinks - j * kKv, 128u) : 0;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) s[c] = c >= from || c < sinks ? s[c] : -INFINITY;
                     }
@@ -567,8 +567,8 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                         }
                     }
                     // Tokens of this round that the products run over; of them those of the chain; of them, once more, those that every row here sees.
-                    const uint32_t rows = min((uint32_t)kKv, (t.len - j_tok + 15) / 16 * 16), valid = min(t.held - j_tok, rows);
-                    const uint32_t clear = !again ? valid : WINDOW ? 0u : min(valid, least >= j_tok ? least - j_tok + 1 : 0u);
+                    const uint32_t rows = min((uint32_t)kKv, (t.len - j * kKv + 15) / 16 * 16), valid = min(t.held - j * kKv, rows);
+                    const uint32_t clear = !again ? valid : WINDOW ? 0u : min(valid, least >= j * kKv ? least - j * kKv + 1 : 0u);
                     if (clear < rows) {
                         // Before this round's weights are announced: V behind the last token of the chain (leftovers of other requests) becomes
                         // zeros, and the second time so does what is not finite in tokens that some rows do not see.
@@ -653,12 +653,11 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                             const unsigned long long in_page = (unsigned long long)(p.a.layer * 2 + 1) * g.T * g.row_bytes + ((unsigned long long)d.head * D + c) * 2;
                             if (mine && !WINDOW)        // tokens behind the tile's first row, of this tile's rounds
                                 add_not_finite<T>(g, chain, max(d.past + d.tok0 + 1, d.j0 * kKv), min(sees + 1, d.j1 * kKv), in_page, o);
-                            if (mine && WINDOW)         // all that the row sees: sinks, and what is in its window
-                                for (uint32_t j = d.j0; j < d.j1; ++j) {
-                                    const uint32_t from = chain_round<true>(d, j) * kKv, to_tok = min(from + kKv, sees + 1);
-                                    add_not_finite<T>(g, chain, from, min(to_tok, p.a.sinks), in_page, o);
-                                    add_not_finite<T>(g, chain, max(from, max(low, p.a.sinks)), to_tok, in_page, o);
-                                }
+                            if (mine && WINDOW) {       // all that the row sees of this tile's rounds: sinks, and what is in its window
+                                const uint32_t from = d.j0 * kKv, end = min(sees + 1, d.j1 * kKv);
+                                add_not_finite<T>(g, chain, from, min(end, p.a.sinks), in_page, o);
+                                add_not_finite<T>(g, chain, max(from, max(low, p.a.sinks)) + d.shift, end + d.shift, in_page, o);
+                            }
                             __syncwarp();
                             tmem_st16(to + c, o);
                         }
@@ -779,10 +778,10 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs p)
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-uint32_t box_of(uint32_t T)
+uint32_t box_of(uint32_t T, uint32_t most)
 {
     uint32_t b = 8;
-    while (b < (uint32_t)kKv && T % (2 * b) == 0) b *= 2;
+    while (b < most && T % (2 * b) == 0) b *= 2;
     return b;
 }
 
@@ -832,7 +831,7 @@ cudaError_t launch_attn_prefix(const Geom &g, const AttnArgs &a, const Launch &l
     p.prefix_blocks = (uint32_t)(((unsigned long long)a.n * p.group + kRows - 1) / kRows);
     const unsigned long long tiles = (unsigned long long)p.prefix_blocks * a.kv_heads;
     p.splits = split_of(tiles, l.n_sms);
-    p.box_tokens = box_of(g.T);
+    p.box_tokens = box_of(g.T, kKv);
     const size_t rows = (size_t)p.splits * a.n * a.q_heads;
     p.parts.ml = reinterpret_cast<float2 *>(a.ws);
     p.parts.o = reinterpret_cast<float *>(a.ws + up256(rows * 8));
@@ -853,7 +852,7 @@ cudaError_t launch_attn_prompt(const Geom &g, const AttnArgs &a, const Launch &l
     PromptArgs p = {};
     p.a = a;
     p.group = a.q_heads / a.kv_heads;
-    p.box_tokens = box_of(g.T);
+    p.box_tokens = box_of(g.T, a.window ? 32 : kKv);        // (with a window: what is read beside it is less than a box)
     const unsigned long long full = (unsigned long long)a.n * (((unsigned long long)g.max_pages * g.T * p.group + kRows - 1) / kRows);
     const unsigned long long most = (unsigned long long)a.total_q * p.group / kRows + a.n;      // row blocks of the buffers' rows
     p.cap = (uint32_t)min(full, most);
