@@ -24,6 +24,27 @@ __device__ __forceinline__ bool named_before(const uint32_t *reqs, uint32_t k, u
     return __syncthreads_or(dup);
 }
 
+// The same for entries k .. k + each - 1 (each <= 4; those behind the n-th are not looked at): a bit for each.  `flags` is a word of
+// shared memory.  Whole CTA.
+__device__ __forceinline__ uint32_t named_before_each(const uint32_t *reqs, uint32_t k, uint32_t each, uint32_t n, uint32_t *flags)
+{
+    const uint32_t last = min(n, k + each);
+    uint32_t r[4], bits = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) r[e] = k + e < last ? reqs[k + e] : 0u;
+    if (threadIdx.x == 0) *flags = 0;
+    __syncthreads();
+    for (uint32_t j = threadIdx.x; j + 1 < last; j += blockDim.x) {
+        const uint32_t x = reqs[j];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) bits |= (uint32_t)(x == r[e] && j < k + e) << e;
+    }
+    bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+    if (bits && threadIdx.x % 32 == 0) atomicOr(flags, bits);
+    __syncthreads();
+    return *flags;
+}
+
 // The rows of all list entries, in runs of `rows` at most: an entry without rows, or with offsets that do not fit the buffers, has
 // one too, so that somebody looks after it.  A CTA walks them in ascending order; the entries' offsets pass through shared memory as
 // many at a time as the CTA has threads.

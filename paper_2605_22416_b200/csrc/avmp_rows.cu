@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
     __shared__ uint32_t pre[kCta + 1];
     __shared__ unsigned long long tmp[32];
     __shared__ uint4 ring[kStages * kSteps][kCta];
+    __shared__ uint32_t flags;
     pdl_prologue();
     const uint32_t half = a.rotary / 2, w = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % LANES;
     // this lane's columns: f .. f + 3 and s .. s + 3; its pairs are 4 l .. 4 l + 3
@@ -44,10 +45,18 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
     };
     Runs runs(a.cu, a.n, a.total, rows, pre, tmp);
     uint32_t k, run;
-    for (unsigned long long i = blockIdx.x; runs.seek(i, &k, &run); i += gridDim.x) {
-        const uint32_t r = a.reqs[k], c0 = a.cu ? a.cu[k] : k, c1 = a.cu ? a.cu[k + 1] : k + 1;
-        const bool rows_ok = c1 >= c0 && c1 <= a.total;
-        const uint32_t row = c0 + run * rows + w % rows;            // this warp's token
+    for (unsigned long long i = blockIdx.x;; i += gridDim.x) {
+        // this warp's token: of a run of one entry, or of as many entries with one token each
+        if (a.cu) {
+            if (!runs.seek(i, &k, &run)) break;
+        } else {
+            if (i * rows >= a.n) break;
+            k = (uint32_t)i * rows + w % rows; run = 0;
+        }
+        const bool listed = k < a.n;
+        const uint32_t r = listed ? a.reqs[k] : kInvalid, c0 = a.cu ? a.cu[k] : k, c1 = a.cu ? a.cu[k + 1] : k + 1;
+        const bool rows_ok = listed && c1 >= c0 && c1 <= a.total;
+        const uint32_t row = a.cu ? c0 + run * rows + w % rows : k;
         const bool mine = rows_ok && row < c1;
         const uint8_t *q = a.q + (unsigned long long)row * a.qs, *kk = a.k + (unsigned long long)row * a.ks, *v = a.v + (unsigned long long)row * a.vs;
         // the warp's stages: those of the query heads, then of the keys, then of the values
@@ -77,8 +86,9 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
 #pragma unroll
         for (int e = 0; e < kStages - 1; ++e) load();               // while the slot and the page are looked up
         const uint32_t held = held_tokens(g, r);
-        if (named_before(a.reqs, k, r) || held == 0 || !rows_ok || c1 - c0 > held) {
-            if (run == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+        const bool again = a.cu ? named_before(a.reqs, k, r) : (named_before_each(a.reqs, (uint32_t)i * rows, rows, a.n, &flags) >> (w % rows) & 1) != 0;
+        if (again || held == 0 || !rows_ok || c1 - c0 > held) {
+            if (listed && run == 0 && lane == 0 && w < (a.cu ? 1u : rows)) record_error(g.st, AVMP_DEV_BAD_REQUEST);
             cp_async_wait<0>();
             continue;
         }
@@ -174,8 +184,9 @@ cudaError_t launch(const Geom &g, const RowsArgs &a, const Launch &l)
 {
     // A token for each warp; where that leaves SMs idle, one or two for all four.
     uint32_t rows = a.cu ? kWarps : 1;
-    while (rows > 1 && a.total / rows < 4u * l.n_sms) rows >>= 1;
-    const unsigned long long runs = a.cu ? (unsigned long long)a.total / rows + a.n : a.n;
+    while (a.cu && rows > 1 && a.total / rows < 4u * l.n_sms) rows >>= 1;
+    while (!a.cu && rows < kWarps && a.n / rows > 5u * l.n_sms) rows <<= 1;      // five CTAs fit on an SM: one wave
+    const unsigned long long runs = a.cu ? (unsigned long long)a.total / rows + a.n : (a.n + rows - 1) / rows;
     const dim3 grid((uint32_t)min(runs, 1ull << 20));
     return a.neighbours ? launch_pdl(rows_kernel<T, D, true>, grid, dim3(kCta), 0, l.stream, g, a, rows)
                         : launch_pdl(rows_kernel<T, D, false>, grid, dim3(kCta), 0, l.stream, g, a, rows);

@@ -373,103 +373,159 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
 }
 
 // ---------------------------------------------------------------- one token
-// CTA (i, j): kEntries entries, the j-th run of `rounds` times kCta * 8 / N channels.  A thread has eight states of a channel, for all entries of
-// the CTA, so that decays and B and C are read once for several states; the next round's loads are on their way while one is worked on.
-constexpr int kEntries = 2;
+// The work is the list of all (tile, entry) pairs, a tile being 16 KB of states (4096 / N channels of a group); each CTA has a share of it, so that
+// a tile's decays stay in registers over many entries.  A thread has four float4 of a tile, one in each quarter: accesses cover whole
+// lines, and steps, gates and outputs are worked out by a lane each, the lanes of a channel sharing out the four.  States and rows come
+// through a ring in shared memory, so that their number in flight costs no registers.
+constexpr int kStep = 256;
+constexpr uint32_t kBatch = 256;      // entries whose blocks are looked up at a time
+
+template <int N>
+struct StepTile {
+    static constexpr uint32_t LANES = N / 4, CH = 4096 / N, kQuarter = CH / 4;       // lanes of a channel; channels of a tile and of a quarter
+    static constexpr uint32_t kStages = 4;                                           // entries: one is worked on, the others are on their way
+    static constexpr uint32_t kRow = CH * 2, oRows = 16384, oBc = oRows + 3 * kRow, kStage = oBc + 4 * N;      // states, u, d, z, B, C
+    static constexpr uint32_t kTotal = kStages * kStage;
+};
 
 template <class T, int N>
-__global__ void __launch_bounds__(kCta) scan_step_kernel(const Geom g, const ScanArgs a, uint32_t rounds)
+__global__ void __launch_bounds__(kStep, 3) scan_step_kernel(const Geom g, const ScanArgs a, uint32_t tiles_group)
 {
-    constexpr int LANES = N / 8;
-    constexpr uint32_t CB = kCta / LANES;
+    using L = StepTile<N>;
+    constexpr uint32_t LANES = L::LANES, OWN = LANES < 4 ? 2 : 1;                    // quarters that a lane finishes
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float *blocks[kBatch];
     pdl_prologue();
-    const uint32_t k0 = blockIdx.x * kEntries, s = threadIdx.x % LANES * 8, end = min(a.channels, (blockIdx.y + 1) * rounds * CB);
-    float *block[kEntries];
-#pragma unroll
-    for (int e = 0; e < kEntries; ++e) block[e] = k0 + e < a.n ? state_block(g, a.layer, a.reqs[k0 + e]) : nullptr;
+    const uint32_t tid = threadIdx.x, w = tid / 32, lane = tid % 32, q = tid % LANES, base = smem_u32(smem);
     const uint32_t per_group = a.channels / a.groups;
-    struct Round {
-        float4 h[kEntries][2], A[2];
-        uint16_t u[kEntries], d[kEntries], z[kEntries];
-        float bias, skip;
-    };
-    auto fetch = [&](Round &r, uint32_t ch) {
-        if (ch >= end) return;
-        const unsigned long long at = (unsigned long long)ch * N + s;
+    const unsigned long long pairs = (unsigned long long)a.groups * tiles_group * a.n, last = pairs * (blockIdx.x + 1) / gridDim.x;
+    auto channel = [&](uint32_t j) { return j * L::kQuarter + tid / LANES; };        // of the tile: this thread's in quarter j
+    // quarters that this lane finishes: j0, and j0 + 1 where a channel has two lanes
+    const uint32_t j0 = LANES < 4 ? 2 * q : q % 4;
+    const bool finishes = q < 4;
+    uint32_t count;
+    for (unsigned long long at = pairs * blockIdx.x / gridDim.x; at < last; at += count) {
+        const uint32_t tile = (uint32_t)(at / a.n), from = (uint32_t)(at % a.n), grp = tile / tiles_group;
+        count = (uint32_t)min((unsigned long long)min(kBatch, a.n - from), last - at);
+        const uint32_t ch0 = grp * per_group + tile % tiles_group * L::CH, chs = min(L::CH, (grp + 1) * per_group - ch0);
+        __syncthreads();                           // the blocks before have been used
+        if (tid < count) blocks[tid] = state_block(g, a.layer, a.reqs[from + tid]);
+        unsigned long long A[4][2];
+        float bias[OWN], skip[OWN];
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) {
-            if (!block[e]) continue;
-            const uint32_t k = k0 + e;
-            r.h[e][0] = *reinterpret_cast<const float4 *>(block[e] + at);
-            r.h[e][1] = *reinterpret_cast<const float4 *>(block[e] + at + 4);
-            r.u[e] = *reinterpret_cast<const uint16_t *>(a.u + k * a.us + ch * 2);
-            r.d[e] = *reinterpret_cast<const uint16_t *>(a.d + k * a.ds + ch * 2);
-            if (a.z) r.z[e] = *reinterpret_cast<const uint16_t *>(a.z + k * a.zs + ch * 2);
+        for (uint32_t j = 0; j < 4; ++j) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (channel(j) < chs) v = *reinterpret_cast<const float4 *>(a.a + (unsigned long long)(ch0 + channel(j)) * N + q * 4);
+            A[j][0] = pack2(v.x * kLog2e, v.y * kLog2e);
+            A[j][1] = pack2(v.z * kLog2e, v.w * kLog2e);
         }
-        r.A[0] = *reinterpret_cast<const float4 *>(a.a + at);
-        r.A[1] = *reinterpret_cast<const float4 *>(a.a + at + 4);
-        r.bias = a.bias ? a.bias[ch] : 0.f;
-        r.skip = a.skip ? a.skip[ch] : 0.f;
-    };
-    uint4 b[kEntries], c[kEntries];
-    uint32_t grp = kInvalid;
-    auto work = [&](Round &r, uint32_t ch) {
-        const bool mine = ch < end;
-        if (mine && ch / per_group != grp) {
-            grp = ch / per_group;
 #pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                if (!block[e]) continue;
-                b[e] = *reinterpret_cast<const uint4 *>(a.b + (k0 + e) * a.bs + (grp * N + s) * 2);
-                c[e] = *reinterpret_cast<const uint4 *>(a.c + (k0 + e) * a.cs + (grp * N + s) * 2);
-            }
+        for (uint32_t o = 0; o < OWN; ++o) {
+            const uint32_t ch = channel(j0 + o);
+            bias[o] = a.bias && ch < chs ? a.bias[ch0 + ch] : 0.f;
+            skip[o] = a.skip && ch < chs ? a.skip[ch0 + ch] : 0.f;
         }
-        const float A[8] = {r.A[0].x, r.A[0].y, r.A[0].z, r.A[0].w, r.A[1].x, r.A[1].y, r.A[1].z, r.A[1].w};
+        __syncthreads();
+        uint32_t next = 0, in = 0;
+        auto load = [&] {
+            if (next < count) {
+                float *block = blocks[next];
+                const unsigned long long k = from + next;
+                const uint32_t to = base + in * L::kStage;
+                if (block) {
+                    const float *src = block + (unsigned long long)ch0 * N + tid * 4;
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) {
-            const bool there = mine && block[e];
-            float y = 0.f, u = 0.f;
-            if (there) {
-                u = T::unpack(r.u[e]).x;
-                float d = T::unpack(r.d[e]).x + r.bias;
-                if (a.softplus) d = softplus(d);
-                const float du = d * u, x = d * kLog2e;
-                const uint32_t bb[4] = {b[e].x, b[e].y, b[e].z, b[e].w}, cc[4] = {c[e].x, c[e].y, c[e].z, c[e].w};
-                float h[8] = {r.h[e][0].x, r.h[e][0].y, r.h[e][0].z, r.h[e][0].w, r.h[e][1].x, r.h[e][1].y, r.h[e][1].z, r.h[e][1].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 B = T::unpack(bb[i]), C = T::unpack(cc[i]);
-                    h[2 * i] = fmaf(exp2_approx(x * A[2 * i]), h[2 * i], du * B.x);
-                    h[2 * i + 1] = fmaf(exp2_approx(x * A[2 * i + 1]), h[2 * i + 1], du * B.y);
-                    y = fmaf(h[2 * i], C.x, fmaf(h[2 * i + 1], C.y, y));
+                    for (uint32_t j = 0; j < 4; ++j)
+                        if (channel(j) < chs) cp_async16(to + j * 4096 + tid * 16, src + j * 1024, true);
+                    constexpr uint32_t kUnits = L::kRow / 16;
+                    for (uint32_t x = tid; x < 3 * kUnits + N / 4; x += kStep) {
+                        const uint32_t part = x / kUnits, unit = x % kUnits;
+                        if (x >= 3 * kUnits) {             // B, then C
+                            const uint32_t y = x - 3 * kUnits, e = y % (N / 8);
+                            cp_async16(to + L::oBc + y * 16, (y < N / 8 ? a.b + k * a.bs : a.c + k * a.cs) + grp * N * 2 + e * 16, true);
+                        } else if (unit * 8 < chs && (part < 2 || a.z)) {
+                            const uint8_t *row = part == 0 ? a.u + k * a.us : part == 1 ? a.d + k * a.ds : a.z + k * a.zs;
+                            cp_async16(to + L::oRows + x * 16, row + (ch0 + unit * 8) * 2, true);
+                        }
+                    }
                 }
-                float *to = block[e] + (unsigned long long)ch * N + s;
-                *reinterpret_cast<float4 *>(to) = make_float4(h[0], h[1], h[2], h[3]);
-                *reinterpret_cast<float4 *>(to + 4) = make_float4(h[4], h[5], h[6], h[7]);
             }
+            cp_async_commit();
+            ++next;
+            in = in + 1 == L::kStages ? 0 : in + 1;
+        };
 #pragma unroll
-            for (int o = LANES / 2; o; o >>= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
-            if (there && s == 0) {
-                y = fmaf(r.skip, u, y);
-                if (a.z) y *= silu(T::unpack(r.z[e]).x);
-                *reinterpret_cast<uint16_t *>(a.out + (k0 + e) * a.os + ch * 2) = (uint16_t)T::pack(y, 0.f);
+        for (uint32_t x = 0; x < L::kStages - 1; ++x) load();
+        // Repeated slots, a warp an entry, while the first copies are on their way.  (What is copied for one is not looked at.)
+        for (uint32_t i = w; i < count; i += kStep / 32) {
+            const uint32_t k = from + i, r = a.reqs[k];
+            bool dup = false;
+            for (uint32_t j = lane; j < k; j += 32) dup |= a.reqs[j] == r;
+            dup = __any_sync(0xFFFFFFFFu, dup);
+            if (lane == 0) {
+                if ((dup || !blocks[i]) && tile == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
+                if (dup) blocks[i] = nullptr;
             }
         }
-    };
-    const uint32_t ch0 = blockIdx.y * rounds * CB + threadIdx.x / LANES;
-    Round r[2];
-    fetch(r[0], ch0);
+        uint32_t out = 0;
+        for (uint32_t i = 0; i < count; ++i) {
+            cp_async_wait<L::kStages - 2>();
+            __syncthreads();                       // this stage is there, and the one before has been read
+            load();
+            const uint8_t *st = smem + out * L::kStage;
+            out = out + 1 == L::kStages ? 0 : out + 1;
+            float *block = blocks[i];
+            if (!block) continue;
+            const unsigned long long k = from + i;
+            auto row = [&](uint32_t part, uint32_t ch) { return T::unpack(*reinterpret_cast<const uint16_t *>(st + L::oRows + part * L::kRow + ch * 2)).x; };
+            float u[OWN], d[OWN], du[OWN];
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {      // while the first loads are on their way
-        if (k0 + e >= a.n) continue;
-        if (named_before(a.reqs, k0 + e, a.reqs[k0 + e])) block[e] = nullptr;
-        if (!block[e] && blockIdx.y == 0 && threadIdx.x == 0) record_error(g.st, AVMP_DEV_BAD_REQUEST);
-    }
-    for (uint32_t i = 0; i < rounds; i += 2) {
-        fetch(r[1], ch0 + (i + 1) * CB);
-        work(r[0], ch0 + i * CB);
-        fetch(r[0], ch0 + (i + 2) * CB);
-        work(r[1], ch0 + (i + 1) * CB);
+            for (uint32_t o = 0; o < OWN; ++o) {
+                u[o] = row(0, channel(j0 + o));
+                d[o] = row(1, channel(j0 + o)) + bias[o];
+                if (a.softplus) d[o] = softplus(d[o]);
+                du[o] = d[o] * u[o];
+            }
+            const uint2 bb = *reinterpret_cast<const uint2 *>(st + L::oBc + q * 8), cc = *reinterpret_cast<const uint2 *>(st + L::oBc + N * 2 + q * 8);
+            auto pair = [](uint32_t v) { const float2 x = T::unpack(v); return pack2(x.x, x.y); };
+            const unsigned long long B[2] = {pair(bb.x), pair(bb.y)}, C[2] = {pair(cc.x), pair(cc.y)};
+            float *to = block + (unsigned long long)ch0 * N + tid * 4;
+            float y[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t owner = lane - q + (LANES < 4 ? j / 2 : j);
+                const float step = __shfl_sync(0xFFFFFFFFu, d[LANES < 4 ? j % 2 : 0], owner), add = __shfl_sync(0xFFFFFFFFu, du[LANES < 4 ? j % 2 : 0], owner);
+                const ulonglong2 h0 = *reinterpret_cast<const ulonglong2 *>(st + j * 4096 + tid * 16);
+                const float2 e0 = unpack2(mul2(A[j][0], both(step))), e1 = unpack2(mul2(A[j][1], both(step)));
+                ulonglong2 h;
+                h.x = fma2(pack2(exp2_approx(e0.x), exp2_approx(e0.y)), h0.x, mul2(both(add), B[0]));
+                h.y = fma2(pack2(exp2_approx(e1.x), exp2_approx(e1.y)), h0.y, mul2(both(add), B[1]));
+                if (channel(j) < chs) *reinterpret_cast<ulonglong2 *>(to + j * 1024) = h;
+                const float2 z = unpack2(fma2(h.x, C[0], mul2(h.y, C[1])));
+                y[j] = z.x + z.y;
+            }
+            // sums over the lanes of a channel: each keeps its own quarters
+#pragma unroll
+            for (uint32_t o = LANES / 2; o >= 4; o >>= 1)
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) y[j] += __shfl_xor_sync(0xFFFFFFFFu, y[j], o);
+            const bool hi = LANES < 4 ? q & 1 : q & 2, odd = q & 1;
+            constexpr uint32_t kFar = LANES < 4 ? 1 : 2;
+            const float s0 = __shfl_xor_sync(0xFFFFFFFFu, hi ? y[0] : y[2], kFar), s1 = __shfl_xor_sync(0xFFFFFFFFu, hi ? y[1] : y[3], kFar);
+            float v[2] = {(hi ? y[2] : y[0]) + s0, (hi ? y[3] : y[1]) + s1};
+            if (LANES >= 4) {
+                const float x = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[0] : v[1], 1);
+                v[0] = (odd ? v[1] : v[0]) + x;
+            }
+#pragma unroll
+            for (uint32_t o = 0; o < OWN; ++o) {
+                const uint32_t ch = channel(j0 + o);
+                float x = fmaf(skip[o], u[o], v[o]);
+                if (a.z) x *= silu(row(2, ch));
+                if (finishes && ch < chs) *reinterpret_cast<uint16_t *>(a.out + k * a.os + (ch0 + ch) * 2) = (uint16_t)T::pack(x, 0.f);
+            }
+        }
+        cp_async_wait<0>();
     }
 }
 
@@ -508,11 +564,12 @@ cudaError_t prompt_type(const Geom &g, const ScanArgs &a, const Launch &l, uint3
 template <class T, int N>
 cudaError_t step_launch(const Geom &g, const ScanArgs &a, const Launch &l)
 {
-    const uint32_t cb = kCta / (N / 8), parts = (a.channels + cb - 1) / cb, groups = (a.n + kEntries - 1) / kEntries;
-    // 8 rounds amortise a CTA's look-ups; fewer where that leaves SMs idle
-    uint32_t rounds = 8;
-    while (rounds > 2 && (unsigned long long)groups * ((parts + rounds - 1) / rounds) < 8ull * l.n_sms) rounds >>= 1;
-    return launch_pdl(scan_step_kernel<T, N>, dim3(groups, (parts + rounds - 1) / rounds), dim3(kCta), 0, l.stream, g, a, rounds);
+    using L = StepTile<N>;
+    const cudaError_t e = allow_smem<scan_step_kernel<T, N>>(l.device, L::kTotal);
+    if (e != cudaSuccess) return e;
+    const uint32_t tiles_group = (a.channels / a.groups + L::CH - 1) / L::CH;
+    const unsigned long long pairs = (unsigned long long)a.groups * tiles_group * a.n, ctas = (unsigned long long)l.n_sms * (L::kTotal > 72 * 1024 ? 2 : 3);
+    return launch_pdl(scan_step_kernel<T, N>, dim3((uint32_t)min(pairs, ctas)), dim3(kStep), L::kTotal, l.stream, g, a, tiles_group);
 }
 template <class T>
 cudaError_t step_type(const Geom &g, const ScanArgs &a, const Launch &l)
