@@ -532,15 +532,22 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                     for (int c = 0; c < 128; c += 32) tmem_ld32(u + c, ts + c);
                     tmem_wait_ld();
                     float *s = reinterpret_cast<float *>(u);
-                    if (__any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
+                    if (!WINDOW && __any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1)) {
                         const int lim = sees >= j * kKv ? (int)min(sees - j * kKv, 127u) : -1;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) s[c] = c <= lim ? s[c] : -INFINITY;
                     }
-                    if (WINDOW && __any_sync(0xFFFFFFFFu, low > j * kKv && low > p.a.sinks)) {
-                        const int from = low > j * kKv ? (int)min(low - j * kKv, 128u) : 0, sinks = p.a.sinks > j * kKv ? (int)min(p.a.sinks - j * kKv, 128u) : 0;
+                    if (WINDOW && __any_sync(0xFFFFFFFFu, sees < j * kKv + kKv - 1 || (low > j * kKv && low > p.a.sinks))) {
+                        // columns up to the row's own, and of them those in its window or among the sinks: a bit each, 32 at a time
+                        auto count = [&](uint32_t x) { return x > j * kKv ? (int)min(x - j * kKv, (uint32_t)kKv) : 0; };
+                        auto below = [](int x) { return x <= 0 ? 0u : 0xFFFFFFFFu >> (32 - min(x, 32)); };
+                        const int seen = count(sees + 1), from = count(low), sinks = count(p.a.sinks);
 #pragma unroll
-                        for (int c = 0; c < 128; ++c) s[c] = c >= from || c < sinks ? s[c] : -INFINITY;
+                        for (int c = 0; c < 128; c += 32) {
+                            const uint32_t bits = below(seen - c) & (~below(from - c) | below(sinks - c));
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) s[c + e] = bits >> e & 1 ? s[c + e] : -INFINITY;
+                        }
                     }
                     float x0 = s[0], x1 = s[1], x2 = s[2], x3 = s[3];
 #pragma unroll
