@@ -456,7 +456,7 @@ AVMP_API int avmp_ssm_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_ssm_des
  *     y_t = bias + sum_j weight[j] x_(t - width + 1 + j),   out_t = y_t, or y_t / (1 + exp(-y_t)) with silu 1.
  * Rows of x and out: [channels].  weight: fp32 [channels][width], 16-byte aligned; bias: fp32 [channels], 16-byte aligned, or NULL.  The
  * window elements of the SSM blocks are the last width - 1 rows of a request, oldest first, [width - 1][channels] in fp32.
- * Supported: ssm_elem_bytes 4, width 2, 3 or 4, channels a multiple of 8, ssm_conv_elems = channels * (width - 1), ssm_state_elems a
+ * Supported: ssm_elem_bytes 4, width 2, 3 or 4, channels a multiple of 8 up to 2^24, ssm_conv_elems = channels * (width - 1), ssm_state_elems a
  * multiple of 4; else AVMP_EINVAL.  The state elements of the block are not touched. */
 typedef struct {
     uint32_t type, channels, width, silu;
@@ -478,8 +478,8 @@ AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_d
  * Rows: u, delta, z and out [channels], b and c [groups][states]; channel i reads group i / (channels / groups).
  * A: fp32 [channels][states], 16-byte aligned, finite (at most 0 where steps are positive, or states grow without bound); D and delta_bias: fp32
  * [channels] or NULL (0); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state.
- * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups, ssm_state_elems = channels * states; else
- * AVMP_EINVAL.  The convolution window of the block is not touched. */
+ * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups up to 2^24, ssm_state_elems = channels *
+ * states; else AVMP_EINVAL.  With softplus a delta of -inf or of the type's lowest value leaves the state as it was.  The convolution window of the block is not touched. */
 typedef struct {
     uint32_t type, channels, groups, states, softplus;
     uint32_t rsvd;             /* 0 */

@@ -158,7 +158,7 @@ bool conv_desc_ok(const avmp_ctx *c, const avmp_conv_desc *d)
 {
     const avmp_model_spec &m = c->spec;
     if (!d || d->type > AVMP_TYPE_F16 || d->silu > 1 || m.ssm_elem_bytes != 4 || m.n_ssm_layers == 0 || m.ssm_state_elems % 4) return false;
-    if (d->width < 2 || d->width > 4 || d->channels == 0 || d->channels % 8) return false;
+    if (d->width < 2 || d->width > 4 || d->channels == 0 || d->channels % 8 || d->channels > 1u << 24) return false;
     if ((uint64_t)d->channels * (d->width - 1) != m.ssm_conv_elems) return false;
     return stride_ok(d->x_stride_bytes, (uint64_t)d->channels * 2) && stride_ok(d->out_stride_bytes, (uint64_t)d->channels * 2);
 }
@@ -184,7 +184,7 @@ bool scan_desc_ok(const avmp_ctx *c, const avmp_scan_desc *d)
     const avmp_model_spec &m = c->spec;
     if (!d || d->type > AVMP_TYPE_F16 || d->softplus > 1 || d->rsvd || m.ssm_elem_bytes != 4 || m.n_ssm_layers == 0) return false;
     if (d->states != 8 && d->states != 16 && d->states != 32 && d->states != 64) return false;
-    if (d->channels == 0 || d->groups == 0 || d->channels % d->groups || d->channels / d->groups % 8) return false;
+    if (d->channels == 0 || d->channels > 1u << 24 || d->groups == 0 || d->channels % d->groups || d->channels / d->groups % 8) return false;
     if ((uint64_t)d->channels * d->states != m.ssm_state_elems) return false;
     const uint64_t row = (uint64_t)d->channels * 2, bc = (uint64_t)d->groups * d->states * 2;
     return stride_ok(d->u_stride_bytes, row) && stride_ok(d->delta_stride_bytes, row) && stride_ok(d->z_stride_bytes, row) &&

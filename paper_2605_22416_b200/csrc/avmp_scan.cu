@@ -25,20 +25,22 @@ ScanPlan scan_plan(uint32_t n, uint32_t channels, uint32_t groups, uint32_t stat
     const unsigned long long wide = (unsigned long long)n * scan_tiles(channels, groups, 128 / lanes);       // CTAs, two on an SM
     const unsigned long long narrow = (unsigned long long)n * scan_tiles(channels, groups, 128 * 4 / states);
     if (wide >= 3ull * n_sms) return {true, 1};
-    if (4 * narrow >= 3ull * n_sms) return {false, 1};
+    // Several prompts are seldom alike, and only their mean is known here: the longest holds an uncut call up, and is better cut finely.
+    if (4 * narrow >= (n == 1 ? 3ull : 6ull) * n_sms) return {false, 1};
     // As many runs as fill the SMs, of 128 tokens or more on the mean: what the first pass costs is two thirds of the second one.
     unsigned long long s = total / n / 128;
     if (s > 64) s = 64;
     if (narrow * s <= 2ull * n_sms) return {false, s < 3 ? 1u : (uint32_t)s};
-    if (s > 2ull * n_sms / wide) s = 2ull * n_sms / wide;
+    const unsigned long long most = (n == 1 ? 2ull : 4ull) * n_sms / wide;
+    if (s > most) s = most;
     return s < 3 ? ScanPlan{false, 1} : ScanPlan{true, (uint32_t)s};
 }
 
 constexpr int kCta = 128;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x| (its argument's rounding is made up for).  log(1 + e) / e on [0, 1] is a polynomial of
-// degree 9 fitted for least relative error (5e-9; 1.4e-7 with its roundings).
+// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x| (its argument's rounding is made up for; 0 from -100 on, infinities included).
+// log(1 + e) / e on [0, 1] is a polynomial of degree 9 fitted for least relative error (5e-9; 1.4e-7 with its roundings).
 __device__ __forceinline__ constexpr float log_poly(int i)
 {
     constexpr float c[10] = {1.f, -4.9999901652e-01f, 3.3329963684e-01f, -2.4954134226e-01f, 1.9675938785e-01f,
@@ -46,22 +48,22 @@ __device__ __forceinline__ constexpr float log_poly(int i)
     return c[i];
 }
 constexpr float kLn2 = 0.6931471806f, kLog2eLow = 1.925963033e-8f;      // log2(e) - kLog2e
+__device__ __forceinline__ float ramp(float x) { return max3_nan(x, 0.f, 0.f); }
 __device__ __forceinline__ float softplus(float x)
 {
-    const float a = -fabsf(x), t = a * kLog2e, rest = fmaf(a, kLog2eLow, fmaf(a, kLog2e, -t));
+    const float a = fmaxf(-fabsf(x), -100.f), t = a * kLog2e, rest = fmaf(a, kLog2eLow, fmaf(a, kLog2e, -t));
     float e = exp2_approx(t);
     e = fmaf(e * kLn2, rest, e);
     float y = log_poly(9);
 #pragma unroll
     for (int i = 8; i >= 0; --i) y = fmaf(y, e, log_poly(i));
-    return fmaf(y, e, fmaxf(x, 0.f));
+    return fmaf(y, e, ramp(x));
 }
 __device__ __forceinline__ unsigned long long both(float x) { return pack2(x, x); }
 // The same of a pair.
 __device__ __forceinline__ float2 softplus2(float2 x)
 {
-    const float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
-    const unsigned long long a2 = pack2(a.x, a.y), t2 = mul2(a2, both(kLog2e));
+    const unsigned long long a2 = pack2(fmaxf(-fabsf(x.x), -100.f), fmaxf(-fabsf(x.y), -100.f)), t2 = mul2(a2, both(kLog2e));
     const float2 t = unpack2(t2);
     const unsigned long long rest = fma2(a2, both(kLog2eLow), fma2(a2, both(kLog2e), pack2(-t.x, -t.y)));
     unsigned long long e = pack2(exp2_approx(t.x), exp2_approx(t.y));
@@ -69,7 +71,7 @@ __device__ __forceinline__ float2 softplus2(float2 x)
     unsigned long long y = both(log_poly(9));
 #pragma unroll
     for (int i = 8; i >= 0; --i) y = fma2(y, e, both(log_poly(i)));
-    return unpack2(fma2(y, e, pack2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f))));
+    return unpack2(fma2(y, e, pack2(ramp(x.x), ramp(x.y))));
 }
 
 // ---------------------------------------------------------------- whole prompts

@@ -438,6 +438,60 @@ def test_nonfinite_numbers_stay_in_their_channel():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("d", [16, 2048])
+def test_masked_steps(dtype, d):
+    """Tokens whose step is masked, by the type's lowest value or minus infinity, leave the state as it was; a step of NaN does not pass for one."""
+    import torch
+    dt = getattr(torch, dtype)
+    n = 16
+    m = _model(d, n, 2, layers=1)
+    ctx = _ctx(m, 4, [0, 1, 2])
+    gen = torch.Generator("cuda").manual_seed(d)
+    st, cv = _fill(ctx, 0, [0, 1, 2], m, gen, dt)
+    tot = 70
+    i = _scan_inputs(d, 1, n, tot, dt, gen)
+    i.delta[:, ::2] = -math.inf
+    i.delta[:, 1::2] = torch.finfo(dt).min
+    out = torch.empty(tot, d, dtype=dt, device="cuda")
+    desc = _scan_desc(i, d, 1, n, dt)
+    args = lambda: (i.u, i.delta, i.b, i.c, i.z, i.a, i.skip, i.bias)
+    ctx.scan_prompt(0, desc, _i32([0, 1]), 2, _i32([0, 69, 70]), tot, _i32([1, 1]), *args(), out)
+    ctx.scan_step(0, desc, _i32([2]), 1, *args(), out)
+    assert torch.equal(_states(ctx, 0, [0, 1, 2], m)[0], st) and torch.isfinite(out).all()
+    h, _, y, bound = _scan_exact(st[2].view(d, n), i.u[:1], torch.full_like(i.delta[:1], -1000.0), i.b[:1, None], i.c[:1, None], i.z[:1], i.a, i.skip, i.bias,
+                                 True)
+    _inside(out[:1], y, bound, dt, "a masked token's output")
+    i.delta[3, 5] = math.nan
+    ctx.scan_prompt(0, desc, _i32([0, 1]), 2, _i32([0, 69, 70]), tot, _i32([1, 1]), *args(), out)
+    got = _states(ctx, 0, [0], m)[0].view(d, n)
+    assert torch.isnan(got[5]).all() and torch.equal(got[:5], st[0].view(d, n)[:5]) and torch.isnan(out[3:69, 5]).all() and torch.isfinite(out[:3]).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_calls_without_rows():
+    """No rows at all, no buffers: fresh requests get zeros, continued ones keep what they have."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt = torch.bfloat16
+    d, n, w = 40, 8, 3
+    m = _model(d, n, w, layers=1)
+    ctx = _ctx(m, 4, [0, 1])
+    gen = torch.Generator("cuda").manual_seed(1)
+    st, cv = _fill(ctx, 0, [0, 1], m, gen, dt)
+    f = torch.zeros(d * n, device="cuda")
+    none = [None] * 5
+    ctx.conv_prompt(0, B.conv_desc(channels=d, width=w, silu=True, dtype=dt), _i32([0, 1]), 2, _i32([0, 0, 0]), 0, _i32([1, 0]), None, f, None, None)
+    ctx.scan_prompt(0, B.scan_desc(channels=d, groups=1, states=n, softplus=True, dtype=dt), _i32([0, 1]), 2, _i32([0, 0, 0]), 0, _i32([1, 0]), *none, f,
+                    None, None, None)
+    st2, cv2 = _states(ctx, 0, [0, 1], m)
+    assert torch.equal(st2[0], st[0]) and torch.equal(cv2[0], cv[0]) and not st2[1].any() and not cv2[1].any()
+    assert ctx.stats()["error_count"] == 0
+    ctx.close()
+
+
+@pytest.mark.gpu
 def test_long_lists_and_offsets():
     """More entries than a CTA has threads, with repeated slots: the first of each stands."""
     import torch
