@@ -90,7 +90,7 @@ struct Tile {
     static constexpr int Q = N / S, P = S / 2;
     static constexpr int J = P > 4 ? 1 : P > 2 ? 2 : 4;              // tokens that are worked out ahead of the state
     static constexpr int W = 32 / Q, CB = kCta / 32 * W;             // channels of a warp and of a CTA
-    static constexpr int kTok = Q == 1 ? 16 : 32;                    // tokens of a tile
+    static constexpr int kTok = Q == 1 ? 8 : 32;                     // tokens of a tile (a lane with all states: 1 400 us with 8, 1 459 with 16, 32 prompts of 1000; else 266 with 32, 281 with 16, one of 4096)
     static constexpr uint32_t kRow = CB * 2, kRows = kTok * kRow, kBc = kTok * N * 2;
     static constexpr uint32_t kStage = 3 * kRows + 2 * kBc;          // u, d, z, B, C
     static constexpr uint32_t kSteps = kTok * CB * 8;                // (D, D u), [token][channel]
