@@ -3,8 +3,13 @@
 // (h, A: [channels][states]; u, d, z, out: a row per token and channel; B, C: a row per token and group of channels).
 //
 // scan_prompt_kernel   whole prompts.  Bound by the exponentials: one per token, channel and state, of which the special-function unit gives
-//                      16 a cycle and SM; the rows are 8 bytes a channel.
-// scan_step_kernel     one token per request: bound by HBM, every state element is read and written once.
+//                      16 a cycle and SM, and three more per token and channel; the rows are 8 bytes a channel.  Measured (16 states): 32 prompts of
+//                      1000 tokens, 8192 channels, 1 400 us (that unit is busy 77 % of the time, 61 % of the issue slots are taken; bytes alone
+//                      322); one of 4096 tokens 266 (60 %: 256 CTAs on 148 SMs, two warps of the scan to a scheduler); 32 of 32 to 512
+//                      tokens, 2048 channels, 84.  An eighth of the exponentials as polynomials on the multiply-add pipe 3 % slower, a quarter 8 %:
+//                      the issue slots are short too.
+// scan_step_kernel     one token per request: bound by HBM, every state element is read and written once.  1 GB of state 395 to 415 us (84 to 88 % of
+//                      the measured copy rate); 32 requests of 128 KB 4.6 (latency).
 #include "avmp_lists.cuh"
 #include "avmp_tc.cuh"
 
@@ -378,7 +383,8 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
 // The work is the list of all (tile, entry) pairs, a tile being 16 KB of states (4096 / N channels of a group); each CTA has a share of it, so that
 // a tile's decays stay in registers over many entries.  A thread has four float4 of a tile, one in each quarter: accesses cover whole
 // lines, and steps, gates and outputs are worked out by a lane each, the lanes of a channel sharing out the four.  States and rows come
-// through a ring in shared memory, so that their number in flight costs no registers.
+// through a ring in shared memory, so that their number in flight costs no registers.  (1 GB of state, loads into registers: 448 us with
+// 40 warps on an SM, 463 with the next round's ahead, 555 with four entries at a time.)
 constexpr int kStep = 256;
 constexpr uint32_t kBatch = 256;      // entries whose blocks are looked up at a time
 
