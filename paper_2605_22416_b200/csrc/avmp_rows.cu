@@ -121,12 +121,22 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
         }
         uint32_t place_out = 0;
         auto heads_of = [&](uint8_t *to, uint32_t heads, uint32_t stages, const float *weight) {
-            // a pair (p, o) becomes by * (p pc - o os, o oc + p ps)
-            float pc[4], os[4], oc[4], ps[4];
+            // A pair (p, o) becomes by * (p pc - o os, o oc + p ps).  Two numbers go through the multiply-add pipe at a time: two pairs' p or o
+            // where they lie so (halves), else one pair.
+            unsigned long long straight[4], cross[4];
+            {
+                float pc[4], os[4], oc[4], ps[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float wp = weight ? weight[NEIGHBOURS ? f + 2 * j : f + j] : 1.f, wo = weight ? weight[NEIGHBOURS ? f + 2 * j + 1 : s + j] : 1.f;
-                pc[j] = wp * cs[j]; os[j] = wo * sn[j]; oc[j] = wo * cs[j]; ps[j] = wp * sn[j];
+                for (int j = 0; j < 4; ++j) {
+                    const float wp = weight ? weight[NEIGHBOURS ? f + 2 * j : f + j] : 1.f, wo = weight ? weight[NEIGHBOURS ? f + 2 * j + 1 : s + j] : 1.f;
+                    pc[j] = wp * cs[j]; os[j] = -wo * sn[j]; oc[j] = wo * cs[j]; ps[j] = wp * sn[j];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int x = 2 * (j % 2);
+                    straight[j] = NEIGHBOURS ? pack2(pc[j], oc[j]) : j < 2 ? pack2(pc[x], pc[x + 1]) : pack2(oc[x], oc[x + 1]);
+                    cross[j] = NEIGHBOURS ? pack2(os[j], ps[j]) : j < 2 ? pack2(os[x], os[x + 1]) : pack2(ps[x], ps[x + 1]);
+                }
             }
             uint32_t h = h0;
             for (uint32_t x = 0; x < stages; ++x) {
@@ -136,32 +146,30 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
                 for (int e = 0; e < kSteps; ++e, h += h_step) {
                     const uint4 in4 = ring[place_out * kSteps + e][threadIdx.x];
                     const uint32_t in[4] = {in4.x, in4.y, in4.z, in4.w};
-                    float y[8];
+                    unsigned long long y[4], sum = 0;          // columns f, f + 1; f + 2, f + 3; s, s + 1; s + 2, s + 3
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float2 z = T::unpack(in[j]);
-                        y[2 * j] = z.x; y[2 * j + 1] = z.y;
+                        y[j] = pack2(z.x, z.y);
+                        sum = j ? fma2(y[j], y[j], sum) : mul2(y[j], y[j]);
                     }
                     float by = 1.f;
                     if (weight) {
-                        float sq = y[0] * y[0];
-#pragma unroll
-                        for (int j = 1; j < 8; ++j) sq = fmaf(y[j], y[j], sq);
+                        const float2 z = unpack2(sum);
+                        float sq = z.x + z.y;
 #pragma unroll
                         for (uint32_t o = LANES / 2; o; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
                         by = rsqrtf(sq * (1.f / D) + a.eps);
                     }
                     uint32_t out[4];
-                    float re[4], im[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float p = y[NEIGHBOURS ? 2 * j : j], o = y[NEIGHBOURS ? 2 * j + 1 : j + 4];
-                        re[j] = by * (p * pc[j] - o * os[j]); im[j] = by * (o * oc[j] + p * ps[j]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (NEIGHBOURS) { out[2 * j] = T::pack(re[2 * j], im[2 * j]); out[2 * j + 1] = T::pack(re[2 * j + 1], im[2 * j + 1]); }
-                        else { out[j] = T::pack(re[2 * j], re[2 * j + 1]); out[2 + j] = T::pack(im[2 * j], im[2 * j + 1]); }
+                        const float2 z = unpack2(y[j]);
+                        const unsigned long long other = NEIGHBOURS ? pack2(z.y, z.x) : y[(j + 2) % 4];
+                        unsigned long long v = mul2(y[j], straight[j]);
+                        if (turns) v = fma2(other, cross[j], v);       // (columns that are not rotated have no partner to take an infinity from)
+                        const float2 r = unpack2(mul2(v, pack2(by, by)));
+                        out[j] = T::pack(r.x, r.y);
                     }
                     if (h < heads) write(to + h * (D * 2), make_uint4(out[0], out[1], out[2], out[3]));
                 }

@@ -530,3 +530,50 @@ def test_long_lists_and_offsets():
         assert torch.equal(cv2[r].view(w - 1, d).double(), new)
     assert ctx.stats()["error_count"] == 4
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_prompts_in_a_graph():
+    """Convolution and a scan cut into runs, captured together and replayed on another stream: the same, bit for bit, as the calls made one by one;
+    continued from where the replay before ended."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt = torch.bfloat16
+    d, n, w, tot = 64, 16, 4, 2000
+    m = _model(d, n, w, layers=1)
+    ctx = _ctx(m, 4, [0, 2])
+    gen = torch.Generator("cuda").manual_seed(9)
+    st, cv = _fill(ctx, 0, [0, 2], m, gen, dt)
+    i = _scan_inputs(d, 1, n, tot, dt, gen)
+    weight = torch.randn(d, w, device="cuda", generator=gen)
+    conv = B.conv_desc(channels=d, width=w, silu=True, dtype=dt, x_stride_bytes=i.us)
+    scan = B.scan_desc(channels=d, groups=1, states=n, softplus=True, dtype=dt, delta_stride_bytes=i.ds, z_stride_bytes=i.zs, b_stride_bytes=i.bs,
+                       c_stride_bytes=i.bs)
+    size = ctx.scan_workspace_bytes(scan, 2, tot)
+    assert size > 0
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    reqs, cu, resume = _i32([2, 0]), _i32([0, 1500, tot]), _i32([1, 1])
+    mid, out = (torch.empty(tot, d, dtype=dt, device="cuda") for _ in range(2))
+
+    def both():
+        ctx.conv_prompt(0, conv, reqs, 2, cu, tot, resume, i.u, weight, None, mid)
+        ctx.scan_prompt(0, scan, reqs, 2, cu, tot, resume, mid, i.delta, i.b, i.c, i.z, i.a, i.skip, i.bias, out, ws, size)
+
+    want = []
+    for _ in range(2):
+        both()
+        want.append((mid.clone(), out.clone(), *_states(ctx, 0, [0, 2], m)))
+    ctx.scatter_ssm(0, _i32([0, 2]), 2, st, cv)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        both()
+    for k in range(2):
+        mid.zero_(), out.zero_(), ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip((mid, out, *_states(ctx, 0, [0, 2], m)), want[k])), k
+    assert ctx.stats()["error_count"] == 0
+    ctx.close()

@@ -165,6 +165,30 @@ def test_rows_bad_items_and_refusals():
     c.ctx.close()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_rows_infinities_stay_in_their_pair(neighbours):
+    """Without norms: an infinity in a rotated column is seen in its pair, one in a column that is not rotated in that column alone."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    c = Cache([3], 2, 64, 16, "bfloat16")
+    q, k, v = (torch.randn(3, h, 64, device="cuda", generator=c.gen).to(c.dt) for h in (4, 2, 2))
+    freq = torch.rand(16, device="cuda", generator=c.gen) + 0.1
+    out = torch.empty(3, 4, 64, dtype=c.dt, device="cuda")
+    desc = B.rows_desc(q_heads=4, rotary_dim=32, neighbours=neighbours, eps=0.0, dtype=c.dt)
+    bad = {(1, 0, 3), (2, 1, 40), (2, 3, 63)}
+    for t, h, col in bad:
+        q[t, h, col] = math.inf
+    c.ctx.attn_rows_prompt(c.layer, desc, _i32([0]), 1, _i32([0, 3]), 3, None, q, k, v, None, None, freq, out)
+    hit = torch.zeros(3, 4, 64, dtype=torch.bool, device="cuda")
+    hit[1, 0, [2, 3] if neighbours else [3, 19]] = True
+    hit[2, 1, 40] = hit[2, 3, 63] = True
+    assert torch.equal(~torch.isfinite(out), hit) and out[2, 1, 40] == math.inf
+    want, bound = _rotated(torch.where(hit, 0, q), None, 0, torch.arange(3, device="cuda"), freq, neighbours)
+    _near(torch.where(hit, 0, out), torch.where(hit, 0, want), bound, "the others")
+    c.ctx.close()
+
+
 # ---------------------------------------------------------------- window
 def _exact(q, kv, scale, past, window, sinks):
     import torch
