@@ -100,7 +100,9 @@ struct Tile {
     static constexpr uint32_t kStage = 3 * kRows + 2 * kBc;          // u, d, z, B, C
     static constexpr uint32_t kSteps = kTok * CB * 8;                // (D, D u), [token][channel]
     static constexpr uint32_t kWide = 2 * kTok * N * 4;              // B and C in 32 bits, [B or C][token][state]
-    static constexpr uint32_t kOut = kTok * CB * 4;                  // sums over the states, [token][channel]
+    // sums over the states, [token][channel]; where four lanes share a channel, of each of them: the warps around the scan add them up
+    static constexpr bool kApart = Q == 4 && S == 4;                 // (with more states there is no room for two CTAs on an SM then)
+    static constexpr uint32_t kParts = kApart ? 4 : 1, kPart = kTok * CB * 4 + (kApart ? 32 : 0), kOut = kParts * kPart;
     static constexpr uint32_t oSteps = kStages * kStage, oWide = oSteps + 2 * kSteps, oOut = oWide + 2 * kWide, kTotal = oOut + 2 * kOut;
 };
 
@@ -217,6 +219,11 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
             for (uint32_t t = myrow; t < kTok; t += kPass) {
                 const uint32_t e = (t * CB + mych) * 2;
                 float4 o = from[e / 8];
+#pragma unroll
+                for (uint32_t x = 1; x < L::kParts; ++x) {
+                    const float4 v = from[x * (L::kPart / 16) + e / 8];
+                    o = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+                }
                 if (a.skip) {
                     const float4 u = unpack4(*reinterpret_cast<const uint2 *>(at + e));
                     o = make_float4(fmaf(skip.x, u.x, o.x), fmaf(skip.y, u.y, o.y), fmaf(skip.z, u.z, o.z), fmaf(skip.w, u.w, o.w));
@@ -296,7 +303,7 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
     for (uint32_t i = 0; i < n_tiles; ++i) {
         const uint8_t *st = smem + L::oSteps + (i & 1) * L::kSteps + mych * 8;
         const unsigned long long *bq = reinterpret_cast<const unsigned long long *>(smem + L::oWide + (i & 1) * L::kWide) + q * P, *cq = bq + kTok * N / 2;
-        float *to = reinterpret_cast<float *>(smem + L::oOut + (i & 1) * L::kOut) + mych;
+        float *to = reinterpret_cast<float *>(smem + L::oOut + (i & 1) * L::kOut + (L::kApart ? q * L::kPart : 0u)) + mych;
         // Some tokens' decays, additions and C, worked out while those before go through the state: a warp may be alone on its scheduler, and
         // nothing but the state itself then waits for what is in front of it.
         struct Ahead {
@@ -329,10 +336,10 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
                 y[j] = z.x + z.y;
             }
         };
-        // sums of four tokens over the lanes of a channel; where there are four, each keeps one
+        // sums of four tokens over the lanes of a channel; where there are four or more, four of them keep one each
         auto put = [&](float (&y)[4], int t) {
             if (locals) return;
-            if (Q == 1) {
+            if (Q == 1 || L::kApart) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) to[(t + j) * CB] = y[j];
                 return;
