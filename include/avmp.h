@@ -476,6 +476,8 @@ AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_d
  *     step = delta_t + delta_bias, with softplus 1: log(1 + exp(that));
  *     h <- exp(step * A) h + step * u_t * B_t,   y = <C_t, h> + D * u_t,   out_t = y * z_t / (1 + exp(-z_t)).
  * Rows: u, delta, z and out [channels], b and c [groups][states]; channel i reads group i / (channels / groups).
+ * An exponential is off by 2^-22 of its value at most and by 3e-8 on the mean where a state decays slowly, always to the same side; that adds up
+ * over the tokens that a state remembers: about 8e-6 of it where they are up to a thousand, 2e-4 where they are twenty thousand.
  * A: fp32 [channels][states], 16-byte aligned, finite (at most 0 where steps are positive, or states grow without bound); D and delta_bias: fp32
  * [channels] or NULL (0); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state.
  * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups up to 2^24, ssm_state_elems = channels *

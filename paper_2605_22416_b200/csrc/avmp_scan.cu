@@ -5,8 +5,8 @@
 // scan_prompt_kernel   whole prompts.  Bound by the exponentials: one per token, channel and state, of which the special-function unit gives
 //                      16 a cycle and SM, and three more per token and channel; the rows are 8 bytes a channel.  Measured (16 states): 32 prompts of
 //                      1000 tokens, 8192 channels, 1 400 us (that unit is busy 77 % of the time, 61 % of the issue slots are taken; bytes alone
-//                      322); one of 4096 tokens 266 (60 %: 256 CTAs on 148 SMs, two warps of the scan to a scheduler); 32 of 32 to 512
-//                      tokens, 2048 channels, 84.  An eighth of the exponentials as polynomials on the multiply-add pipe 3 % slower, a quarter 8 %:
+//                      322); one of 4096 tokens 258 (60 %: 256 CTAs on 148 SMs, two warps of the scan to a scheduler); 32 of 32 to 512
+//                      tokens, 2048 channels, 83.  An eighth of the exponentials as polynomials on the multiply-add pipe 3 % slower, a quarter 8 %:
 //                      the issue slots are short too.
 // scan_step_kernel     one token per request: bound by HBM, every state element is read and written once.  1 GB of state 395 to 415 us (84 to 88 % of
 //                      the measured copy rate); 32 requests of 128 KB 4.6 (latency).
@@ -95,12 +95,13 @@ struct Tile {
     static constexpr int Q = N / S, P = S / 2;
     static constexpr int J = P > 4 ? 1 : P > 2 ? 2 : 4;              // tokens that are worked out ahead of the state
     static constexpr int W = 32 / Q, CB = kCta / 32 * W;             // channels of a warp and of a CTA
-    static constexpr int kTok = Q == 1 ? 8 : 32;                     // tokens of a tile (a lane with all states: 1 400 us with 8, 1 459 with 16, 32 prompts of 1000; else 266 with 32, 281 with 16, one of 4096)
+    static constexpr int kTok = Q == 1 ? 8 : 32;                     // tokens of a tile (a lane with all states: 1 400 us with 8, 1 459 with 16, 32 prompts of 1000; else 266 with 32, 281 with 16, one of 4096, before kApart)
     static constexpr uint32_t kRow = CB * 2, kRows = kTok * kRow, kBc = kTok * N * 2;
     static constexpr uint32_t kStage = 3 * kRows + 2 * kBc;          // u, d, z, B, C
     static constexpr uint32_t kSteps = kTok * CB * 8;                // (D, D u), [token][channel]
     static constexpr uint32_t kWide = 2 * kTok * N * 4;              // B and C in 32 bits, [B or C][token][state]
     // sums over the states, [token][channel]; where four lanes share a channel, of each of them: the warps around the scan add them up
+    // (one of 4096 tokens 258 us, 266 with the sums put together across lanes by the warps that scan)
     static constexpr bool kApart = Q == 4 && S == 4;                 // (with more states there is no room for two CTAs on an SM then)
     static constexpr uint32_t kParts = kApart ? 4 : 1, kPart = kTok * CB * 4 + (kApart ? 32 : 0), kOut = kParts * kPart;
     static constexpr uint32_t oSteps = kStages * kStage, oWide = oSteps + 2 * kSteps, oOut = oWide + 2 * kWide, kTotal = oOut + 2 * kOut;
