@@ -812,9 +812,9 @@ int avmp_conv_step(avmp_ctx *c, uint32_t layer, const avmp_conv_desc *desc, cons
 size_t avmp_scan_workspace_bytes(const avmp_ctx *c, const avmp_scan_desc *desc, uint32_t n, uint32_t total_tokens)
 {
     if (!c || !scan_desc_ok(c, desc)) return 0;
-    // Fewer requests are cut into more runs; from n_sms requests up none is (see scan_plan).
+    // Fewer requests are cut into more runs; with more than 4 n_sms / 3 none is cut (see scan_plan: three runs each would pass 4 n_sms).
     size_t most = 0;
-    for (uint32_t k = 1; k <= n && k <= (uint32_t)c->n_sms; ++k) {
+    for (uint32_t k = 1; k <= n && k <= 4 * (uint32_t)c->n_sms / 3; ++k) {
         const size_t b = scan_ws_bytes(c, desc, k, total_tokens);
         if (b > most) most = b;
     }

@@ -577,3 +577,32 @@ def test_prompts_in_a_graph():
         assert all(torch.equal(p, q) for p, q in zip((mid, out, *_states(ctx, 0, [0, 2], m)), want[k])), k
     assert ctx.stats()["error_count"] == 0
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d,states,tot", [(197, 32, 16, 197 * 384), (151, 24, 8, 58086), (167, 8, 16, 64246), (98, 32, 16, 98 * 800)])
+def test_scratch_of_many_requests_that_are_cut(n, d, states, tot):
+    """Many requests (at times more than SMs), each cut into runs: the call stays within the scratch that the query asks for."""
+    import torch
+    dt = torch.bfloat16
+    m = _model(d, states, 4, layers=1)
+    ctx = _ctx(m, n, range(n))
+    gen = torch.Generator("cuda").manual_seed(n)
+    st, _ = _fill(ctx, 0, range(n), m, gen, dt)
+    i = _scan_inputs(d, 1, states, tot, dt, gen)
+    desc = _scan_desc(i, d, 1, states, dt)
+    size, guard = ctx.scan_workspace_bytes(desc, n, tot), 1 << 20
+    assert size > 0
+    ws = torch.full((size + guard,), 0x5A, dtype=torch.uint8, device="cuda")
+    cu = np.linspace(0, tot, n + 1).astype(np.int64)
+    out = torch.empty(tot, d, dtype=dt, device="cuda")
+    ctx.scan_prompt(0, desc, _i32(range(n)), n, _i32(cu), tot, _i32([1] * n), i.u, i.delta, i.b, i.c, i.z, i.a, i.skip, i.bias, out, ws, size)
+    st2, _ = _states(ctx, 0, range(n), m)
+    assert (ws[size:] == 0x5A).all()
+    for e in (0, n - 1):
+        r = slice(cu[e], cu[e + 1])
+        h, err, y, bound = _scan_exact(st[e].view(d, states), i.u[r], i.delta[r], i.b[r, None], i.c[r, None], i.z[r], i.a, i.skip, i.bias, True)
+        _inside(st2[e].view(d, states), h, err, None, f"state {e}")
+        _inside(out[r], y, bound, dt, f"rows of {e}")
+    assert ctx.stats()["error_count"] == 0
+    ctx.close()
