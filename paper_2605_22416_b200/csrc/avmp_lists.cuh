@@ -25,7 +25,7 @@ __device__ __forceinline__ bool named_before(const uint32_t *reqs, uint32_t k, u
 }
 
 // The same for entries k .. k + each - 1 (each <= 4; those behind the n-th are not looked at): a bit for each.  `flags` is a word of
-// shared memory.  Whole CTA.
+// shared memory; a barrier has to stand between two calls.  Whole CTA.
 __device__ __forceinline__ uint32_t named_before_each(const uint32_t *reqs, uint32_t k, uint32_t each, uint32_t n, uint32_t *flags)
 {
     const uint32_t last = min(n, k + each);

@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
             if (!runs.seek(i, &k, &run)) break;
         } else {
             if (i * rows >= a.n) break;
+            if (i != blockIdx.x) __syncthreads();      // `flags` of the entries before have been read
             k = (uint32_t)i * rows + w % rows; run = 0;
         }
         const bool listed = k < a.n;
