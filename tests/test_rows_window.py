@@ -479,3 +479,43 @@ def test_hybrid_layers_over_a_prompt_and_tokens(dtype):
         # a key may be rounded the other way than here: eps/2 of a score's terms, next to the roundings of the weights
         assert float((o.double() - want).norm() / want.norm()) <= 4 * torch.finfo(dt).eps / 2, "attention"
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_long_lists_of_single_tokens(dtype):
+    """Lists of more entries than a CTA looks after or plans by itself, with a slot out of range and repeated slots: the first of each is written."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    n, hk, hq, dim, window, sinks = 1600, 1, 2, 64, 9, 2
+    rng = np.random.default_rng(4)
+    held = [int(h) for h in rng.integers(1, 40, n)]
+    c = Cache(held, hk, dim, 16, dtype, seed=1)
+    reqs = rng.permutation(n)
+    reqs[1100], reqs[7], reqs[1599] = 70000, reqs[5], reqs[300]
+    bad = [7, 1100, 1599]
+    q, k, v = (torch.randn(n, h, dim, device="cuda", generator=c.gen).to(c.dt) for h in (hq, hk, hk))
+    freq = torch.rand(dim // 2, device="cuda", generator=c.gen)
+    out = torch.full((n, hq, dim), 7.0, dtype=c.dt, device="cuda")
+    c.ctx.attn_rows_step(c.layer, B.rows_desc(q_heads=hq, rotary_dim=dim, neighbours=False, eps=1e-6, dtype=c.dt), _i32(reqs), n, None, q, k, v,
+                         None, None, freq, out)
+    good = torch.tensor([e for e in range(n) if e not in bad], device="cuda")
+    place = torch.tensor([held[r] - 1 if r < n else 0 for r in reqs], device="cuda")
+    assert (out[bad] == 7).all() and c.ctx.stats()["error_count"] == 3
+    want, bound = _rotated(q, None, 0, place, freq, False)
+    _near(out[good], want[good], bound[good], "queries")
+    want_k, bound_k = _rotated(k, None, 0, place, freq, False)
+    c.ctx.clear_error()
+    desc = B.attn_desc(q_heads=hq, dtype=c.dt, scale=dim ** -0.5)
+    ws, size = c.workspace(desc, n)
+    seen, lse = torch.full((n, hq, dim), 7.0, dtype=c.dt, device="cuda"), torch.empty(n, hq, device="cuda")
+    c.ctx.attn_window_decode(c.layer, desc, window, sinks, _i32(reqs), n, out, seen, lse, ws, size)
+    assert c.ctx.stats()["error_count"] == 1 and (seen[1100] == 7).all()
+    for e in (0, 4, 5, 6, 300, 301, 777, 1099, 1101, 1598):
+        r = int(reqs[e])
+        kk, vv = _cached(c, r)
+        assert torch.equal(kk[:-1], c.rows[r][0][:-1]) and torch.equal(vv[:-1], c.rows[r][1][:-1]) and torch.equal(vv[-1], v[e])
+        _near(kk[-1:], want_k[e:e + 1], bound_k[e:e + 1], f"key of entry {e}")
+        o, ll = _exact(out[e:e + 1], torch.stack([kk, vv]), dim ** -0.5, held[r] - 1, window, sinks)
+        _check(seen[e:e + 1], lse[e:e + 1], o, ll, f"entry {e}")
+    c.ctx.close()
