@@ -159,14 +159,14 @@ __device__ __forceinline__ Work make_work(const PromptArgs &p, uint32_t k, uint3
 }
 
 // One warp hands the CTA's tiles out, a few ahead of the others, through a ring in shared memory.  `give(work)` returns
-// false when the CTA stops; `wanted(n)` tells whether the CTA's n-th tile is to be given.
+// false when the CTA stops; `wanted(n)` tells whether the CTA's n-th tile is to be given; `report`: bad entries are recorded (the first time).
 //   prefix: row blocks of the whole batch.
 //   up to 32 list entries: a lane per entry; tiles in descending order of their KV rounds over all entries, so that the
 //     long ones start first.  How many row blocks have R rounds or more has a closed form per entry, so the i-th of
 //     that order is found by bisection over R and a sum over the lanes, without a list.
 //   more: the list that prompt_plan_kernel wrote.
 template <bool PREFIX, bool WINDOW, class Wanted, class Give>
-__device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Wanted wanted, Give give)
+__device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, bool report, Wanted wanted, Give give)
 {
     const uint32_t lane = threadIdx.x % 32, per = p.a.kv_heads * p.splits;
     if (PREFIX) {
@@ -191,7 +191,7 @@ __device__ __forceinline__ void hand_out(const Geom &g, const PromptArgs &p, Wan
                 nq = q1 - q0;
                 blocks = (nq * p.group + kRows - 1) / kRows;      // total_q * q_heads < 2^31
                 if (nq) top = (held + kKv - 1) / kKv;
-            } else if (blockIdx.x == 0) {
+            } else if (report && blockIdx.x == 0) {
                 record_error(g.st, AVMP_DEV_BAD_REQUEST);
             }
         }
@@ -460,11 +460,11 @@ attn_tile_kernel(const Geom g, const PromptArgs p, const __grid_constant__ CUten
                 return true;
             };
             Work none = {};
-            hand_out<PREFIX, WINDOW>(g, p, [](uint32_t) { return true; }, give);
+            hand_out<PREFIX, WINDOW>(g, p, true, [](uint32_t) { return true; }, give);
             if (!PREFIX) {
                 give(none);
                 bar_sync(kRowsBar, kRowsBarThreads);
-                if (*(volatile uint32_t *)&any_redo) hand_out<PREFIX, WINDOW>(g, p, [&](uint32_t i) { return (redo[i % kRedo / 32] >> (i % 32) & 1) != 0; }, give);
+                if (*(volatile uint32_t *)&any_redo) hand_out<PREFIX, WINDOW>(g, p, false, [&](uint32_t i) { return (redo[i % kRedo / 32] >> (i % 32) & 1) != 0; }, give);
             }
             none.end = true;
             give(none);
