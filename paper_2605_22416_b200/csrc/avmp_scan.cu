@@ -79,6 +79,17 @@ __device__ __forceinline__ float2 softplus2(float2 x)
     return unpack2(fma2(y, e, pack2(ramp(x.x), ramp(x.y))));
 }
 
+// 2^x h + s of a pair, 2^x being the decay of a whole run.  By itself that may pass the range of 32 bits where the product does not, and would make NaN
+// of a zero or an infinity then.  So it is taken as two factors, the second being 1 up to 2^+-125 (both within the range: together up to
+// 2^+-250, from where on all but zeros, infinities and numbers below 2^-122 have left it).
+__device__ __forceinline__ unsigned long long over_run(unsigned long long h, float2 x, unsigned long long s)
+{
+    x = make_float2(fminf(fmaxf(x.x, -250.f), 250.f), fminf(fmaxf(x.y, -250.f), 250.f));
+    const float2 near = make_float2(fminf(fmaxf(x.x, -125.f), 125.f), fminf(fmaxf(x.y, -125.f), 125.f));
+    const unsigned long long far = pack2(exp2_approx(x.x - near.x), exp2_approx(x.y - near.y));
+    return fma2(pack2(exp2_approx(near.x), exp2_approx(near.y)), mul2(far, h), s);
+}
+
 // ---------------------------------------------------------------- whole prompts
 // One CTA per (request, CB channels of a group, run of tokens), of eight warps.  Four scan: a lane has S states of a channel, Q = states / S lanes
 // share a channel (lane q * 32 / Q + c has part q of channel c), and a warp works token by token; sums over the states are put together
@@ -294,10 +305,7 @@ __global__ void __launch_bounds__(kBoth, 2) scan_prompt_kernel(const Geom g, con
         for (uint32_t j = 1; j <= run; ++j) {
             const unsigned long long d2 = both(ws_sum(j)[mych]);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const float2 e = unpack2(mul2(A[p], d2));
-                h[p] = fma2(pack2(exp2_approx(e.x), exp2_approx(e.y)), h[p], pairs(ws_state(j))[p]);
-            }
+            for (int p = 0; p < P; ++p) h[p] = over_run(h[p], unpack2(mul2(A[p], d2)), pairs(ws_state(j))[p]);
         }
     }
     __syncthreads();

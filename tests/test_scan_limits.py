@@ -1,0 +1,59 @@
+"""Selective scan where decays, states or rows reach the ends of the 32-bit range, and what a missing row means there."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+from test_conv_scan import _fill, _inside, _model, _scan_exact, _scan_inputs
+from test_ssm_ops import _ctx, _i32, _states
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("n,d", [(1, 16), (20, 256)])
+def test_decay_of_a_whole_run_passes_the_range(dtype, n, d):
+    """Prompts that are cut into runs, with steps of 1 for 80 tokens, 0 for the others: the product of a run's decays is e^(80 A), as much as 2^173 or
+    as little as 2^-173.  States are what they are token by token: zeros stay zeros, infinities infinities, and small or large ones come into or stay
+    within the range.  Inputs are zero, so that nothing is added."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, states, most = getattr(torch, dtype), 16, 3000 if n == 1 else 500
+    m = _model(d, states, 2, layers=1)
+    ctx = _ctx(m, n, range(n))
+    gen = torch.Generator("cuda").manual_seed(d)
+    st, cv = _fill(ctx, 0, range(n), m, gen, dt)
+    a = torch.full((d, states), 0.25, device="cuda")
+    a[:, 1::4], a[:, 2::4], a[:, 3::4] = -0.25, 1.5, -1.5
+    st = st.view(n, d, states)
+    st[:, 0::4] = 0
+    st[:, 1::4] = math.inf
+    st[:, 2::4, 2::4] *= 1e-30                          # times 2^173: within the range again
+    st[:, 2::4, 3::4] *= 1e30                           # times 2^-173: still within it
+    st[:, 3::4, 2::4], st[:, 3::4, 3::4] = 1e20, 1e-20  # out of it, at either end
+    ctx.scatter_ssm(0, _i32(range(n)), n, st.reshape(n, -1), cv)
+    tot = n * most
+    step = torch.zeros(tot, d, dtype=dt, device="cuda")
+    for e in range(n):
+        step[e * most + 5: e * most + 85] = 1           # (in the first of the runs, which take 128 tokens or more)
+    zeros = torch.zeros(tot, d, dtype=dt, device="cuda")
+    bc = torch.randn(tot, 2 * states, device="cuda", generator=gen).to(dt)
+    desc = B.scan_desc(channels=d, groups=1, states=states, softplus=False, dtype=dt, b_stride_bytes=4 * states, c_stride_bytes=4 * states)
+    size = ctx.scan_workspace_bytes(desc, n, tot)
+    assert size > 0
+    ws, out = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda"), torch.empty(tot, d, dtype=dt, device="cuda")
+    ctx.scan_prompt(0, desc, _i32(range(n)), n, _i32(np.arange(n + 1) * most), tot, _i32([1] * n), zeros, step, bc, bc[:, states:], None, a, None, None,
+                    out, ws, size)
+    got = _states(ctx, 0, range(n), m)[0].view(n, d, states)
+    want = st.double() * (80 * a.double()).exp()
+    # 80 exponentials, their argument's roundings, the sum of steps, a rounding a token; and once more of the product of decays, in four parts
+    bound = want.abs() * (80 * 2.0 ** -22 + 80 * a.double().abs() * 2.0 ** -21 + (80 + 8) * 2.0 ** -23) + 2.0 ** -126
+    assert (got[:, 0::4] == 0).all() and (got[:, 1::4] == math.inf).all()
+    large = torch.isfinite(want) & (want.abs() > torch.finfo(torch.float32).max)
+    assert (got[large] == math.inf).all() and large.any()
+    rest = torch.isfinite(want) & ~large
+    assert float(((got.double() - want).abs() - bound)[rest].max()) <= 0
+    assert (want[:, 2::4, 3::4].abs() > 1e-30).any()
+    assert (out[:, 0::4] == 0).all() and ctx.stats()["error_count"] == 0
+    ctx.close()
