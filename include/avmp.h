@@ -479,7 +479,7 @@ AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_d
  * An exponential is off by 2^-22 of its value at most and by 3e-8 on the mean where a state decays slowly, always to the same side; that adds up
  * over the tokens that a state remembers: about 8e-6 of it where they are up to a thousand, 2e-4 where they are twenty thousand.
  * A: fp32 [channels][states], 16-byte aligned, finite (at most 0 where steps are positive, or states grow without bound); D and delta_bias: fp32
- * [channels] or NULL (0); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state; the decay of a
+ * [channels] or NULL (without that term); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state; the decay of a
  * single token that is beyond the range of fp32 counts as an infinity (which makes NaN of a zero state).
  * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups up to 2^24, ssm_state_elems = channels *
  * states; else AVMP_EINVAL.  With softplus a delta of -inf or of the type's lowest value leaves the state as it was.  The convolution window of the block is not touched. */

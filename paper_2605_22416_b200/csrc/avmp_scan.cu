@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(kStep, 3) scan_step_kernel(const Geom g, const
 #pragma unroll
             for (uint32_t o = 0; o < OWN; ++o) {
                 const uint32_t ch = channel(j0 + o);
-                float x = fmaf(skip[o], u[o], v[o]);
+                float x = a.skip ? fmaf(skip[o], u[o], v[o]) : v[o];
                 if (a.z) x *= silu(row(2, ch));
                 if (finishes && ch < chs) *reinterpret_cast<uint16_t *>(a.out + k * a.os + (ch0 + ch) * 2) = (uint16_t)T::pack(x, 0.f);
             }

@@ -57,3 +57,34 @@ def test_decay_of_a_whole_run_passes_the_range(dtype, n, d):
     assert (want[:, 2::4, 3::4].abs() > 1e-30).any()
     assert (out[:, 0::4] == 0).all() and ctx.stats()["error_count"] == 0
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", [8, 16, 64])
+def test_infinite_rows_without_the_skip_term(states):
+    """Without D an infinite row is seen through the state alone, by single tokens as by prompts: there is no 0 * infinity."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, d = torch.bfloat16, 40
+    m = _model(d, states, 2, layers=1)
+    ctx = _ctx(m, 2, [0, 1])
+    gen = torch.Generator("cuda").manual_seed(states)
+    st, cv = _fill(ctx, 0, [0, 1], m, gen, dt)
+    st[1] = st[0]
+    ctx.scatter_ssm(0, _i32([0, 1]), 2, st, cv)
+    u, delta = (torch.randn(1, d, device="cuda", generator=gen).to(dt) for _ in range(2))
+    b, c = (torch.rand(1, states, device="cuda", generator=gen).to(dt) + 0.5 for _ in range(2))
+    u[0, 3], u[0, 17], u[0, 39] = math.inf, -math.inf, math.inf
+    a = -torch.rand(d, states, device="cuda", generator=gen) - 0.1
+    desc = B.scan_desc(channels=d, groups=1, states=states, softplus=True, dtype=dt)
+    outs = [torch.empty(1, d, dtype=dt, device="cuda") for _ in range(2)]
+    ctx.scan_prompt(0, desc, _i32([0]), 1, _i32([0, 1]), 1, _i32([1]), u, delta, b, c, None, a, None, None, outs[0])
+    ctx.scan_step(0, desc, _i32([1]), 1, u, delta, b, c, None, a, None, None, outs[1])
+    hit = torch.isinf(u[0])
+    got, _ = _states(ctx, 0, [0, 1], m)
+    for o, h in zip(outs, got.view(2, d, states)):
+        assert torch.equal(o[0, hit].float(), u[0, hit].float()) and torch.equal(h[hit], u[0, hit].float()[:, None].expand(-1, states))
+        hh, err, y, bound = _scan_exact(st[0].view(d, states)[~hit], u[:, ~hit], delta[:, ~hit], b[:, None], c[:, None], None, a[~hit], None, None, True)
+        _inside(o[:, ~hit], y, bound, dt, "the others")
+        _inside(h[~hit], hh, err, None, "the others' states")
+    ctx.close()
