@@ -75,15 +75,14 @@ struct Taps {
 template <class T, int W, bool ACT>
 __global__ void __launch_bounds__(kCta) conv_prompt_kernel(const Geom g, const ConvArgs a, uint32_t rows)
 {
-    __shared__ uint32_t pre[kCta + 1];
-    __shared__ unsigned long long tmp[32];
+    __shared__ unsigned long long pre[kCta], tmp[32];
     __shared__ uint2 ring[kStages * kFly][kCta];
     pdl_prologue();
     const uint32_t ch = (blockIdx.x * kCta + threadIdx.x) * kCh, slot0 = smem_u32(&ring[0][threadIdx.x]);
     const bool mine = ch < a.channels;
     Taps<W> taps;
     if (mine) taps.load(a, ch);
-    Runs runs(a.cu, a.n, a.total, rows, pre, tmp);
+    Runs runs(a.cu, a.n, a.total, rows, a.total, pre, tmp);
     uint32_t k, run;
     for (unsigned long long i = blockIdx.y; runs.seek(i, &k, &run); i += gridDim.y) {
         const uint32_t r = a.reqs[k], c0 = a.cu[k], c1 = a.cu[k + 1];

@@ -45,19 +45,22 @@ __device__ __forceinline__ uint32_t named_before_each(const uint32_t *reqs, uint
     return *flags;
 }
 
-// The rows of all list entries, in runs of `rows` at most: an entry without rows, or with offsets that do not fit the buffers, has
-// one too, so that somebody looks after it.  A CTA walks them in ascending order; the entries' offsets pass through shared memory as
-// many at a time as the CTA has threads.
+// The rows of all list entries, in runs of `rows` at most: an entry without rows, with offsets that do not fit the buffers, or with more rows
+// than `most` has one too, so that somebody looks after it.  A CTA walks them in ascending order; the entries' offsets pass through shared
+// memory as many at a time as the CTA has threads.  (Offsets that swing to and fro may name the buffers' rows many times over: runs are
+// counted in 64 bits.)
 struct Runs {
     const uint32_t *cu;          // null: one row each
     uint32_t n, total, rows;
-    uint32_t *pre;               // shared, blockDim.x + 1
+    unsigned long long most;
+    unsigned long long *pre;     // shared, blockDim.x
     unsigned long long *tmp;     // shared, 32
     uint32_t k0, cnt;
     unsigned long long begin, end;
 
-    __device__ Runs(const uint32_t *cu_, uint32_t n_, uint32_t total_, uint32_t rows_, uint32_t *pre_, unsigned long long *tmp_)
-        : cu(cu_), n(n_), total(total_), rows(rows_), pre(pre_), tmp(tmp_), k0(0), cnt(0), begin(0), end(0) {}
+    __device__ Runs(const uint32_t *cu_, uint32_t n_, uint32_t total_, uint32_t rows_, unsigned long long most_, unsigned long long *pre_,
+                    unsigned long long *tmp_)
+        : cu(cu_), n(n_), total(total_), rows(rows_), most(most_), pre(pre_), tmp(tmp_), k0(0), cnt(0), begin(0), end(0) {}
     // Run i: its entry and its number there.  False behind the last one.  Whole CTA; i ascends from call to call.
     __device__ bool seek(unsigned long long i, uint32_t *k, uint32_t *run)
     {
@@ -73,15 +76,19 @@ struct Runs {
             unsigned long long mine = 0, all;
             if (threadIdx.x < cnt) {
                 const uint32_t c0 = cu[k0 + threadIdx.x], c1 = cu[k0 + threadIdx.x + 1];
-                mine = c1 > c0 && c1 <= total ? (c1 - c0 + rows - 1) / rows : 1u;
+                mine = c1 > c0 && c1 <= total && c1 - c0 <= most ? (c1 - c0 + rows - 1) / rows : 1u;
             }
             const unsigned long long incl = block_incl_scan(mine, tmp, &all);
-            pre[threadIdx.x] = (uint32_t)(incl - mine);
+            pre[threadIdx.x] = incl - mine;
             begin = end; end += all;
             __syncthreads();
         }
-        const uint32_t at = find_owner(pre, 0, cnt, 0, (uint32_t)(i - begin));
-        *k = k0 + at; *run = (uint32_t)(i - begin) - pre[at];
+        uint32_t lo = 0, hi = cnt;                 // the last entry that begins at run i or before
+        while (lo + 1 < hi) {
+            const uint32_t mid = (lo + hi) >> 1;
+            if (pre[mid] <= i - begin) lo = mid; else hi = mid;
+        }
+        *k = k0 + lo; *run = (uint32_t)(i - begin - pre[lo]);
         return true;
     }
 };

@@ -29,8 +29,7 @@ template <class T, int D, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs a, uint32_t rows)
 {
     constexpr uint32_t LANES = D / 8, HEADS = 32 / LANES;      // lanes of a head; heads a warp has at a time
-    __shared__ uint32_t pre[kCta + 1];
-    __shared__ unsigned long long tmp[32];
+    __shared__ unsigned long long pre[kCta], tmp[32];
     __shared__ uint4 ring[kStages * kSteps][kCta];
     __shared__ uint32_t flags;
     pdl_prologue();
@@ -47,7 +46,7 @@ __global__ void __launch_bounds__(kCta) rows_kernel(const Geom g, const RowsArgs
             *reinterpret_cast<uint2 *>(p + s * 2) = make_uint2(v.z, v.w);
         }
     };
-    Runs runs(a.cu, a.n, a.total, rows, pre, tmp);
+    Runs runs(a.cu, a.n, a.total, rows, (unsigned long long)g.max_pages * g.T, pre, tmp);
     uint32_t k, run;
     for (unsigned long long i = blockIdx.x;; i += gridDim.x) {
         // this warp's token: of a run of one entry, or of as many entries with one token each

@@ -313,3 +313,28 @@ def test_window_prompts_of_whole_tiles(dtype, n, hk, group, dim, page, window, s
     assert (out[cu[1]:cu[2]] == 7).all() and (lse[cu[1]:cu[2]] == 7).all() and (out[tot:] == 7).all() and (lse[tot:] == 7).all()
     assert c.ctx.stats()["error_count"] == 1
     c.ctx.close()
+
+
+@pytest.mark.gpu
+def test_rows_of_offsets_that_swing():
+    """Offsets that run over all of 2^28 rows and back, again and again: skipped items, whose runs together pass 2^32.  The one good entry behind
+    them is served."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dim, n, tot = 64, 129, (1 << 28) + 64
+    c = Cache([40] + [1] * (n - 1), 1, dim, 16, "bfloat16")
+    freq = torch.rand(dim // 2, device="cuda", generator=c.gen)
+    x, out = (torch.empty(tot, 1, dim, dtype=c.dt, device="cuda") for _ in range(2))
+    x[:64] = torch.randn(64, 1, dim, device="cuda", generator=c.gen).to(c.dt)
+    out[:64] = 7.0
+    cu = [0, tot] * (n // 2) + [0, 40]
+    reqs = list(range(1, n)) + [0]
+    desc = B.rows_desc(q_heads=1, rotary_dim=dim, neighbours=False, eps=1e-6, dtype=c.dt)
+    c.ctx.attn_rows_prompt(c.layer, desc, _i32(reqs), n, _i32(cu), tot, None, x, x, x, None, None, freq, out)
+    assert c.ctx.stats()["error_count"] == n - 1
+    want, bound = _rotated(x[:40], None, 0, torch.arange(40, device="cuda"), freq, False)
+    _near(out[:40], want, bound, "queries")
+    assert (out[40:64] == 7).all() and torch.equal(_cached(c, 0)[1], x[:40])
+    c.ctx.close()
+    del x, out
+    torch.cuda.empty_cache()
