@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t named_before_each(const uint32_t *reqs, uint
 // memory as many at a time as the CTA has threads.  (Offsets that swing to and fro may name the buffers' rows many times over: runs are
 // counted in 64 bits.)
 struct Runs {
-    const uint32_t *cu;          // null: one row each
+    const uint32_t *cu;
     uint32_t n, total, rows;
     unsigned long long most;
     unsigned long long *pre;     // shared, blockDim.x
@@ -64,10 +64,6 @@ struct Runs {
     // Run i: its entry and its number there.  False behind the last one.  Whole CTA; i ascends from call to call.
     __device__ bool seek(unsigned long long i, uint32_t *k, uint32_t *run)
     {
-        if (!cu) {
-            *k = (uint32_t)i; *run = 0;
-            return i < n;
-        }
         while (i >= end) {
             if (k0 + cnt >= n) return false;
             k0 += cnt;
