@@ -278,7 +278,7 @@ def test_rows_of_many_single_tokens(dtype, n, hk, group, dim, neighbours):
 # ---------------------------------------------------------------- window
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("n,hk,group,dim,page", [(12, 8, 4, 128, 16), (40, 2, 8, 128, 32), (9, 16, 3, 64, 8)])
+@pytest.mark.parametrize("n,hk,group,dim,page", [(12, 8, 4, 128, 16), (40, 2, 8, 128, 32), (9, 16, 3, 64, 8), (10, 4, 8, 64, 24)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (60, 5), (257, 129), (1024, 4), (1 << 20, 1)])
 def test_window_prompts_of_whole_tiles(dtype, n, hk, group, dim, page, window, sinks):
     """Enough tiles for all SMs, so that none is split: up to 32 requests handed out without a list, more with one.  What no row of a request sees
