@@ -7,9 +7,9 @@
 // a lane has 8 columns of a head such that both columns of every pair are its own, so that a rotation needs no exchange, and
 // weights, sines and cosines, multiplied once, serve all heads of the token from registers.  Angles are taken in 64 bits: 2^-24 of a far
 // position's angle would be thousandths of a turn.  Heads come through a ring in shared memory by asynchronous copies, a lane's own columns for
-// itself: with loads into registers too little is on its way (112 us for what takes 82 so).
+// itself: with loads into registers too little is on its way (112 us for what took 82 so).
 //
-// Measured (heads of 128, 8 KV heads): 12 turns of 256 to 2048 tokens, 64 query heads, 82 us (79 % of the measured copy rate; 61 % of the issue slots
+// Measured (heads of 128, 8 KV heads): 12 turns of 256 to 2048 tokens, 64 query heads, 78 us (83 % of the measured copy rate; 61 % of the issue slots
 // are taken, 29 % of the warps' places: a token's look-ups take 2 to 3 us before its first head goes out); one token for 1024 requests,
 // 32 query heads, 11 (floor 3.8), for 32 requests 5.
 #include "avmp_lists.cuh"

@@ -4,9 +4,9 @@
 //
 // scan_prompt_kernel   whole prompts.  Bound by the exponentials: one per token, channel and state, of which the special-function unit gives
 //                      16 a cycle and SM, and three more per token and channel; the rows are 8 bytes a channel.  Measured (16 states): 32 prompts of
-//                      1000 tokens, 8192 channels, 1 400 us (that unit is busy 77 % of the time, 61 % of the issue slots are taken; bytes alone
-//                      322); one of 4096 tokens 258 (60 %: 256 CTAs on 148 SMs, two warps of the scan to a scheduler); 32 of 32 to 512
-//                      tokens, 2048 channels, 83.  An eighth of the exponentials as polynomials on the multiply-add pipe 3 % slower, a quarter 8 %:
+//                      1000 tokens, 8192 channels, 1 414 us (that unit is busy 76 % of the time, 61 % of the issue slots are taken; bytes alone
+//                      322); one of 4096 tokens 258 (61 %: 256 CTAs on 148 SMs, two warps of the scan to a scheduler); 32 of 32 to 512
+//                      tokens, 2048 channels, 84.  An eighth of the exponentials as polynomials on the multiply-add pipe 3 % slower, a quarter 8 %:
 //                      the issue slots are short too.
 // scan_step_kernel     one token per request: bound by HBM, every state element is read and written once.  1 GB of state 395 to 415 us (84 to 88 % of
 //                      the measured copy rate); 32 requests of 128 KB 4.6 (latency).
