@@ -483,7 +483,8 @@ AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_d
  * [channels] or NULL (without that term); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state; the decay of a
  * single token that is beyond the range of fp32 counts as an infinity (which makes NaN of a zero state).
  * Supported: ssm_elem_bytes 4, states 8, 16, 32 or 64, channels a multiple of 8 * groups up to 2^24, ssm_state_elems = channels *
- * states; else AVMP_EINVAL.  With softplus a delta of -inf or of the type's lowest value leaves the state as it was.  The convolution window of the block is not touched. */
+ * states; else AVMP_EINVAL.  With softplus a delta of -inf or of the type's lowest value leaves the state as it was (u and b
+ * of that token being finite: what is added is 0 times their product).  The convolution window of the block is not touched. */
 typedef struct {
     uint32_t type, channels, groups, states, softplus;
     uint32_t rsvd;             /* 0 */
