@@ -477,8 +477,8 @@ AVMP_API int avmp_conv_step(avmp_ctx *ctx, uint32_t ssm_layer, const avmp_conv_d
  *     h <- exp(step * A) h + step * u_t * B_t,   y = <C_t, h> + D * u_t,   out_t = y * z_t / (1 + exp(-z_t)).
  * Rows: u, delta, z and out [channels], b and c [groups][states]; channel i reads group i / (channels / groups).
  * A decay exp(step * A) is off by 2^-22 (1 + |step * A|) of its value at most, and 0 below 2^-126.  In a state this adds up over the tokens that
- * it remembers: 5e-6 of it on the mean where they are a thousand, 1.4e-4 where they are twenty thousand (always to the same side); where
- * steps are all alike as much as 9e-5 and 1.7e-3 (exponentials exact but for their rounding to 32 bits: 4e-5 and 7e-4).
+ * it remembers: 3e-6 of it on the mean where they are a thousand, 2.2e-5 where they are twenty thousand; where steps are all alike as much
+ * as 9e-5 and 1.6e-3 (exponentials exact but for their rounding to 32 bits: 4e-5 and 7e-4).
  * A: fp32 [channels][states], 16-byte aligned, finite (at most 0 where steps are positive, or states grow without bound); D and delta_bias: fp32
  * [channels] or NULL (without that term); z NULL: out_t = y.  A NaN or an infinity in a channel's rows or state stays in that channel's state; the decay of a
  * single token that is beyond the range of fp32 counts as an infinity (which makes NaN of a zero state).

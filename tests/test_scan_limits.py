@@ -88,3 +88,57 @@ def test_infinite_rows_without_the_skip_term(states):
         _inside(o[:, ~hit], y, bound, dt, "the others")
         _inside(h[~hit], hh, err, None, "the others' states")
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("call", ["prompt", "step"])
+def test_mean_error_of_a_decay(call):
+    """What a state loses or gains by one token's decay, on the mean over a million states: a part of 5e-9 at most for exponents of 2^-13 to 2^-9 (the
+    instruction by itself 6e-9 too little), 1.8e-8 for 2^-7.5 to 2^-1 (by itself 2.1e-8 too little).  A rounding of the state is 3e-8 at most and to
+    either side: 3e-11 on the mean."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, d, states, n = torch.bfloat16, 4096, 16, 16
+    m = _model(d, states, 2, layers=1)
+    ctx = _ctx(m, n, range(n))
+    gen = torch.Generator("cuda").manual_seed(3)
+    zeros, ones = torch.zeros(n, d, dtype=dt, device="cuda"), torch.ones(n, d, dtype=dt, device="cuda")
+    bc, out = torch.ones(n, states, dtype=dt, device="cuda"), torch.empty(n, d, dtype=dt, device="cuda")
+    desc = B.scan_desc(channels=d, groups=1, states=states, softplus=False, dtype=dt)
+    ws, size = torch.empty(max(16, ctx.scan_workspace_bytes(desc, n, n)), dtype=torch.uint8, device="cuda"), ctx.scan_workspace_bytes(desc, n, n)
+    for lo, hi, most in ((-13.0, -9.0, 5e-9), (-7.5, -1.0, 1.8e-8)):
+        a = -torch.exp2(lo + (hi - lo) * torch.rand(d, states, device="cuda", generator=gen)) * math.log(2)
+        st = torch.rand(n, d, states, device="cuda", generator=gen) + 0.5
+        ctx.scatter_ssm(0, _i32(range(n)), n, st.reshape(n, -1), torch.zeros(n, m.ssm_conv_elems, device="cuda"))
+        rows = (zeros, ones, bc, bc, None, a, None, None, out)
+        if call == "prompt":
+            ctx.scan_prompt(0, desc, _i32(range(n)), n, _i32(range(n + 1)), n, _i32([1] * n), *rows, ws, size)
+        else:
+            ctx.scan_step(0, desc, _i32(range(n)), n, *rows)
+        want = st.double() * a.double().exp()
+        off = float(((_states(ctx, 0, range(n), m)[0].view(n, d, states).double() - want) / want).mean())
+        assert abs(off) <= most, (lo, hi, off)
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,most", [(300, 2.5e-6), (20000, 6e-5)])
+def test_slow_states_on_the_mean(tokens, most):
+    """States that remember `tokens` tokens (0.7 to 1.4 times as many), fed with ones: on the mean they are off by the decays' mean error as many
+    times, 3e-9 at most where that is 20 000, 8e-9 for 300."""
+    import torch
+    from paper_2605_22416_b200 import binding as B
+    dt, d, states, total = torch.bfloat16, 4096, 16, tokens * 2
+    m = _model(d, states, 2, layers=1)
+    ctx = _ctx(m, 1, [0])
+    a = -1 / torch.linspace(0.7 * tokens, 1.4 * tokens, d * states, device="cuda").view(d, states)
+    ones, bc = torch.ones(total, d, dtype=dt, device="cuda"), torch.ones(total, states, dtype=dt, device="cuda")
+    desc = B.scan_desc(channels=d, groups=1, states=states, softplus=False, dtype=dt)
+    size = ctx.scan_workspace_bytes(desc, 1, total)
+    ws = torch.empty(max(16, size), dtype=torch.uint8, device="cuda")
+    ctx.scan_prompt(0, desc, _i32([0]), 1, _i32([0, total]), total, None, ones, ones, bc, bc, None, a, None, None, torch.empty_like(ones), ws, size)
+    decay = a.double().exp()
+    want = (1 - decay ** total) / (1 - decay)
+    off = float(((_states(ctx, 0, [0], m)[0].view(d, states).double() - want) / want).mean())
+    assert abs(off) <= most, off
+    ctx.close()
